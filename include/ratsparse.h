@@ -64,7 +64,8 @@ enum {
     RS_WORKSPACE_TOO_SMALL = 3, /* ws == NULL or ws_bytes below what the entry point needs */
     RS_LAUNCH_FAILED = 4,       /* hipGetLastError() after a launch */
     RS_ASYNC_TIMEOUT = 5,       /* reported by ratsparse_async_status(): a bounded in-kernel wait expired */
-    RS_SCRATCH_LIMIT = 6        /* sparse_attn_decode_static: the shape needs more than RS_STATIC_SCRATCH_BYTES */
+    RS_SCRATCH_LIMIT = 6,       /* sparse_attn_decode_static: the shape needs more than RS_STATIC_SCRATCH_BYTES */
+    RS_POOL_REFUSED = 7         /* reported by ratsparse_async_status(): a page_pool call found too few free pages, or a sequence it cannot take */
 };
 
 enum { RS_F32 = 0, RS_BF16 = 1 };
@@ -93,7 +94,8 @@ const char *ratsparse_version(void);
 int32_t ratsparse_workspace_init(void *ws, size_t ws_bytes, void *stream);
 
 /* Waits for `stream`, then returns RS_OK, or RS_ASYNC_TIMEOUT if a kernel that used
- * `ws` gave up a bounded wait (its outputs are then undefined); clears the record. */
+ * `ws` gave up a bounded wait (its outputs are then undefined), or RS_POOL_REFUSED if a page_pool call
+ * that used it changed nothing; clears the record. */
 int32_t ratsparse_async_status(void *ws, void *stream);
 
 /* Measurement aid (no part of the method): enqueue a plain streaming read of `bytes` bytes at
@@ -347,6 +349,109 @@ int32_t snapkv_compress_lse(const rs_shape *s, const void *q_win, const void *k_
                             int32_t pool_kernel, float scale, const float *lse_win, void *kc_out,
                             void *vc_out, int64_t Tcap_out, int32_t *idx_out, float *votes_out,
                             void *ws, size_t ws_bytes, void *stream);
+
+/* ---- Sequences in a pool of pages -------------------------------------------------------
+ * Not in the paper; offered for serving many sequences of different lengths, some of which begin alike.
+ * A pool is one layer's cache without a batch: for every KV head N pages of P rows,
+ *   k_pool, v_pool [Hkv, N P, D] dtype, meta [Hkv, N, 2, D] dtype (Quest page bounds) or NULL
+ * described by an rs_shape with Tcap = N P.  (A batch entry of a contiguous cache is a pool of
+ * Tcap / P pages, so page_copy also moves rows between the two.)  Which sequence holds which page is kept
+ * once for all layers, in device memory of the caller:
+ *   table [S, M] int32   page of the sequence's tokens j P .. j P + P - 1; -1 where there is none
+ *   len   [S]    int32   tokens of the sequence (0: an empty row)
+ *   refs  [N]    int32   how many sequences hold the page; 0: it is free
+ * A new pool: table filled with -1, len and refs with 0.  Every sequence's full pages may be held by others
+ * too, a partly filled last page is its own; the calls below keep it so.  A list names each sequence once.
+ * page_pool_reserve, _fork and _free are decided as a whole on the device: if one entry cannot be taken (a
+ * sequence out of range or listed twice, more tokens than M pages hold, too few free pages) nothing at all
+ * changes, and ratsparse_async_status() answers RS_POOL_REFUSED.  None keeps state on the host: all calls of this
+ * section may be captured into a graph and replayed. */
+typedef struct rs_pool {
+    int32_t N; /* pages of the pool; N P < 2^31 */
+    int32_t S; /* sequences (rows of the table), at most 32768 */
+    int32_t M; /* pages a sequence can hold; M P < 2^31 */
+    int32_t P; /* tokens a page: 16, 32, 64, 128, 256 or 512 */
+} rs_pool;
+
+size_t page_pool_workspace_bytes(const rs_pool *p);
+
+/* Room for new tokens: sequence seq[i] gets the pages that len + want[i] tokens need beyond those it holds, and len grows by
+ * want[i].  The pages are the lowest numbered free ones, ascending in the order of the list.
+ *   seq [n] int32;  want [n] int32 or NULL: T_new for each (0 is allowed)
+ *   granted [n] int32 or NULL: want[i], or 0 for all where the call is refused; what rat_append_paged and
+ *                              attn_paged take as n_new, so that after a refusal they do nothing */
+int32_t page_pool_reserve(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, const int32_t *seq, int32_t n,
+                          const int32_t *want, int32_t T_new, int32_t *granted, void *ws, size_t ws_bytes, void *stream);
+
+/* dst[i] becomes a copy of src[i]: it holds the same full pages, and a page of its own for a partly filled last
+ * one.  Every dst has to be empty and in neither list again; a src may be named several times.
+ *   pairs_out [n, 2] int32: (page, its copy's page), (-1, -1) where the last page is full or there is none:
+ *                           what page_copy takes, once for every layer
+ *   carry_out [n, 2] int32 or NULL: (src, dst): what rat_state_copy takes.  All -1 where the call is refused */
+int32_t page_pool_fork(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, const int32_t *src, const int32_t *dst,
+                       int32_t n, int32_t *pairs_out, int32_t *carry_out, void *ws, size_t ws_bytes, void *stream);
+
+/* The listed sequences give up their pages and become empty. */
+int32_t page_pool_free(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, const int32_t *seq, int32_t n, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/* The pages in use move to the front: with L of them, those numbered L and above go, in order, to the free ones below L; table
+ * and refs follow.  The pages from L on are then one free run (for a pool that is to give memory back, or to take
+ * a prompt's cache as one piece).  Never refused.
+ *   pairs_out [N / 2, 2] int32 (at least one entry): (page, where it went) in ascending order, then (-1, -1): for page_copy, once
+ *                        for every layer, before anything else writes into the pool
+ *   n_pairs_out [1] int32: how many there are */
+int32_t page_pool_compact(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, int32_t *pairs_out, int32_t *n_pairs_out,
+                          void *ws, size_t ws_bytes, void *stream);
+
+/* Which neighbours of a list begin with the same pages: the list is cut into runs in which every sequence has at least
+ * min_pages (>= 1) leading full pages in common with the one before it.
+ *   share_out [n, 3] int32: for every sequence its run's first place in the list, the run's length, and the pages that all of it
+ *                           share (the fewest that two neighbours do; 0 for a run of one)
+ * It stays right while the sequences only grow; a fork, a release or a compaction of one of them calls for a new one.
+ * n <= 1024 (RS_UNSUPPORTED above).  A sequence out of range shares nothing. */
+int32_t page_pool_share(const rs_pool *p, const int32_t *table, const int32_t *len, const int32_t *seq, int32_t n, int32_t min_pages,
+                        int32_t *share_out, void *stream);
+
+/* Copies pages of every KV head, with their bounds: page pairs[i][0] of the source pool to page pairs[i][1] of the destination.
+ * The two shapes agree in Hkv, D, P and dtype and may differ in Tcap; B counts for nothing (for a batch
+ * entry of a contiguous cache hand in that entry's pointers).  No page may be written twice, or both read and written.
+ *   pairs [n, 2] int32; a pair with a page outside its pool (-1) is passed over
+ *   n_pairs [1] int32 on the device or NULL: how many of the n count (page_pool_compact's)
+ *   meta_src, meta_dst: both or neither */
+int32_t page_copy(const rs_shape *s_src, const void *k_src, const void *v_src, const void *meta_src, const rs_shape *s_dst,
+                  void *k_dst, void *v_dst, void *meta_dst, const int32_t *pairs, int32_t n, const int32_t *n_pairs, void *stream);
+
+/* Copies the carries state_k, state_v [S, Hkv, D] float32 of sequence pairs[i][0] to sequence pairs[i][1]; a pair with a number
+ * outside 0 .. S - 1 is passed over; no sequence may be written twice, or both read and written. */
+int32_t rat_state_copy(const rs_shape *s, float *state_k, float *state_v, int32_t S, const int32_t *pairs, int32_t n, void *stream);
+
+/* rat_scan's append through the table: the last n_new[i] tokens of sequence seq[i], which page_pool_reserve has made room for
+ * (positions len - n_new[i] .. len - 1).  Sequences may hold different numbers of them.
+ *   k, v [B, Hkv, T_new, D] dtype, g [B, Hkv, T_new, D] float32, B = s->B listed sequences; what lies past n_new[i] tokens is not read
+ *   state_k, state_v [S, Hkv, D] float32, rows by sequence number, as in rat_scan
+ *   meta: the bounds of every page that gets a row are brought up to date, or NULL
+ *   n_new [B] int32 or NULL: T_new for each; counts above T_new are taken as T_new, below 0 as 0
+ * Nothing is done for a sequence out of range, listed before, or with fewer than n_new tokens; rows whose table entry names
+ * no page are not written.  Long prompts are better scanned as contiguous rows (rat_scan) and copied into their pages. */
+int32_t rat_append_paged(const rs_shape *s, const rs_pool *p, const void *k, const void *v, const float *g, float *state_k,
+                         float *state_v, void *k_pool, void *v_pool, void *meta, const int32_t *table, const int32_t *len,
+                         const int32_t *seq, const int32_t *n_new, int32_t T_new, void *stream);
+
+/* Dense attention (Eq. 4 with every token) of the newest tokens of B = s->B listed sequences, each over its own pages: the query of
+ * token i, at position len - n_new + i, sees the positions up to its own.
+ *   q   [B, Hq, T_new, D] dtype; rows past n_new[b] are not read
+ *   out [B, Hq, T_new, D] dtype, lse_out [B, Hq, T_new] float32 or NULL; rows past n_new[b] are left as they were; a row that sees
+ *       nothing (a sequence out of range or shorter than n_new) gets zeros and a log-sum-exp of -inf
+ *   n_new [B] int32 or NULL: T_new for each (clipped to 0 .. T_new)
+ *   share [B, 3] int32 or NULL: as page_pool_share writes it for the same list: a run's common pages are read once for all its
+ *       sequences.  Its values are taken on trust in one respect: the first sequence's pages are used for the
+ *       whole run.  A table entry that names no page hides its tokens.
+ * B <= 1024.  Workspace: attn_paged_workspace_bytes().  Results do not depend on the order in which workgroups finish. */
+size_t attn_paged_workspace_bytes(const rs_shape *s, const rs_pool *p, int32_t T_new);
+int32_t attn_paged(const rs_shape *s, const rs_pool *p, const void *q, const void *k_pool, const void *v_pool, const int32_t *table,
+                   const int32_t *len, const int32_t *seq, const int32_t *n_new, int32_t T_new, const int32_t *share, float scale,
+                   void *out, float *lse_out, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -28,9 +28,13 @@ class rs_shape(ctypes.Structure):
                 ("dtype", ctypes.c_int32)]
 
 
+class rs_pool(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("S", ctypes.c_int32), ("M", ctypes.c_int32), ("P", ctypes.c_int32)]
+
+
 _vp, _i64, _i32, _f32, _sz = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
                               ctypes.c_size_t)
-_shp = ctypes.POINTER(rs_shape)
+_shp, _pool = ctypes.POINTER(rs_shape), ctypes.POINTER(rs_pool)
 
 # every symbol include/ratsparse.h declares: name -> (restype, argtypes)
 SIGNATURES = {
@@ -71,6 +75,17 @@ SIGNATURES = {
                                _vp, _vp, _vp, _sz, _vp]),
     "snapkv_compress_lse": (_i32, [_shp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _i64,
                                    _vp, _vp, _vp, _sz, _vp]),
+    "page_pool_workspace_bytes": (_sz, [_pool]),
+    "page_pool_reserve": (_i32, [_pool, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _sz, _vp]),
+    "page_pool_fork": (_i32, [_pool, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "page_pool_free": (_i32, [_pool, _vp, _vp, _vp, _vp, _i32, _vp, _sz, _vp]),
+    "page_pool_compact": (_i32, [_pool, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "page_pool_share": (_i32, [_pool, _vp, _vp, _vp, _i32, _i32, _vp, _vp]),
+    "page_copy": (_i32, [_shp, _vp, _vp, _vp, _shp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "rat_state_copy": (_i32, [_shp, _vp, _vp, _i32, _vp, _i32, _vp]),
+    "rat_append_paged": (_i32, [_shp, _pool, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp]),
+    "attn_paged_workspace_bytes": (_sz, [_shp, _pool, _i32]),
+    "attn_paged": (_i32, [_shp, _pool, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _f32, _vp, _vp, _vp, _sz, _vp]),
 }
 
 
@@ -134,6 +149,11 @@ def _dtype_code(t):
 def make_shape(B, Hq, Hkv, D, Tcap, P, dtype):
     code = dtype if isinstance(dtype, int) else (RS_BF16 if dtype == torch.bfloat16 else RS_F32)
     return rs_shape(B, Hq, Hkv, D, Tcap, P, code)
+
+
+def make_pool(N, S, M, P):
+    """N pages of P tokens, rows for S sequences of at most M pages."""
+    return rs_pool(N, S, M, P)
 
 
 class Workspace:
@@ -287,3 +307,104 @@ def snapkv_compress_lse(s, q_win, k_cache, v_cache, T, W, K_keep, pool_kernel, s
     _check(load().snapkv_compress_lse(ctypes.byref(s), _ptr(q_win), _ptr(k_cache), _ptr(v_cache), T, W,
                                       K_keep, pool_kernel, scale, _ptr(lse_win), _ptr(kc_out), _ptr(vc_out),
                                       Tcap_out, _ptr(idx_out), _ptr(votes_out), ws.ptr, ws.nbytes, _stream()))
+
+
+# ---- sequences in a pool of pages: the tensors' shapes and types are looked at here, since the kernels go by them ----
+
+
+def _need(t, dtype, *shape):
+    """The address of a device tensor of this type and shape on the current device; None: null."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise RatsparseError("a %s tensor of shape %s is needed, not %s %s" % (dtype, shape, t.dtype, tuple(t.shape)))
+    p = _ptr(t)
+    if t.get_device() != torch.cuda.current_device():
+        raise RatsparseError("the tensors have to be on the current device")
+    return p
+
+
+def _sequences(p, table, len, refs):
+    return (_need(table, torch.int32, p.S, p.M), _need(len, torch.int32, p.S), _need(refs, torch.int32, p.N))
+
+
+def _rows(s, k, v, meta):
+    """Addresses of a pool's (or one batch entry's) rows and bounds."""
+    dt = torch.bfloat16 if s.dtype == RS_BF16 else torch.float32
+    return (_need(k, dt, s.Hkv, s.Tcap, s.D), _need(v, dt, s.Hkv, s.Tcap, s.D), _need(meta, dt, s.Hkv, s.Tcap // s.P, 2, s.D))
+
+
+def page_pool_workspace_bytes(p):
+    return load().page_pool_workspace_bytes(ctypes.byref(p))
+
+
+def page_pool_reserve(p, table, len, refs, seq, want, T_new, granted, ws):
+    n = seq.numel()
+    _check(load().page_pool_reserve(ctypes.byref(p), *_sequences(p, table, len, refs), _need(seq, torch.int32, n), n,
+                                    _need(want, torch.int32, n), T_new, _need(granted, torch.int32, n), ws.ptr, ws.nbytes,
+                                    _stream()))
+
+
+def page_pool_fork(p, table, len, refs, src, dst, pairs_out, carry_out, ws):
+    n = src.numel()
+    _check(load().page_pool_fork(ctypes.byref(p), *_sequences(p, table, len, refs), _need(src, torch.int32, n),
+                                 _need(dst, torch.int32, n), n, _need(pairs_out, torch.int32, n, 2),
+                                 _need(carry_out, torch.int32, n, 2), ws.ptr, ws.nbytes, _stream()))
+
+
+def page_pool_free(p, table, len, refs, seq, ws):
+    n = seq.numel()
+    _check(load().page_pool_free(ctypes.byref(p), *_sequences(p, table, len, refs), _need(seq, torch.int32, n), n, ws.ptr,
+                                 ws.nbytes, _stream()))
+
+
+def page_pool_compact(p, table, len, refs, pairs_out, n_pairs_out, ws):
+    _check(load().page_pool_compact(ctypes.byref(p), *_sequences(p, table, len, refs),
+                                    _need(pairs_out, torch.int32, max(p.N // 2, 1), 2), _need(n_pairs_out, torch.int32, 1),
+                                    ws.ptr, ws.nbytes, _stream()))
+
+
+def page_pool_share(p, table, len, seq, min_pages, share_out):
+    n = seq.numel()
+    _check(load().page_pool_share(ctypes.byref(p), _need(table, torch.int32, p.S, p.M), _need(len, torch.int32, p.S),
+                                  _need(seq, torch.int32, n), n, min_pages, _need(share_out, torch.int32, n, 3), _stream()))
+
+
+def page_copy(s_src, k_src, v_src, meta_src, s_dst, k_dst, v_dst, meta_dst, pairs, n_pairs):
+    n = pairs.shape[0]
+    _check(load().page_copy(ctypes.byref(s_src), *_rows(s_src, k_src, v_src, meta_src), ctypes.byref(s_dst),
+                            *_rows(s_dst, k_dst, v_dst, meta_dst), _need(pairs, torch.int32, n, 2), n,
+                            _need(n_pairs, torch.int32, 1), _stream()))
+
+
+def rat_state_copy(s, state_k, state_v, pairs):
+    S, n = state_k.shape[0], pairs.shape[0]
+    _check(load().rat_state_copy(ctypes.byref(s), _need(state_k, torch.float32, S, s.Hkv, s.D),
+                                 _need(state_v, torch.float32, S, s.Hkv, s.D), S, _need(pairs, torch.int32, n, 2), n, _stream()))
+
+
+def rat_append_paged(s, p, k, v, g, state_k, state_v, k_pool, v_pool, meta, table, len, seq, n_new, T_new):
+    dt, new, carry = k.dtype, (s.B, s.Hkv, T_new, s.D), (p.S, s.Hkv, s.D)
+    if _dtype_code(k) != s.dtype:
+        raise RatsparseError("k is not of the shape's type")
+    kp, vp, mp = _rows(s, k_pool, v_pool, meta)
+    _check(load().rat_append_paged(ctypes.byref(s), ctypes.byref(p), _need(k, dt, *new), _need(v, dt, *new),
+                                   _need(g, torch.float32, *new), _need(state_k, torch.float32, *carry),
+                                   _need(state_v, torch.float32, *carry), kp, vp, mp, _need(table, torch.int32, p.S, p.M),
+                                   _need(len, torch.int32, p.S), _need(seq, torch.int32, s.B), _need(n_new, torch.int32, s.B),
+                                   T_new, _stream()))
+
+
+def attn_paged_workspace_bytes(s, p, T_new):
+    return load().attn_paged_workspace_bytes(ctypes.byref(s), ctypes.byref(p), T_new)
+
+
+def attn_paged(s, p, q, k_pool, v_pool, table, len, seq, n_new, T_new, share, scale, out, lse_out, ws):
+    dt, rows = q.dtype, (s.B, s.Hq, T_new)
+    if _dtype_code(q) != s.dtype:
+        raise RatsparseError("q is not of the shape's type")
+    kp, vp, _ = _rows(s, k_pool, v_pool, None)
+    _check(load().attn_paged(ctypes.byref(s), ctypes.byref(p), _need(q, dt, *rows, s.D), kp, vp, _need(table, torch.int32, p.S, p.M),
+                             _need(len, torch.int32, p.S), _need(seq, torch.int32, s.B), _need(n_new, torch.int32, s.B), T_new,
+                             _need(share, torch.int32, s.B, 3), scale, _need(out, dt, *rows, s.D),
+                             _need(lse_out, torch.float32, *rows), ws.ptr, ws.nbytes, _stream()))

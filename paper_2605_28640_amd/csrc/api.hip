@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "append.h"
+#include "check.h"
 #include "common.h"
 #include "decode_fused.h"
 #include "knobs.h"
@@ -90,27 +91,6 @@ static uint32_t next_tag()
     uint32_t t = g_epoch.fetch_add(0x9E3779B1u) + 0x9E3779B1u;
     return t ? t : 0x5bd1e995u;
 }
-
-static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-static size_t esize(int dtype) { return dtype == RS_BF16 ? 2 : 4; }
-
-static int check_shape(const rs_shape *s, bool need_page)
-{
-    if (!s) return RS_INVALID_ARG;
-    if (s->B <= 0 || s->Hq <= 0 || s->Hkv <= 0 || s->Tcap <= 0) return RS_INVALID_ARG;
-    if (s->Hq % s->Hkv != 0) return RS_INVALID_ARG;
-    if (s->dtype != RS_F32 && s->dtype != RS_BF16) return RS_UNSUPPORTED;
-    if (s->D != 64 && s->D != 128) return RS_UNSUPPORTED;
-    if (need_page) {
-        if (s->P != 16 && s->P != 32 && s->P != 64 && s->P != 128 && s->P != 256 && s->P != 512) return RS_UNSUPPORTED;
-        if (s->Tcap % s->P != 0) return RS_INVALID_ARG;
-    }
-    if ((long)s->B * s->Hq > kMaxUnits) return RS_UNSUPPORTED;
-    return RS_OK;
-}
-
-static int launch_status() { return hipGetLastError() == hipSuccess ? RS_OK : RS_LAUNCH_FAILED; }
 
 // work split of the two-launch kernels: `target_wgs` workgroups in all (about one 512-thread
 // workgroup per CU), never less than `min_items_per_split` items in a split
@@ -440,6 +420,7 @@ const char *ratsparse_status_string(int32_t status)
         case RS_WORKSPACE_TOO_SMALL: return "workspace too small";
         case RS_LAUNCH_FAILED: return "kernel launch failed";
         case RS_ASYNC_TIMEOUT: return "a bounded in-kernel wait expired";
+        case RS_POOL_REFUSED: return "the page pool could not take the call (too few free pages, or a sequence out of range, listed twice or not empty)";
         case RS_SCRATCH_LIMIT: return "the shape needs more scratch than the library's static buffer holds";
         default: return "unknown status";
     }
@@ -502,7 +483,7 @@ int32_t ratsparse_async_status(void *ws, void *stream)
     if (flag) {
         fill_zero_kernel<<<1, 64, 0, (hipStream_t)stream>>>((uint32_t *)ws, 3);  // error word and scan counters
         (void)hipStreamSynchronize((hipStream_t)stream);
-        return RS_ASYNC_TIMEOUT;
+        return flag == 2u ? RS_POOL_REFUSED : RS_ASYNC_TIMEOUT;  // (2: pool.hip's refusals)
     }
     return RS_OK;
 }

@@ -1,0 +1,670 @@
+// Sequences in a pool of pages: who holds which page (reserve, fork, free, compact, share), the copies of a layer's rows that
+// follow from it, and the recurrence's append through a table.
+//
+// A page is free exactly when its reference count is 0, and the lowest numbered free page is always taken first, so there is
+// no free list to keep in step: the counts are the only state.  Finding pages is one workgroup's pass over the counts (4 bytes
+// a page), in order, with a prefix sum over its threads; a fork's and a release's table rows are a launch of their own over all
+// CUs.  Every call is decided as a whole by that one workgroup before anything is written: refused calls change nothing.
+#include "check.h"
+#include "common.h"
+
+namespace rs {
+
+constexpr int kPoolThreads = 1024;
+constexpr int kMaxSeqs = 32768;      // a bit of LDS each
+constexpr int kMaxShared = 1024;     // sequences of one page_pool_share call: a thread each
+constexpr uint32_t kErrPages = 2u;   // the asynchronous error word of a refused call
+
+struct PoolView {
+    int32_t *table, *len, *refs;
+    int N, S, M, shift;  // shift: log2 of the page size
+};
+
+__device__ __forceinline__ int pages_of(int tokens, int shift) { return (int)(((uint32_t)tokens + (1u << shift) - 1) >> shift); }
+
+// inclusive prefix sum over a wave
+__device__ __forceinline__ int wave_scan_i(int v)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int o = __shfl_up(v, d, kWave);
+        if (lane_id() >= d) v += o;
+    }
+    return v;
+}
+
+// what precedes this thread's value among the workgroup's, and (total) their sum; tot: LDS of one word a wave
+__device__ __forceinline__ int block_scan_i(int v, int *tot, int &total)
+{
+    const int wave = threadIdx.x >> 6, inc = wave_scan_i(v);
+    if (lane_id() == kWave - 1) tot[wave] = inc;
+    __syncthreads();
+    int before = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < kPoolThreads / kWave; ++w) {
+        const int x = tot[w];
+        if (w < wave) before += x;
+        sum += x;
+    }
+    __syncthreads();
+    total = sum;
+    return before + inc - v;
+}
+
+// The pages of [lo, hi) that are free (FREE) or held, ascending, to emit(rank, page) for ranks below `most`; returns how many
+// there are, but stops looking once there are `most`.  Called by the whole workgroup.
+template <bool FREE, typename Emit>
+__device__ __forceinline__ int collect_pages(const int32_t *refs, int lo, int hi, int most, int *tot, Emit emit)
+{
+    constexpr int EACH = 16;
+    int found = 0;
+    for (long base = lo & ~3; base < hi && found < most; base += kPoolThreads * EACH) {
+        const long p0 = base + (long)threadIdx.x * EACH;
+        uint32_t mask = 0u;
+        if (p0 < hi) {
+            int r[EACH];
+            if (p0 + EACH <= hi) {
+#pragma unroll
+                for (int u = 0; u < EACH / 4; ++u) {
+                    const int4 x = *reinterpret_cast<const int4 *>(refs + p0 + 4 * u);
+                    r[4 * u] = x.x, r[4 * u + 1] = x.y, r[4 * u + 2] = x.z, r[4 * u + 3] = x.w;
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < EACH; ++u) r[u] = refs[p0 + u < hi ? p0 + u : hi - 1];
+            }
+#pragma unroll
+            for (int u = 0; u < EACH; ++u)
+                if (p0 + u >= lo && p0 + u < hi && (r[u] <= 0) == FREE) mask |= 1u << u;
+        }
+        int total;
+        int at = found + block_scan_i(__popc(mask), tot, total);
+        for (; mask && at < most; mask &= mask - 1, ++at) emit(at, (int)(p0 + __builtin_ctz(mask)));
+        found += total;
+    }
+    return found;
+}
+
+// the list entry whose pages include number r: the last i with offs[i] <= r
+__device__ __forceinline__ int entry_of(const int32_t *offs, int n, int r)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (offs[mid] <= r) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// sets a bit of LDS; whether it was set
+__device__ __forceinline__ bool seen_before(uint32_t *bits, int s)
+{
+    return (atomicOr(&bits[s >> 5], 1u << (s & 31)) >> (s & 31)) & 1u;
+}
+
+// offs: n words; list: N words
+__global__ __launch_bounds__(kPoolThreads) void pool_reserve_kernel(PoolView p, const int32_t *__restrict__ seq, int n,
+                                                                    const int32_t *__restrict__ want, int T_new, int32_t *granted,
+                                                                    int32_t *offs, int32_t *list, uint32_t *err)
+{
+    __shared__ uint32_t seen[kMaxSeqs / 32];
+    __shared__ int tot[kPoolThreads / kWave];
+    const int tid = threadIdx.x;
+    seen[tid] = 0u;
+    __syncthreads();
+    bool bad = false;
+    long needed = 0;
+    for (int i0 = 0; i0 < n; i0 += kPoolThreads) {
+        const int i = i0 + tid;
+        int need = 0;
+        if (i < n) {
+            const int s = seq[i], t = want ? want[i] : T_new;
+            if (s < 0 || s >= p.S || t < 0 || seen_before(seen, s)) {
+                bad = true;
+            } else {
+                const int L = p.len[s];
+                if (L < 0 || (long)L + t > (long)p.M << p.shift) bad = true;
+                else need = pages_of(L + t, p.shift) - pages_of(L, p.shift);
+            }
+        }
+        int total;
+        const int at = block_scan_i(need, tot, total);
+        if (i < n) offs[i] = (int)needed + at;
+        needed += total;
+        if (needed > p.N) bad = true;  // (and the sum stays far from the end of its range)
+        if (__syncthreads_or(bad)) break;
+    }
+    bad = __syncthreads_or(bad);
+    const int total = (int)needed;
+    if (!bad && total > 0)
+        bad = collect_pages<true>(p.refs, 0, p.N, total, tot, [&](int r, int page) { list[r] = page; }) < total;
+    __syncthreads();
+    if (bad) {
+        if (granted)
+            for (int i = tid; i < n; i += kPoolThreads) granted[i] = 0;
+        if (tid == 0) *err = kErrPages;
+        return;
+    }
+    for (int r = tid; r < total; r += kPoolThreads) {
+        const int i = entry_of(offs, n, r), s = seq[i], page = list[r];
+        p.table[(long)s * p.M + pages_of(p.len[s], p.shift) + (r - offs[i])] = page;
+        p.refs[page] = 1;
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += kPoolThreads) {
+        const int t = want ? want[i] : T_new;
+        p.len[seq[i]] += t;
+        if (granted) granted[i] = t;
+    }
+}
+
+// full: n words, the pages that entry i takes over from its source (none where the call is refused)
+__global__ __launch_bounds__(kPoolThreads) void pool_fork_kernel(PoolView p, const int32_t *__restrict__ src,
+                                                                 const int32_t *__restrict__ dst, int n, int2 *pairs, int2 *carry,
+                                                                 int32_t *full, int32_t *list, uint32_t *err)
+{
+    __shared__ uint32_t seen[kMaxSeqs / 32];
+    __shared__ int tot[kPoolThreads / kWave];
+    const int tid = threadIdx.x;
+    seen[tid] = 0u;
+    __syncthreads();
+    bool bad = false;
+    for (int i = tid; i < n; i += kPoolThreads) {
+        const int d = dst[i], s = src[i];
+        if (d < 0 || d >= p.S || s < 0 || s >= p.S || seen_before(seen, d) || p.len[d] != 0 || p.len[s] < 0 ||
+            p.len[s] > (long)p.M << p.shift)
+            bad = true;
+    }
+    bad = __syncthreads_or(bad);
+    for (int i = tid; !bad && i < n; i += kPoolThreads)
+        if ((seen[src[i] >> 5] >> (src[i] & 31)) & 1u) bad = true;  // also a destination
+    bad = __syncthreads_or(bad);
+    int needed = 0;
+    for (int i0 = 0; !bad && i0 < n; i0 += kPoolThreads) {  // which of the new pages each entry gets
+        const int i = i0 + tid;
+        const int need = (i < n && (p.len[src[i]] & ((1 << p.shift) - 1))) ? 1 : 0;
+        int total;
+        const int at = block_scan_i(need, tot, total);
+        if (i < n) full[i] = need ? needed + at : -1;
+        needed += total;
+    }
+    if (!bad && needed > 0)
+        bad = collect_pages<true>(p.refs, 0, p.N, needed, tot, [&](int r, int page) { list[r] = page; }) < needed;
+    __syncthreads();
+    for (int i = tid; i < n; i += kPoolThreads) {
+        int2 pr = make_int2(-1, -1), cr = make_int2(-1, -1);
+        int whole = 0;
+        if (!bad) {
+            const int s = src[i], d = dst[i], L = p.len[s], at = full[i];
+            whole = L >> p.shift;
+            if (at >= 0) {
+                pr = make_int2(p.table[(long)s * p.M + whole], list[at]);
+                p.refs[pr.y] = 1;
+                p.table[(long)d * p.M + whole] = pr.y;
+            }
+            p.len[d] = L;
+            cr = make_int2(s, d);
+        }
+        full[i] = whole;
+        pairs[i] = pr;
+        if (carry) carry[i] = cr;
+    }
+    if (bad && tid == 0) *err = kErrPages;
+}
+
+// the rows of a fork: the source's full pages, one more reference each
+__global__ __launch_bounds__(256) void pool_fork_rows_kernel(PoolView p, const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
+                                                             const int32_t *__restrict__ full)
+{
+    const int i = blockIdx.x, n = full[i];
+    if (n == 0) return;
+    const long s = (long)src[i] * p.M, d = (long)dst[i] * p.M;
+    for (int j = blockIdx.y * 256 + threadIdx.x; j < n; j += gridDim.y * 256) {
+        const int page = p.table[s + j];
+        p.table[d + j] = page;
+        if (page >= 0 && page < p.N) atomicAdd(&p.refs[page], 1);
+    }
+}
+
+// held: n words, the pages that entry i gives up (none where the call is refused)
+__global__ __launch_bounds__(kPoolThreads) void pool_free_kernel(PoolView p, const int32_t *__restrict__ seq, int n, int32_t *held,
+                                                                 uint32_t *err)
+{
+    __shared__ uint32_t seen[kMaxSeqs / 32];
+    const int tid = threadIdx.x;
+    seen[tid] = 0u;
+    __syncthreads();
+    bool bad = false;
+    for (int i = tid; i < n; i += kPoolThreads) {
+        const int s = seq[i];
+        if (s < 0 || s >= p.S || seen_before(seen, s) || p.len[s] < 0 || p.len[s] > (long)p.M << p.shift) bad = true;
+    }
+    bad = __syncthreads_or(bad);
+    for (int i = tid; i < n; i += kPoolThreads) {
+        held[i] = bad ? 0 : pages_of(p.len[seq[i]], p.shift);
+        if (!bad) p.len[seq[i]] = 0;
+    }
+    if (bad && tid == 0) *err = kErrPages;
+}
+
+__global__ __launch_bounds__(256) void pool_free_rows_kernel(PoolView p, const int32_t *__restrict__ seq, const int32_t *__restrict__ held)
+{
+    const int i = blockIdx.x, n = held[i];
+    if (n == 0) return;
+    const long row = (long)seq[i] * p.M;
+    for (int j = blockIdx.y * 256 + threadIdx.x; j < n; j += gridDim.y * 256) {
+        const int page = p.table[row + j];
+        p.table[row + j] = -1;
+        if (page >= 0 && page < p.N) atomicSub(&p.refs[page], 1);
+    }
+}
+
+// L pages are held: those among them with numbers from L on go, in order, to the free ones below L.  to[page]: where page goes
+// (pages from L on that are held); holes: N words; count[0] = L.
+__global__ __launch_bounds__(kPoolThreads) void pool_compact_kernel(PoolView p, int32_t *to, int32_t *holes, int32_t *count, int2 *pairs,
+                                                                    int32_t *n_pairs)
+{
+    __shared__ int tot[kPoolThreads / kWave];
+    const int L = collect_pages<false>(p.refs, 0, p.N, p.N, tot, [](int, int) {});
+    const int n = collect_pages<true>(p.refs, 0, L, L, tot, [&](int r, int page) { holes[r] = page; });
+    __syncthreads();
+    collect_pages<false>(p.refs, L, p.N, n, tot, [&](int r, int page) {
+        const int hole = holes[r];
+        to[page] = hole;
+        pairs[r] = make_int2(page, hole);
+    });
+    __syncthreads();
+    for (int r = threadIdx.x; r < n; r += kPoolThreads) {
+        const int2 pr = pairs[r];
+        p.refs[pr.y] = p.refs[pr.x];
+        p.refs[pr.x] = 0;
+    }
+    if (threadIdx.x == 0) {
+        count[0] = L;
+        n_pairs[0] = n;
+    }
+}
+
+// the table under the new numbers, and the rest of the list of pairs
+__global__ __launch_bounds__(256) void pool_renumber_kernel(PoolView p, const int32_t *__restrict__ to, const int32_t *__restrict__ count,
+                                                            int2 *pairs, const int32_t *__restrict__ n_pairs, int room)
+{
+    const int L = count[0], n = n_pairs[0];
+    const long tid = (long)blockIdx.x * 256 + threadIdx.x, all = (long)gridDim.x * 256;
+    for (long r = n + tid; r < room; r += all) pairs[r] = make_int2(-1, -1);
+    const long cells = (long)p.S * p.M;
+    for (long c = tid; c < cells; c += all) {
+        const int page = p.table[c];
+        if (page >= L && page < p.N && (int)(c % p.M) < pages_of(p.len[c / p.M], p.shift)) p.table[c] = to[page];
+    }
+}
+
+// leading full pages that sequence i of the list has in common with the one before it, to share[3 i + 1]
+__global__ __launch_bounds__(256) void pool_common_kernel(PoolView p, const int32_t *__restrict__ seq, int32_t *share)
+{
+    const int i = blockIdx.x, tid = threadIdx.x;
+    int n = 0;
+    if (i > 0) {
+        const int a = seq[i - 1], b = seq[i];
+        if (a >= 0 && a < p.S && b >= 0 && b < p.S) {
+            const int la = p.len[a] >> p.shift, lb = p.len[b] >> p.shift;
+            int most = la < lb ? la : lb;
+            if (most > p.M) most = p.M;
+            const int32_t *ra = p.table + (long)a * p.M, *rb = p.table + (long)b * p.M;
+            __shared__ int first;
+            for (; n < most; n += 1024) {
+                if (tid == 0) first = most;
+                __syncthreads();
+                int differ = most;
+#pragma unroll
+                for (int u = 3; u >= 0; --u) {
+                    const int j = n + u * 256 + tid;
+                    if (j < most && (ra[j] != rb[j] || ra[j] < 0)) differ = j;
+                }
+                if (differ < most) atomicMin(&first, differ);
+                __syncthreads();
+                const int f = first;
+                __syncthreads();
+                if (f < most) {
+                    n = f;
+                    most = f;
+                    break;
+                }
+            }
+            n = most < 0 ? 0 : most;
+        }
+    }
+    if (tid == 0) share[3 * i + 1] = n;
+}
+
+// runs of neighbours with at least `least` pages in common; a run's pages are the fewest that two neighbours in it share
+__global__ __launch_bounds__(kMaxShared) void pool_runs_kernel(int32_t *share, int n, int least)
+{
+    __shared__ int first[kMaxShared], size[kMaxShared], pages[kMaxShared];
+    const int i = threadIdx.x;
+    const int common = i < n ? share[3 * i + 1] : 0;
+    const bool begins = i == 0 || common < least;
+    size[i] = 0;
+    pages[i] = 0x7fffffff;
+    first[i] = begins ? i : 0;
+    __syncthreads();
+    for (int d = 1; d < kMaxShared; d <<= 1) {  // running maximum
+        const int o = i >= d ? first[i - d] : 0;
+        __syncthreads();
+        if (o > first[i]) first[i] = o;
+        __syncthreads();
+    }
+    const int f = first[i];
+    if (i < n) {
+        atomicAdd(&size[f], 1);
+        if (!begins) atomicMin(&pages[f], common);
+    }
+    __syncthreads();
+    if (i < n) {
+        share[3 * i] = f;
+        share[3 * i + 1] = size[f];
+        share[3 * i + 2] = size[f] > 1 ? pages[f] : 0;
+    }
+}
+
+struct CopyView {
+    const char *k, *v, *meta;
+    long head;       // bytes of a KV head's rows
+    long meta_head;  // bytes of a KV head's bounds
+    int N;
+};
+
+// Listed pages of every KV head from one pool to another (or the same).  Nothing but bytes: a page of one head is one run of
+// P rows, 2 KB and more.  A workgroup takes (pair, head) after (pair, head).
+__global__ __launch_bounds__(256) void page_copy_kernel(CopyView s, CopyView d, const int2 *__restrict__ pairs, int n,
+                                                        const int32_t *__restrict__ n_pairs, int Hkv, int page_bytes, int meta_bytes)
+{
+    if (n_pairs) n = min(n, max(n_pairs[0], 0));
+    const long items = (long)n * Hkv;
+    for (long it = blockIdx.x; it < items; it += gridDim.x) {
+        const int2 pr = pairs[it / Hkv];
+        const long h = it % Hkv;
+        if (pr.x < 0 || pr.x >= s.N || pr.y < 0 || pr.y >= d.N) continue;
+        const uint4 *ks = reinterpret_cast<const uint4 *>(s.k + h * s.head + (long)pr.x * page_bytes);
+        const uint4 *vs = reinterpret_cast<const uint4 *>(s.v + h * s.head + (long)pr.x * page_bytes);
+        uint4 *kd = reinterpret_cast<uint4 *>(const_cast<char *>(d.k) + h * d.head + (long)pr.y * page_bytes);
+        uint4 *vd = reinterpret_cast<uint4 *>(const_cast<char *>(d.v) + h * d.head + (long)pr.y * page_bytes);
+        for (int c = threadIdx.x; c < page_bytes / 16; c += 256) {
+            const uint4 a = ks[c], b = vs[c];
+            kd[c] = a;
+            vd[c] = b;
+        }
+        if (s.meta) {
+            const uint4 *ms = reinterpret_cast<const uint4 *>(s.meta + h * s.meta_head + (long)pr.x * meta_bytes);
+            uint4 *md = reinterpret_cast<uint4 *>(const_cast<char *>(d.meta) + h * d.meta_head + (long)pr.y * meta_bytes);
+            for (int c = threadIdx.x; c < meta_bytes / 16; c += 256) md[c] = ms[c];
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void state_copy_kernel(float4 *state_k, float4 *state_v, int S, const int2 *__restrict__ pairs, int row4)
+{
+    const int2 pr = pairs[blockIdx.x];
+    if (pr.x < 0 || pr.x >= S || pr.y < 0 || pr.y >= S) return;
+    for (int c = blockIdx.y * 256 + threadIdx.x; c < row4; c += gridDim.y * 256) {
+        state_k[(long)pr.y * row4 + c] = state_k[(long)pr.x * row4 + c];
+        state_v[(long)pr.y * row4 + c] = state_v[(long)pr.x * row4 + c];
+    }
+}
+
+struct AppendParams {
+    const void *k, *v;
+    const float *g;
+    float *state_k, *state_v;
+    void *k_pool, *v_pool, *meta;
+    const int32_t *table, *len, *seq, *n_new;
+    int Hkv, S, M, N, shift, T_new;
+};
+
+// The recurrence over a sequence's new tokens, a thread for every (sequence, KV head, channel): s = g s + (1 - g) x in float32, the
+// rounded state to the token's row, its key into the page's bounds.
+template <typename ST, int D>
+__global__ __launch_bounds__(256) void append_paged_kernel(const AppendParams a)
+{
+    const int b = blockIdx.x, s = a.seq[b];
+    if (s < 0 || s >= a.S) return;
+    int again = 0;  // listed before: nothing is appended twice
+    for (int o = threadIdx.x; o < b; o += 256) again |= a.seq[o] == s;
+    if (__syncthreads_or(again)) return;
+    int n = a.n_new ? a.n_new[b] : a.T_new;
+    n = n < 0 ? 0 : n > a.T_new ? a.T_new : n;
+    const int L = a.len[s], P = 1 << a.shift;
+    if (n == 0 || L < n || L > (long)a.M << a.shift) return;
+    const int e = blockIdx.y * 256 + threadIdx.x;  // head * D + channel
+    if (e >= a.Hkv * D) return;
+    const int h = e / D, c = e % D;
+    const long st = (long)s * a.Hkv * D + e;
+    float sk = a.state_k[st], sv = a.state_v[st];
+    const long in0 = ((long)(b * a.Hkv + h) * a.T_new) * D + c;
+    const ST *k = (const ST *)a.k + in0, *v = (const ST *)a.v + in0;
+    const float *g = a.g + in0;
+    const int32_t *row = a.table + (long)s * a.M;
+    const long rows = (long)a.N << a.shift;
+    ST *kp = (ST *)a.k_pool + (long)h * rows * D + c, *vp = (ST *)a.v_pool + (long)h * rows * D + c;
+    ST *mt = a.meta ? (ST *)a.meta + (long)h * a.N * 2 * D + c : nullptr;
+    int page = -1;
+    float lo = 0.f, hi = 0.f;
+    for (int t = 0; t < n; ++t) {
+        const int pos = L - n + t, in_page = pos & (P - 1);
+        if (t == 0 || in_page == 0) {
+            page = row[pos >> a.shift];
+            if (page < 0 || page >= a.N) page = -1;
+        }
+        const float gg = g[(long)t * D], om = 1.f - gg;
+        sk = fmaf(gg, sk, om * to_f32(k[(long)t * D]));
+        sv = fmaf(gg, sv, om * to_f32(v[(long)t * D]));
+        ST ks, vs;
+        from_f32(ks, sk);
+        from_f32(vs, sv);
+        if (page < 0) continue;
+        const long at = (((long)page << a.shift) + in_page) * D;
+        kp[at] = ks;
+        vp[at] = vs;
+        if (mt) {
+            const float x = to_f32(ks);
+            ST *m = mt + (long)page * 2 * D;
+            if (in_page == 0) lo = hi = x;
+            else if (t == 0) lo = fminf(to_f32(m[0]), x), hi = fmaxf(to_f32(m[D]), x);
+            else lo = fminf(lo, x), hi = fmaxf(hi, x);
+            if (t + 1 == n || in_page == P - 1) {
+                from_f32(m[0], lo);
+                from_f32(m[D], hi);
+            }
+        }
+    }
+    a.state_k[st] = sk;
+    a.state_v[st] = sv;
+}
+
+static PoolView view(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs)
+{
+    return PoolView{table, len, refs, p->N, p->S, p->M, __builtin_ctz((unsigned)p->P)};
+}
+
+int check_pool(const rs_pool *p)
+{
+    if (!p || p->N <= 0 || p->S <= 0 || p->M <= 0) return RS_INVALID_ARG;
+    if (!page_size_ok(p->P)) return RS_UNSUPPORTED;
+    if ((long)p->N * p->P > 0x7fffffffL || (long)p->M * p->P > 0x7fffffffL || p->S > kMaxSeqs) return RS_UNSUPPORTED;
+    return RS_OK;
+}
+
+// scratch behind the control words: a word for every listed sequence, two for every page, one more
+static size_t pool_ws_bytes(const rs_pool *p)
+{
+    return RS_WS_CTRL_BYTES + align256((size_t)p->S * 4) + 2 * align256((size_t)p->N * 4) + 256;
+}
+
+struct PoolScratch {
+    uint32_t *err;
+    int32_t *seqs, *pages, *pages2, *word;
+};
+static PoolScratch scratch(const rs_pool *p, void *ws)
+{
+    char *w = (char *)ws + RS_WS_CTRL_BYTES;
+    PoolScratch x;
+    x.err = (uint32_t *)ws + kCtrlAsyncErr;
+    x.seqs = (int32_t *)w;
+    x.pages = (int32_t *)(w + align256((size_t)p->S * 4));
+    x.pages2 = (int32_t *)((char *)x.pages + align256((size_t)p->N * 4));
+    x.word = (int32_t *)((char *)x.pages2 + align256((size_t)p->N * 4));
+    return x;
+}
+
+// what the calls that change a pool ask for in common
+static int check_pool_call(const rs_pool *p, const void *table, const void *len, const void *refs, int n, const void *ws, size_t ws_bytes)
+{
+    const int st = check_pool(p);
+    if (st != RS_OK) return st;
+    if (!table || !len || !refs || !aligned16(table) || !aligned16(len) || !aligned16(refs)) return RS_INVALID_ARG;
+    if (n < 1 || n > p->S) return RS_INVALID_ARG;
+    if (!ws || !aligned16(ws) || ws_bytes < pool_ws_bytes(p)) return RS_WORKSPACE_TOO_SMALL;
+    return RS_OK;
+}
+
+// workgroups along a table's row: 256 entries each, 64 at most
+static unsigned row_groups(const rs_pool *p) { return (unsigned)(p->M >= 64 * 256 ? 64 : (p->M + 255) / 256); }
+
+}  // namespace rs
+
+using namespace rs;
+
+extern "C" {
+
+size_t page_pool_workspace_bytes(const rs_pool *p) { return check_pool(p) == RS_OK ? pool_ws_bytes(p) : 0; }
+
+int32_t page_pool_reserve(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, const int32_t *seq, int32_t n, const int32_t *want,
+                          int32_t T_new, int32_t *granted, void *ws, size_t ws_bytes, void *stream)
+{
+    const int st = check_pool_call(p, table, len, refs, n, ws, ws_bytes);
+    if (st != RS_OK) return st;
+    if (!seq || !aligned16(seq) || (want && !aligned16(want)) || (granted && !aligned16(granted)) || T_new < 0) return RS_INVALID_ARG;
+    const PoolScratch x = scratch(p, ws);
+    pool_reserve_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(view(p, table, len, refs), seq, n, want, T_new, granted, x.seqs,
+                                                                     x.pages, x.err);
+    return launch_status();
+}
+
+int32_t page_pool_fork(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, const int32_t *src, const int32_t *dst, int32_t n,
+                       int32_t *pairs_out, int32_t *carry_out, void *ws, size_t ws_bytes, void *stream)
+{
+    const int st = check_pool_call(p, table, len, refs, n, ws, ws_bytes);
+    if (st != RS_OK) return st;
+    if (!src || !dst || !pairs_out || !aligned16(src) || !aligned16(dst) || !aligned16(pairs_out) || (carry_out && !aligned16(carry_out)))
+        return RS_INVALID_ARG;
+    const PoolScratch x = scratch(p, ws);
+    const PoolView v = view(p, table, len, refs);
+    pool_fork_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, src, dst, n, (int2 *)pairs_out, (int2 *)carry_out, x.seqs, x.pages,
+                                                                  x.err);
+    pool_fork_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, src, dst, x.seqs);
+    return launch_status();
+}
+
+int32_t page_pool_free(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, const int32_t *seq, int32_t n, void *ws,
+                       size_t ws_bytes, void *stream)
+{
+    const int st = check_pool_call(p, table, len, refs, n, ws, ws_bytes);
+    if (st != RS_OK) return st;
+    if (!seq || !aligned16(seq)) return RS_INVALID_ARG;
+    const PoolScratch x = scratch(p, ws);
+    const PoolView v = view(p, table, len, refs);
+    pool_free_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, seq, n, x.seqs, x.err);
+    pool_free_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, seq, x.seqs);
+    return launch_status();
+}
+
+int32_t page_pool_compact(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs, int32_t *pairs_out, int32_t *n_pairs_out, void *ws,
+                          size_t ws_bytes, void *stream)
+{
+    const int st = check_pool_call(p, table, len, refs, 1, ws, ws_bytes);
+    if (st != RS_OK) return st;
+    if (!pairs_out || !n_pairs_out || !aligned16(pairs_out) || !aligned16(n_pairs_out)) return RS_INVALID_ARG;
+    const PoolScratch x = scratch(p, ws);
+    const PoolView v = view(p, table, len, refs);
+    pool_compact_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, x.pages, x.pages2, x.word, (int2 *)pairs_out, n_pairs_out);
+    const long cells = (long)p->S * p->M;
+    const unsigned groups = (unsigned)(cells >= 2048l * 256 ? 2048 : (cells + 255) / 256);
+    pool_renumber_kernel<<<groups, 256, 0, (hipStream_t)stream>>>(v, x.pages, x.word, (int2 *)pairs_out, n_pairs_out, p->N / 2);
+    return launch_status();
+}
+
+int32_t page_pool_share(const rs_pool *p, const int32_t *table, const int32_t *len, const int32_t *seq, int32_t n, int32_t min_pages,
+                        int32_t *share_out, void *stream)
+{
+    const int st = check_pool(p);
+    if (st != RS_OK) return st;
+    if (!table || !len || !seq || !share_out || !aligned16(table) || !aligned16(len) || !aligned16(seq) || !aligned16(share_out))
+        return RS_INVALID_ARG;
+    if (n < 1 || min_pages < 1) return RS_INVALID_ARG;
+    if (n > kMaxShared) return RS_UNSUPPORTED;
+    const PoolView v = view(p, const_cast<int32_t *>(table), const_cast<int32_t *>(len), nullptr);
+    pool_common_kernel<<<(unsigned)n, 256, 0, (hipStream_t)stream>>>(v, seq, share_out);
+    pool_runs_kernel<<<1, kMaxShared, 0, (hipStream_t)stream>>>(share_out, n, min_pages);
+    return launch_status();
+}
+
+int32_t page_copy(const rs_shape *s_src, const void *k_src, const void *v_src, const void *meta_src, const rs_shape *s_dst, void *k_dst,
+                  void *v_dst, void *meta_dst, const int32_t *pairs, int32_t n, const int32_t *n_pairs, void *stream)
+{
+    int st = check_shape(s_src, true);
+    if (st == RS_OK) st = check_shape(s_dst, true);
+    if (st != RS_OK) return st;
+    if (s_src->Hkv != s_dst->Hkv || s_src->D != s_dst->D || s_src->P != s_dst->P || s_src->dtype != s_dst->dtype) return RS_INVALID_ARG;
+    if (!k_src || !v_src || !k_dst || !v_dst || !pairs || (meta_src == nullptr) != (meta_dst == nullptr)) return RS_INVALID_ARG;
+    if (!aligned16(k_src) || !aligned16(v_src) || !aligned16(k_dst) || !aligned16(v_dst) || !aligned16(meta_src) || !aligned16(meta_dst) ||
+        !aligned16(pairs) || !aligned16(n_pairs) || n < 1)
+        return RS_INVALID_ARG;
+    const int row = s_src->D * (int)esize(s_src->dtype);
+    auto pool = [row](const rs_shape *s, const void *k, const void *v, const void *meta) {
+        return CopyView{(const char *)k, (const char *)v, (const char *)meta, (long)s->Tcap * row, (long)(s->Tcap / s->P) * 2 * row, s->Tcap / s->P};
+    };
+    const long items = (long)n * s_src->Hkv;
+    const unsigned groups = (unsigned)(items < 2048 ? items : 2048);
+    page_copy_kernel<<<groups, 256, 0, (hipStream_t)stream>>>(pool(s_src, k_src, v_src, meta_src), pool(s_dst, k_dst, v_dst, meta_dst),
+                                                              (const int2 *)pairs, n, n_pairs, s_src->Hkv, s_src->P * row, 2 * row);
+    return launch_status();
+}
+
+int32_t rat_state_copy(const rs_shape *s, float *state_k, float *state_v, int32_t S, const int32_t *pairs, int32_t n, void *stream)
+{
+    const int st = check_shape(s, false);
+    if (st != RS_OK) return st;
+    if (!state_k || !state_v || !pairs || !aligned16(state_k) || !aligned16(state_v) || !aligned16(pairs) || n < 1 || S < 1) return RS_INVALID_ARG;
+    const int row4 = s->Hkv * s->D / 4;
+    state_copy_kernel<<<dim3((unsigned)n, (unsigned)(row4 < 4096 ? (row4 + 255) / 256 : 16)), 256, 0, (hipStream_t)stream>>>(
+        (float4 *)state_k, (float4 *)state_v, S, (const int2 *)pairs, row4);
+    return launch_status();
+}
+
+int32_t rat_append_paged(const rs_shape *s, const rs_pool *p, const void *k, const void *v, const float *g, float *state_k, float *state_v,
+                         void *k_pool, void *v_pool, void *meta, const int32_t *table, const int32_t *len, const int32_t *seq,
+                         const int32_t *n_new, int32_t T_new, void *stream)
+{
+    int st = check_shape(s, true);
+    if (st == RS_OK) st = check_pool(p);
+    if (st != RS_OK) return st;
+    if (p->P != s->P || (long)p->N * p->P != s->Tcap || T_new < 1) return RS_INVALID_ARG;
+    if (!k || !v || !g || !state_k || !state_v || !k_pool || !v_pool || !table || !len || !seq) return RS_INVALID_ARG;
+    for (const void *x : {k, v, (const void *)g, (const void *)state_k, (const void *)state_v, (const void *)k_pool, (const void *)v_pool,
+                          (const void *)meta, (const void *)table, (const void *)len, (const void *)seq, (const void *)n_new})
+        if (!aligned16(x)) return RS_INVALID_ARG;
+    const AppendParams a{k, v, g, state_k, state_v, k_pool, v_pool, meta, table, len, seq, n_new, s->Hkv, p->S, p->M, p->N,
+                         __builtin_ctz((unsigned)p->P), T_new};
+    const dim3 grid((unsigned)s->B, (unsigned)((s->Hkv * s->D + 255) / 256));
+    if (s->dtype == RS_BF16) {
+        if (s->D == 128) append_paged_kernel<bf16, 128><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+        else append_paged_kernel<bf16, 64><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+    } else {
+        if (s->D == 128) append_paged_kernel<float, 128><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+        else append_paged_kernel<float, 64><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+    }
+    return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,305 @@
+"""Pages of a pool: who holds which, against a model in plain Python (every number equal); the copies that follow; the append
+through the table against the recurrence in 64 bits."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import say, tdtype
+from pool_model import Pool, recurrence
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Device:
+    """A pool on the device beside its model."""
+
+    def __init__(self, rs, N, S, M, P):
+        self.rs, self.m, self.p = rs, Pool(N, S, M, P), rs.make_pool(N, S, M, P)
+        self.table = torch.full((S, M), -1, dtype=torch.int32, device="cuda")
+        self.len, self.refs = ints([0] * S), ints([0] * N)
+        self.ws = rs.Workspace(rs.page_pool_workspace_bytes(self.p))
+
+    def state(self):
+        return self.p, self.table, self.len, self.refs
+
+    def check(self, what, taken=True):
+        torch.cuda.synchronize()
+        if taken:
+            self.ws.async_status()
+        else:
+            with pytest.raises(self.rs.RatsparseError, match="status 7"):
+                self.ws.async_status()
+            self.ws.async_status()  # reported once
+        assert self.table.tolist() == self.m.table, what
+        assert self.len.tolist() == self.m.len, what
+        assert self.refs.tolist() == self.m.refs, what
+
+    def reserve(self, seq, want):
+        granted = ints([7] * len(seq))
+        self.rs.page_pool_reserve(*self.state(), ints(seq), ints(want), 5, granted, self.ws)
+        taken = self.m.reserve(seq, want)
+        self.check(("reserve", seq, want), taken)
+        assert granted.tolist() == (want if taken else [0] * len(seq))
+        return taken
+
+    def fork(self, src, dst):
+        pairs, carry = ints([[5, 5]] * len(src)), ints([[5, 5]] * len(src))
+        self.rs.page_pool_fork(*self.state(), ints(src), ints(dst), pairs, carry, self.ws)
+        taken, mp, mc = self.m.fork(src, dst)
+        self.check(("fork", src, dst), taken)
+        assert pairs.tolist() == mp and carry.tolist() == mc
+        return taken
+
+    def free(self, seq):
+        self.rs.page_pool_free(*self.state(), ints(seq), self.ws)
+        taken = self.m.free(seq)
+        self.check(("free", seq), taken)
+        return taken
+
+    def compact(self):
+        pairs, n = ints([[5, 5]] * max(1, self.m.N // 2)), ints([9])
+        self.rs.page_pool_compact(*self.state(), pairs, n, self.ws)
+        moves = self.m.compact()
+        self.check("compact")
+        assert n.tolist() == [len(moves)]
+        if self.m.N > 1:
+            assert pairs.tolist() == moves + [[-1, -1]] * (self.m.N // 2 - len(moves))
+        return moves
+
+    def share(self, seq, least):
+        out = ints([[5, 5, 5]] * len(seq))
+        self.rs.page_pool_share(self.p, self.table, self.len, ints(seq), least, out)
+        assert out.tolist() == self.m.share(seq, least)
+
+
+@pytest.mark.parametrize("N,S,M,P,seed", [(1, 1, 1, 16, 0), (37, 5, 9, 16, 1), (400, 40, 30, 32, 2), (16400, 9, 8000, 16, 3),
+                                          (40003, 3000, 17, 512, 4)])
+def test_a_pool_s_life(rs, N, S, M, P, seed):
+    """Calls of every kind in no order, some of which cannot be taken."""
+    say("pool", N, S, M, P)
+    d, r = Device(rs, N, S, M, P), random.Random(seed)
+    seen = {}
+    for _ in range(60 if N < 1000 else 25):
+        kind = r.choice(["reserve", "reserve", "fork", "free", "compact", "share"])
+        some = r.sample(range(S), r.randint(1, min(S, r.choice([3, S]))))
+        if kind == "reserve":
+            top = r.choice([1, P, M * P // 4 + 1, M * P])
+            taken = d.reserve(some, [r.choice([0, 1, r.randint(0, top)]) for _ in some])
+        elif kind == "fork":
+            empty = [s for s in some if d.m.len[s] == 0] or some
+            taken = d.fork([r.randrange(S) for _ in empty], empty)
+        elif kind == "free":
+            taken = d.free(some[:max(1, len(some) // 2)])
+        elif kind == "compact":
+            taken = len(d.compact()) > 0
+        else:
+            taken = d.share([r.choice(some) for _ in range(r.randint(1, 40))], r.randint(1, 3))
+        seen[kind, bool(taken)] = seen.get((kind, bool(taken)), 0) + 1
+    say("  ", seen)
+
+
+def test_refused_as_a_whole(rs):
+    d = Device(rs, 10, 4, 6, 16)
+    assert d.reserve([2, 0], [40, 17])
+    for seq, want in (([1, 1], [1, 1]), ([-1], [1]), ([4], [1]), ([1], [-1]), ([0], [80]), ([1, 3], [1, 80]), ([2 ** 31 - 1], [1]),
+                      ([1], [2 ** 31 - 1])):
+        assert not d.reserve(seq, want), (seq, want)
+    for src, dst in (([2], [0]), ([2, 2], [1, 1]), ([2], [2]), ([9], [1]), ([2], [4]), ([1], [1]), ([2, 3], [3, 1])):
+        assert not d.fork(src, dst), (src, dst)
+    for seq in ([0, 0], [0, 4], [-1]):
+        assert not d.free(seq), seq
+    assert d.reserve([1], [80])  # the pool is full: no page for a fork's partial one
+    assert not d.fork([0], [3]) and d.free([1, 3])
+    assert d.fork([3], [1]) and d.m.len[1] == 0  # an empty one
+    assert d.reserve([0, 1], [0, 0])
+
+
+def test_share(rs):
+    d = Device(rs, 300, 12, 250, 16)
+    assert d.reserve([0, 1, 2], [3213, 16 * 5, 7])
+    assert d.fork([0, 0, 0, 1, 1, 2], [3, 4, 5, 6, 7, 8])
+    assert d.reserve([4, 5, 6], [30, 1, 17])
+    for seq in ([0], [0, 3, 4, 5], [3, 6, 7, 1, 4, 5], [2, 8], [6, 7, 3, 4], [0, 0, 3], [-1, 0, 3, 12], [10, 11, 0, 4] * 100):
+        for least in (1, 6, 200, 201):
+            d.share(seq, least)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,P,Hkv", [(64, 16, 3), (128, 64, 2), (128, 512, 1)])
+def test_page_copy(rs, dtype, D, P, Hkv):
+    """Between two pools of different size, with bounds and without; pairs to pass over; a count on the device."""
+    dt, gen = tdtype(dtype), torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *n: torch.randn(*n, device="cuda", generator=gen).to(dt)
+    N, M = 9, 23
+    s, o = rs.make_shape(1, Hkv, Hkv, D, N * P, P, dt), rs.make_shape(5, Hkv, Hkv, D, M * P, P, dt)
+    src = [rnd(Hkv, N * P, D), rnd(Hkv, N * P, D), rnd(Hkv, N, 2, D)]
+    pairs = [[3, 20], [-1, 2], [8, 0], [1, -1], [9, 4], [0, 23], [2, 22], [7, 7], [2 ** 31 - 1, 1], [5, 11]]
+    for count in (None, 0, 3, 10, 99, -4):
+        for bounds in (True, False):
+            dst = [rnd(Hkv, M * P, D), rnd(Hkv, M * P, D), rnd(Hkv, M, 2, D)]
+            want = [x.clone() for x in dst]
+            for a, b in pairs[:len(pairs) if count is None else max(0, count)]:
+                if 0 <= a < N and 0 <= b < M:
+                    for w, x, n in zip(want, src, (P, P, 2)) if bounds else list(zip(want, src, (P, P, 2)))[:2]:
+                        w.view(Hkv, M, n, D)[:, b] = x.view(Hkv, N, n, D)[:, a]
+            rs.page_copy(s, *(src if bounds else src[:2] + [None]), o, *(dst if bounds else dst[:2] + [None]), ints(pairs),
+                         None if count is None else ints([count]))
+            assert all(torch.equal(x, y) for x, y in zip(dst, want)), (count, bounds)
+
+
+def test_more_pages_than_workgroups(rs):
+    """Within one pool, every other page to the page after it."""
+    dt, N, P, D, Hkv = torch.bfloat16, 3000, 16, 64, 4
+    s = rs.make_shape(1, Hkv, Hkv, D, N * P, P, dt)
+    k, v = (torch.randn(Hkv, N * P, D, device="cuda").to(dt) for _ in range(2))
+    wk, wv = k.clone(), v.clone()
+    for x in (wk, wv):
+        y = x.view(Hkv, N, P, D)
+        y[:, 1::2] = y[:, ::2]
+    rs.page_copy(s, k, v, None, s, k, v, None, ints([[2 * i, 2 * i + 1] for i in range(N // 2)]), None)
+    assert torch.equal(k, wk) and torch.equal(v, wv)
+
+
+@pytest.mark.parametrize("Hkv,D", [(1, 64), (5, 128), (40, 128)])
+def test_state_copy(rs, Hkv, D):
+    s = rs.make_shape(1, Hkv, Hkv, D, 16, 16, torch.float32)
+    a, b = torch.randn(6, Hkv, D, device="cuda"), torch.randn(6, Hkv, D, device="cuda")
+    wa, wb = a.clone(), b.clone()
+    for w in (wa, wb):
+        w[4], w[0] = w[1], w[5]
+    rs.rat_state_copy(s, a, b, ints([[1, 4], [-1, -1], [5, 0], [6, 2], [2, 6]]))
+    assert torch.equal(a, wa) and torch.equal(b, wb)
+
+
+APPEND = [
+    # B, Hkv, D, P, T_new, lengths before, counts (None: T_new for all)
+    (1, 1, 64, 16, 1, [0], None),
+    (3, 2, 128, 16, 1, [15, 16, 17], None),
+    (4, 3, 64, 32, 7, [0, 31, 40, 5], [7, 0, 1, 3]),
+    (2, 2, 128, 16, 100, [3, 160], [100, 99]),
+    (2, 1, 64, 512, 700, [100, 0], None),
+    (5, 2, 128, 64, 33, [64, 63, 1, 130, 0], [33, 2, 33, 9, 40]),  # (counts above T_new are cut)
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", range(len(APPEND)))
+def test_append(rs, case, dtype):
+    B, Hkv, D, P, T, before, counts = APPEND[case]
+    say("append", case, dtype)
+    dt, S, r = tdtype(dtype), B + 2, np.random.default_rng(case)
+    M = -(-(max(before) + T) // P) + 1
+    d = Device(rs, S * M, S, M, P)
+    seq = r.permutation(S)[:B].tolist()
+    for i in r.permutation(B):  # (pages in no order)
+        assert d.reserve([seq[i]], [before[i]])
+    s = rs.make_shape(B, Hkv, Hkv, D, S * M * P, P, dt)
+    rnd = lambda *n: torch.from_numpy(r.standard_normal(n).astype(np.float32)).cuda()
+    k, v = rnd(B, Hkv, T, D).to(dt), rnd(B, Hkv, T, D).to(dt)
+    g = torch.sigmoid(rnd(B, Hkv, T, D) + 2.5)
+    cut = [min(T, c) for c in counts] if counts else [T] * B
+    for i in range(B):  # what lies past the counts is not read
+        for x in (k, v, g):
+            x[i, :, cut[i]:] = float("nan")
+    sk, sv = rnd(S, Hkv, D), rnd(S, Hkv, D)
+    kp, vp = rnd(Hkv, S * M * P, D).to(dt), rnd(Hkv, S * M * P, D).to(dt)
+    meta = rnd(Hkv, S * M, 2, D).to(dt)
+    for i in range(B):  # bounds are current before
+        for j in range(d.m.held(seq[i])):
+            rows = kp[:, d.m.rows(seq[i])[j * P:(j + 1) * P]].float()
+            meta[:, d.m.table[seq[i]][j], 0], meta[:, d.m.table[seq[i]][j], 1] = rows.amin(1).to(dt), rows.amax(1).to(dt)
+    olds = [x.clone() for x in (sk, sv, kp, vp, meta)]
+    assert d.reserve(seq, cut)
+    rs.rat_append_paged(s, d.p, k, v, g, sk, sv, kp, vp, meta, d.table, d.len, ints(seq), ints(counts) if counts else None, T)
+    torch.cuda.synchronize()
+    eps = 2.0 ** -24
+    touched = {}
+    for x, state, pool, old_state, old_pool in ((k, sk, kp, olds[0], olds[2]), (v, sv, vp, olds[1], olds[3])):
+        want_pool = old_pool.clone()
+        for i in range(B):
+            if cut[i] == 0:
+                continue
+            hx, hg = (y[i, :, :cut[i]].float().cpu().numpy().swapaxes(0, 1) for y in (x, g))
+            every = recurrence(old_state[seq[i]].cpu().numpy(), hx, hg)  # [T, Hkv, D]
+            # three roundings of at most half a step a token, of values no larger than what went in; later gates shrink them
+            tol = 3 * cut[i] * eps * max(np.abs(hx).max(), float(old_state[seq[i]].abs().max()))
+            assert np.abs(state[seq[i]].double().cpu().numpy() - every[-1]).max() <= tol
+            rows = d.m.rows(seq[i])[-cut[i]:]
+            stored = pool[:, rows].double().cpu().numpy().swapaxes(0, 1)
+            half = 2.0 ** -8 if dtype == "bf16" else 0.0
+            assert (np.abs(stored - every) <= half * (np.abs(every) + tol) + tol).all()
+            want_pool[:, rows] = pool[:, rows]
+            touched[i] = rows
+        assert torch.equal(pool, want_pool)  # nothing else is written
+        others = [i for i in range(S) if i not in seq or cut[seq.index(i)] == 0]
+        assert torch.equal(state[others], old_state[others])
+    want_meta = olds[4].clone()
+    for i in touched:
+        L, row = d.m.len[seq[i]], d.m.table[seq[i]]
+        for j in range((L - cut[i]) // P, (L - 1) // P + 1):
+            rows = kp[:, row[j] * P:row[j] * P + min(P, L - j * P)]
+            want_meta[:, row[j], 0], want_meta[:, row[j], 1] = rows.amin(1), rows.amax(1)
+    assert torch.equal(meta, want_meta)
+    # the same without bounds; the carries as bits
+    again = [x.clone() for x in olds[:4]]
+    rs.rat_append_paged(s, d.p, k, v, g, *again, None, d.table, d.len, ints(seq), ints(cut), T)
+    assert all(torch.equal(x, y) for x, y in zip(again, (sk, sv, kp, vp)))
+
+
+def test_append_passes_over_what_it_cannot_take(rs):
+    """A sequence out of range, listed twice, too short; a table entry that names no page."""
+    dt, P, S, M, N, Hkv, D, T = torch.float32, 16, 4, 3, 12, 2, 64, 4
+    d = Device(rs, N, S, M, P)
+    assert d.reserve([0, 1, 2], [20, 18, 3])
+    d.table[1, 1] = N  # no such page
+    seq = [0, 7, 0, -1, 2, 1]
+    s = rs.make_shape(len(seq), Hkv, Hkv, D, N * P, P, dt)
+    k, v, g = torch.ones(6, Hkv, T, D, device="cuda"), torch.ones(6, Hkv, T, D, device="cuda"), torch.full((6, Hkv, T, D), 0.5, device="cuda")
+    sk, sv = torch.zeros(S, Hkv, D, device="cuda"), torch.zeros(S, Hkv, D, device="cuda")
+    kp, vp, meta = (torch.zeros(*n, device="cuda") for n in ((Hkv, N * P, D), (Hkv, N * P, D), (Hkv, N, 2, D)))
+    rs.rat_append_paged(s, d.p, k, v, g, sk, sv, kp, vp, meta, d.table, d.len, ints(seq), None, T)
+    want = torch.tensor([0.5, 0.75, 0.875, 0.9375], device="cuda")
+    assert sk[0].eq(0.9375).all() and sk[1].eq(0.9375).all() and not sk[2:].any()
+    assert torch.equal(kp[0, d.m.rows(0)[-4:], 5], want)
+    assert torch.equal(kp[0, d.m.rows(1, 16)[-2:], 5], want[:2])  # positions 14, 15; 16 and 17 have no page
+    written = set(d.m.rows(0)[-4:].tolist()) | set(d.m.rows(1, 16)[-2:].tolist())
+    assert set(kp[1, :, 0].nonzero()[:, 0].tolist()) == written and set(vp[1, :, 0].nonzero()[:, 0].tolist()) == written
+
+
+def test_as_the_contiguous_append_does_it(rs):
+    """The same tokens into a contiguous cache by rat_scan, one by one: equal bits."""
+    dt, P, Hkv, D, T0, steps, B = torch.bfloat16, 16, 2, 128, 30, 5, 2
+    M = 4
+    d = Device(rs, B * M, B, M, P)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *n: torch.randn(*n, device="cuda", generator=gen)
+    s = rs.make_shape(B, Hkv, Hkv, D, M * P, P, dt)
+    kc, vc, meta = torch.zeros(B, Hkv, M * P, D, device="cuda", dtype=dt), torch.zeros(B, Hkv, M * P, D, device="cuda", dtype=dt), \
+        torch.zeros(B, Hkv, M, 2, D, device="cuda", dtype=dt)
+    sk, sv = torch.zeros(B, Hkv, D, device="cuda"), torch.zeros(B, Hkv, D, device="cuda")
+    ws = rs.Workspace(rs.rat_scan_workspace_bytes(s, T0))
+    rs.rat_scan(s, rnd(B, Hkv, T0, D).to(dt), rnd(B, Hkv, T0, D).to(dt), torch.sigmoid(rnd(B, Hkv, T0, D) + 4), sk, sv, kc, vc, 0, T0, ws, meta)
+    # the prompts' rows into pages
+    o = rs.make_shape(B, Hkv, Hkv, D, B * M * P, P, dt)
+    kp, vp, pm = torch.zeros(Hkv, B * M * P, D, device="cuda", dtype=dt), torch.zeros(Hkv, B * M * P, D, device="cuda", dtype=dt), \
+        torch.zeros(Hkv, B * M, 2, D, device="cuda", dtype=dt)
+    assert d.reserve([1, 0], [T0, T0])
+    for b in range(B):
+        rs.page_copy(s, kc[b], vc[b], meta[b], o, kp, vp, pm, ints([[j, d.m.table[b][j]] for j in range(2)]), None)
+    pk, pv = sk.clone(), sv.clone()
+    for t in range(steps):
+        k, v, g = rnd(B, Hkv, 1, D).to(dt), rnd(B, Hkv, 1, D).to(dt), torch.sigmoid(rnd(B, Hkv, 1, D) + 4)
+        rs.rat_scan(s, k, v, g, sk, sv, kc, vc, T0 + t, 1, ws, meta)
+        assert d.reserve([0, 1], [1, 1])
+        rs.rat_append_paged(o, d.p, k, v, g, pk, pv, kp, vp, pm, d.table, d.len, ints([0, 1]), None, 1)
+    assert torch.equal(pk, sk) and torch.equal(pv, sv)
+    for b in range(B):
+        rows = torch.from_numpy(d.m.rows(b)).cuda()
+        assert torch.equal(kp[:, rows], kc[b, :, :T0 + steps]) and torch.equal(vp[:, rows], vc[b, :, :T0 + steps])
+        assert torch.equal(pm[:, d.m.table[b][:3]], meta[b, :, :3])
