@@ -40,6 +40,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;  // the softmax's reference point moves when the maximum has grown by more (base-2 exponent)
 
 constexpr int kFew = 32, kMany = 128;  // rows of a tile
+constexpr int kPartUnits = 1;          // what beginning and ending a tile costs, in units of keys
 
 // keys a wave takes at a time
 template <typename ST>
@@ -62,14 +63,17 @@ struct PagedParams {
 struct Seq {
     int L, n, c, first;  // tokens, new ones, pages of the run's shared part (0: none), the run's first place
 };
+// A tile of n units takes kPartUnits + n places of the line, the first of them empty; a tile without units none.
+__device__ __forceinline__ int places(int n) { return n > 0 ? n + kPartUnits : 0; }
 struct Plan {
     Seq *seq;      // [B]
-    int *start;    // [B + 1] units before this place of the list
+    int *start;    // [B + 1] places of the line before this entry of the list
     int *members;  // [B] members of the run that begins here (0: none begins, or it shares nothing)
     int *fewest;   // [B] pages a run can share
-    __device__ __forceinline__ Plan(char *at, int B) : seq((Seq *)at), start((int *)(seq + B)), members(start + B + 1), fewest(members + B) {}
+    int *row;      // [B] the sequence's row of the table
+    __device__ __forceinline__ Plan(char *at, int B) : seq((Seq *)at), start((int *)(seq + B)), members(start + B + 1), fewest(members + B), row(fewest + B) {}
 };
-static size_t plan_bytes(int B) { return (size_t)B * 16 + (size_t)(3 * B + 1) * 4; }
+static size_t plan_bytes(int B) { return (size_t)B * 16 + (size_t)(4 * B + 1) * 4; }
 
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 
@@ -111,6 +115,7 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
         pl.seq[b] = Seq{L, n, c, first};
         pl.members[b] = (c > 0 && first == b) ? a.share[3 * b + 1] : 0;
         pl.fewest[b] = 0x7fffffff;
+        pl.row[b] = s;
     }
     __syncthreads();
     if (a.share) {
@@ -126,9 +131,9 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
         int units = 0, k0, k1;
         if (x.first == b && x.c > 0) {
             const int rows = pl.members[b] * a.T * a.G;
-            units += div_up(rows, shared_rows<ST>(rows)) * div_up(x.c << a.shift, UNIT);
+            units += div_up(rows, shared_rows<ST>(rows)) * places(div_up(x.c << a.shift, UNIT));
         }
-        for (int rt = 0; rt * a.own_rows < x.n * a.G; ++rt) units += own_units<UNIT>(x, rt, a.own_rows, a.G, a.shift, k0, k1);
+        for (int rt = 0; rt * a.own_rows < x.n * a.G; ++rt) units += places(own_units<UNIT>(x, rt, a.own_rows, a.G, a.shift, k0, k1));
         pl.start[b] = units;
         pl.seq[b].c = x.c;
         sum += units;
@@ -154,10 +159,13 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
     __syncthreads();
 }
 
-// where a tile's part in workgroup w goes: 2: all of the tile is here; 0, 1: a boundary record
+// Workgroup w of `groups` (no more than there are places) has the places [share_begin(w), share_begin(w + 1)) of the whole line.
+__device__ __forceinline__ long share_begin(long w, long all, int groups) { return w * all / groups; }
+__device__ __forceinline__ long owner_of(long place, long all, int groups) { return ((place + 1) * groups - 1) / all; }
+// where the part of a tile (its units at s0 .. s1 - 1) that lies in [wb, we) goes: 2: all of it is there; 0, 1: a boundary record
 __device__ __forceinline__ int record_of(long s0, long s1, long wb, long we) { return (s0 >= wb && s1 <= we) ? 2 : s0 <= wb ? 0 : 1; }
 
-// the last place of the list whose units begin at or before off (places without units are passed over)
+// the last entry of the list that begins at or before off (entries without units are passed over)
 __device__ __forceinline__ int place_of(const Plan &pl, int B, int off)
 {
     int lo = 0, hi = B;
@@ -179,43 +187,47 @@ struct TileWork {
     int record;               // record_of()
     long slot;                // of the boundary record
     bool direct;              // a whole tile without a second part
+    int entries;              // this lane's first entry of the table (PageList)
 };
 
-// the tile that unit `at` of the whole line belongs to; n: its units, off: which of them it is
+// the tile that place `at` of the whole line belongs to; its units are those at s0 .. s1 - 1
 template <typename ST>
-__device__ __forceinline__ void find_tile(const PagedParams &a, const Plan &pl, long at, int line, TileWork &w, int &n, int &off)
+__device__ __forceinline__ void find_tile(const PagedParams &a, const Plan &pl, long at, int line, TileWork &w, long &s0, long &s1)
 {
     constexpr int UNIT = kPagedWaves * kKeys<ST>;
     w.kvh = (int)(at / line);
-    off = (int)(at % line);
+    int off = (int)(at % line), n;
     const int lo = w.b = place_of(pl, a.B, off);
     off -= pl.start[lo];
     const Seq x = pl.seq[lo];
+    w.row_seq = pl.row[lo];
     int su = 0, st = 0;
     if (x.first == lo && x.c > 0) {
         w.rows = pl.members[lo] * a.T * a.G;
         w.tile_rows = shared_rows<ST>(w.rows);
-        su = div_up(x.c << a.shift, UNIT);
+        n = div_up(x.c << a.shift, UNIT);
+        su = places(n);
         st = div_up(w.rows, w.tile_rows);
     }
-    int k0 = 0;
+    w.key0 = 0;
     w.shared = off < su * st;
     if (w.shared) {
         w.rt = off / su;
         off -= w.rt * su;
-        n = su;
         w.limit = x.c << a.shift;
     } else {
         off -= su * st;
         w.rt = 0;
         w.rows = x.n * a.G;
         w.tile_rows = a.own_rows;
-        while (off >= (n = own_units<UNIT>(x, w.rt, a.own_rows, a.G, a.shift, k0, w.limit))) {
-            off -= n;
-            ++w.rt;
+        for (;; ++w.rt) {
+            n = own_units<UNIT>(x, w.rt, a.own_rows, a.G, a.shift, w.key0, w.limit);
+            if (off < places(n)) break;
+            off -= places(n);
         }
     }
-    w.key0 = k0 + off * UNIT;
+    s0 = at - off + kPartUnits;
+    s1 = s0 + n;
 }
 
 // the query behind row r of a segment; false: none
@@ -264,25 +276,47 @@ struct PageList {
     const int32_t *row;
     int first, stride, last, limit, N, shift, listed;
     __device__ __forceinline__ int key(int n) const { return first + n / PER * stride + n % PER * 16; }
-    // before the first entry of a step is asked for (64 % PER == 0): all lanes
+    // this lane's entry of the 64 from n on, as the table has it
+    __device__ __forceinline__ int fetch(int n) const
+    {
+        const int m = n + lane_id(), k = key(m);
+        int page = -1;
+        if (m < last && k < limit) page = row[k >> shift];
+        return page;
+    }
+    __device__ __forceinline__ void take(int page)
+    {
+        listed = (page < 0 || page >= N) ? -1 : page;
+        asm volatile("" : "+v"(listed));  // (waited for here, and not by every step)
+    }
+    // before the first entry of a step after the first is asked for (64 % PER == 0): all lanes
     __device__ __forceinline__ void fill(int n)
     {
-        if ((n & 63) == 0) {
-            const int m = n + lane_id(), k = key(m);
-            int page = -1;
-            if (m < last && k < limit) page = row[k >> shift];
-            listed = (page < 0 || page >= N) ? -1 : page;
-            asm volatile("" : "+v"(listed));  // (waited for here, and not by every step)
-        }
+        if ((n & 63) == 0) take(fetch(n));
     }
     // rows that exist (0 .. 16), and the first of them
     __device__ __forceinline__ int rows(int n, long &at) const
     {
         const int page = __builtin_amdgcn_readlane(listed, n & 63), k = key(n), left = limit - k;
         at = page < 0 ? 0l : ((long)page << shift) + (k & ((1 << shift) - 1));
-        return page < 0 ? 0 : left < 16 ? max(left, 0) : 16;
+        // (a scalar, which the compiler does not see in the clamp: the descriptors made of it would be a loop over the lanes each)
+        return __builtin_amdgcn_readfirstlane(page < 0 || left < 0 ? 0 : left < 16 ? left : 16);
     }
 };
+
+// the lists of the two kinds of tile
+template <typename ST>
+__device__ __forceinline__ PageList<kKeys<ST> / 16> few_pages(const PagedParams &a, const TileWork &w)
+{
+    constexpr int KT = kKeys<ST>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    return PageList<KT / 16>{a.table + (long)w.row_seq * a.M, w.key0 + wave * KT, kPagedWaves * KT, w.units * (KT / 16), w.limit, a.N, a.shift, -1};
+}
+__device__ __forceinline__ PageList<2> many_pages(const PagedParams &a, const TileWork &w)
+{
+    const int end = min(w.limit, w.key0 + w.units * (kPagedWaves * 32));
+    return PageList<2>{a.table + (long)w.row_seq * a.M, w.key0, 32, 2 * ((end - w.key0 + 31) / 32), w.limit, a.N, a.shift, -1};
+}
 
 __device__ __forceinline__ s16x4 paged_read_tr16(const char *p)
 {
@@ -412,14 +446,15 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
 
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const ST *kb = (const ST *)a.k + pool * D, *vb = (const ST *)a.v + pool * D;
-    PageList<NH> pages{a.table + (long)w.row_seq * a.M, w.key0 + wave * KT, kPagedWaves * KT, w.units * NH, w.limit, a.N, a.shift, -1};
+    PageList<NH> pages = few_pages<ST>(a, w);
+    pages.take(w.entries);
 
     f32x4 kf[NH][NK];
     LdsSource v_src[NH];
     int valid[NH];
     const uint32_t k_at = (uint32_t)(l16 * ROW + lg * 16);
     auto load_k = [&](int u) __attribute__((always_inline)) {  // also looks up where the step's rows are
-        pages.fill(u * NH);
+        if (u > 0) pages.fill(u * NH);
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
             long at;
@@ -646,8 +681,9 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     const int lq = lane & 31, h = lane >> 5;
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const bf16 *kb = (const bf16 *)a.k + pool * D, *vb = (const bf16 *)a.v + pool * D;
-    const int end = min(w.limit, w.key0 + w.units * (kPagedWaves * 32)), n_steps = (end - w.key0 + 31) / 32;
-    PageList<2> pages{a.table + (long)w.row_seq * a.M, w.key0, 32, 2 * n_steps, w.limit, a.N, a.shift, -1};
+    PageList<2> pages = many_pages(a, w);
+    const int n_steps = pages.last / 2;
+    pages.take(w.entries);
 
     // staging: pass i of a tile: this wave fetches RW rows, rows RPI i + RW wave on, all of one 16-key group
     const int row0 = (RW * wave + lane / CR) & 15;  // in the group
@@ -655,7 +691,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     const uint32_t gv = (uint32_t)(row0 * ROW + (((lane % CR) ^ chunk_swizzle<D>(row0 & 7)) * 16));
     LdsSource k_src[CPT], v_src[CPT];
     auto look_up = [&](int step) __attribute__((always_inline)) -> int {  // valid rows of the two groups, 8 bits each
-        pages.fill(2 * step);
+        if (step > 0) pages.fill(2 * step);
         long at[2];
         const int r0 = pages.rows(2 * step, at[0]), r1 = pages.rows(2 * step + 1, at[1]);
 #pragma unroll
@@ -863,26 +899,44 @@ __global__ __launch_bounds__(kPagedThreads, PAGED_OCC) void paged_attend_kernel(
             to.seq[b] = pl.seq[b];
             to.start[b] = pl.start[b];
             to.members[b] = pl.members[b];
+            to.row[b] = pl.row[b];
         }
         if (threadIdx.x == 0) to.start[a.B] = pl.start[a.B];
     }
-    // Workgroups are dealt to the eight XCDs in turn: those of one XCD take neighbouring stretches of the line, tiles of one KV head
-    // as a rule, whose rows they find in their L2.
-    const int me = (int)(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8);
     const int line = pl.start[a.B];
-    const long all = (long)line * a.Hkv, each = (all + gridDim.x - 1) / gridDim.x;
-    const long wb = each * me, we = min(wb + each, all);
+    const long all = (long)line * a.Hkv;
+    const int groups = (int)min((long)gridDim.x, all);
+    // Workgroups are dealt to the eight XCDs in turn: those of one XCD take neighbouring shares of the line, tiles of one KV head
+    // as a rule, whose rows they find in their L2; less work than workgroups goes to all XCDs.
+    const int me = groups < (int)gridDim.x ? (int)blockIdx.x : (int)(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8);
+    if (me >= groups) return;
+    const long wb = share_begin(me, all, groups), we = share_begin(me + 1, all, groups);
+    long at = wb;
+    // the next part of this workgroup's, with the first entries of its table row on their way
+    auto next = [&](TileWork &w) __attribute__((always_inline)) -> bool {
+        while (at < we) {
+            long s0, s1;
+            find_tile<ST>(a, pl, at, line, w, s0, s1);
+            const long from = max(at, s0), to = min(we, s1);
+            at = s1;
+            if (from >= to) continue;  // only the place before the units
+            w.key0 += (int)(from - s0) * (kPagedWaves * kKeys<ST>);
+            w.units = (int)(to - from);
+            w.record = record_of(s0, s1, wb, we);
+            w.slot = 2l * me + (w.record & 1);
+            w.direct = w.record == 2 && !w.shared && pl.seq[w.b].c == 0;
+            if (sizeof(ST) == 2 && w.tile_rows == kMany) w.entries = many_pages(a, w).fetch(0);
+            else w.entries = few_pages<ST>(a, w).fetch(0);
+            return true;
+        }
+        return false;
+    };
+    TileWork w;
+    bool more = next(w);
 #pragma unroll 1
-    for (long at = wb; at < we;) {
-        TileWork w;
-        int n, off;
-        find_tile<ST>(a, pl, at, line, w, n, off);
-        const long s0 = at - off;
-        w.row_seq = a.seq[w.b];
-        w.units = (int)min((long)(n - off), we - at);
-        w.record = record_of(s0, s0 + n, wb, we);
-        w.slot = 2l * me + (w.record & 1);
-        w.direct = w.record == 2 && !w.shared && pl.seq[w.b].c == 0;
+    while (more) {
+        TileWork then;
+        more = next(then);
         if (sizeof(ST) == 2 && w.tile_rows == kMany) {
             if constexpr (sizeof(ST) == 2) attend_many<D>(a, pl, w, ring);
         } else if (w.rows - w.rt * kFew <= 16) {
@@ -890,7 +944,7 @@ __global__ __launch_bounds__(kPagedThreads, PAGED_OCC) void paged_attend_kernel(
         } else {
             attend_few<ST, D, 2>(a, pl, w, ring, s_m, s_l);
         }
-        at += w.units;
+        w = then;
     }
 }
 
@@ -910,12 +964,12 @@ struct Join {
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + v[j] * f1;
     }
-    // every step-th record of a tile's row, from the lo-th on: units s0 .. s0 + n - 1 of the line; row r of the tile; whole: its row record
-    __device__ __forceinline__ void add_tile(const PagedParams &a, long s0, int n, long each, long all, int r, long whole, int lo, int step, int c4)
+    // every step-th record of a tile's row, from the lo-th on: its units are at s0 .. s1 - 1; row r of the tile; whole: its row record
+    __device__ __forceinline__ void add_tile(const PagedParams &a, long s0, long s1, long all, int groups, int r, long whole, int lo, int step, int c4)
     {
-        const long w0 = s0 / each, w1 = (s0 + n - 1) / each;
+        const long w0 = owner_of(s0, all, groups), w1 = owner_of(s1 - 1, all, groups);
         for (long w = w0 + lo; w <= w1; w += step) {
-            const int rec = record_of(s0, s0 + n, w * each, min(w * each + each, all));
+            const int rec = record_of(s0, s1, share_begin(w, all, groups), share_begin(w + 1, all, groups));
             const long at = rec == 2 ? whole : (2 * w + rec) * a.cut_rows + r;
             const float2 ml = *reinterpret_cast<const float2 *>((rec == 2 ? a.row_ml : a.cut_ml) + at * 2);
             add(ml.x, ml.y, *reinterpret_cast<const f32x4 *>((rec == 2 ? a.row_o : a.cut_o) + at * D + 4 * c4));
@@ -941,7 +995,8 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_rows_kernel(const Pa
     const int c4 = threadIdx.x % J::C4, grp = threadIdx.x / J::C4;
     const long rows = (long)a.B * a.Hq * a.T;
     const int line = pl.start[a.B];
-    const long all = (long)line * a.Hkv, each = max((all + a.groups - 1) / a.groups, 1l);
+    const long all = (long)line * a.Hkv;
+    const int groups = (int)min((long)a.groups, all);
     for (long row = blockIdx.x; row < rows; row += gridDim.x) {
         const int t = (int)(row % a.T), hq = (int)(row / a.T % a.Hq), b = (int)(row / a.T / a.Hq);
         const Seq x = pl.seq[b];
@@ -950,16 +1005,17 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_rows_kernel(const Pa
         J j;
         int k0, k1;
         const int own = own_units<UNIT>(x, 0, a.own_rows, a.G, a.shift, k0, k1);
-        long s0 = (long)kvh * line + pl.start[b];
+        long s0 = (long)kvh * line + pl.start[b] + kPartUnits;
         if (x.c > 0) {
             const int lead = x.first, su = div_up(x.c << a.shift, UNIT), all_rows = pl.members[lead] * a.T * a.G, tile = shared_rows<ST>(all_rows);
             const int r = ((b - lead) * a.T + t) * a.G + g;
-            j.add_tile(a, (long)kvh * line + pl.start[lead] + (long)(r / tile) * su, su, each, all, r % tile, row, grp, J::NG, c4);
-            if (lead == b) s0 += (long)su * div_up(all_rows, tile);
-        } else if (own > 0 && s0 / each == (s0 + own - 1) / each) {
+            const long t0 = (long)kvh * line + pl.start[lead] + (long)(r / tile) * places(su) + kPartUnits;
+            j.add_tile(a, t0, t0 + su, all, groups, r % tile, row, grp, J::NG, c4);
+            if (lead == b) s0 += (long)places(su) * div_up(all_rows, tile);
+        } else if (own > 0 && owner_of(s0, all, groups) == owner_of(s0 + own - 1, all, groups)) {
             continue;  // written as it is (the same for the whole workgroup)
         }
-        if (own > 0) j.add_tile(a, s0, own, each, all, t * a.G + g, rows + row, J::NG - 1 - grp, J::NG, c4);
+        if (own > 0) j.add_tile(a, s0, s0 + own, all, groups, t * a.G + g, rows + row, J::NG - 1 - grp, J::NG, c4);
         if (c4 == 0) {
             s_m[grp] = j.m;
             s_l[grp] = j.l;
@@ -976,7 +1032,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_rows_kernel(const Pa
     }
 }
 
-// Where they do not: only the tiles that the line's cuts go through, workgroup i looking at the cut before stretch i + 1; and the rows that see
+// Where they do not: only the tiles that the line's cuts go through, workgroup i looking at the end of the i-th share; and the rows that see
 // nothing, which may have no tile.
 template <typename ST, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const PagedParams a)
@@ -992,19 +1048,21 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const Pa
         }
     }
     const int line = pl.start[a.B];
-    const long all = (long)line * a.Hkv, each = max((all + a.groups - 1) / a.groups, 1l), cut = (blockIdx.x + 1) * each;
-    if (cut >= all) return;
+    const long all = (long)line * a.Hkv;
+    const int groups = (int)min((long)a.groups, all);
+    if ((int)blockIdx.x + 1 >= groups) return;
+    const long cut = share_begin(blockIdx.x + 1, all, groups);
     TileWork w;
-    int n, off;
-    find_tile<ST>(a, pl, cut, line, w, n, off);
-    if (off == 0 || off > each) return;  // between two tiles; not the tile's first cut
+    long s0, s1;
+    find_tile<ST>(a, pl, cut, line, w, s0, s1);
+    if (cut <= s0 || share_begin(blockIdx.x, all, groups) > s0) return;  // not through its units; not its first
     const int rows = min(w.rows - w.rt * w.tile_rows, w.tile_rows);
     for (int r = grp; r < rows; r += J::NG) {
         int bq, t, g;
         w.shared = false;
         if (!query_of(a, pl, w, w.rt * w.tile_rows + r, bq, t, g)) continue;
         J j;
-        j.add_tile(a, cut - off, n, each, all, r, 0, 0, 1, c4);
+        j.add_tile(a, s0, s1, all, groups, r, 0, 0, 1, c4);
         j.put(a, out_row(a, w, bq, t, g), c4);
     }
 }
