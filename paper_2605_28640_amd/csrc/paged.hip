@@ -6,21 +6,22 @@
 // part, attended by the rows of all sequences of the run at once, a sequence's own pages another, and each is split
 // further along its keys for balance.
 //
-// Work.  Segments (a run's shared pages, a sequence's own pages) times tiles of query rows, each cut into units of 128 (float32: 64) keys;
-// per KV head the units of all segments form one line, the lines of the heads another, and every workgroup takes an equal
-// share of it, whatever the lengths are.  Where that line is cut and which unit belongs to whom follows from the lengths alone: each workgroup
-// works it out for itself (a prefix sum over the list), so lengths live on the device and nothing has to be planned by the host.
-// What a workgroup holds of a tile goes to one of its two boundary records if the tile goes on elsewhere, to the row's record
-// if it has a second part (shared and own), else straight to the output; a second launch joins the records.
-//
 // Two kinds of tile:
-//   few rows (at most 32: a sequence's heads at decode): bound by the bytes of K and V.  A workgroup's four waves take 32 keys (float32: 16) each
-//     of a unit, every wave by itself: no barrier, its own softmax state, joined at the end of the tile.  K goes
-//     from memory into registers in the matrix operand's own layout, V through a wave's own LDS tile; while one is used the other is on its way.
-//   many rows (tiles of 128; bfloat16): bound by the matrix units.  Every wave takes 32 rows, all four go through the same keys, K
-//     and V tiles in a ring of three LDS slots filled two steps ahead, one barrier a step.
+//   few rows (at most 32: a sequence's heads at decode; and all of float32): bound by the bytes of K and V.  A wave by itself: it streams
+//     32 keys (float32: 16) a step, K from memory into registers in the matrix operand's own layout, V through two LDS tiles of its
+//     own, the next step's K and the V of two steps on their way.  No barrier anywhere; what a wave waits for at
+//     a tile's beginning and end, the others of its CU fill.
+//   many rows (tiles of 128; bfloat16): bound by the matrix units.  A workgroup: every wave takes 32 rows, all four go through the same
+//     keys, K and V tiles in a ring of four LDS slots filled three steps ahead, one barrier a step.
 // In both S^T = K Q^T and O^T = V^T P^T, so that a lane holds the keys of one query and P^T goes from the accumulators into the
 // second product as it is.
+//
+// Work.  The tiles of each kind, cut into units of keys, form a line: of every segment (a run's shared pages, a sequence's own) its
+// tiles, per KV head.  Every wave takes an equal share of the line of few-row tiles and every workgroup one of the line of many-row
+// tiles, whatever the lengths are (every other workgroup the one first, so that a CU has both at hand).  Where a line is cut follows from the
+// lengths alone: each workgroup works it out for itself, by a prefix sum over the list, so lengths live on the device and nothing has to
+// be planned by the host.  What a share holds of a tile goes to one of its two boundary records if the tile goes on in another
+// share, to the row's record if the row has a second part (shared and own), else straight to the output; a second launch joins the records.
 #include <type_traits>
 
 #include "check.h"
@@ -34,67 +35,104 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
+constexpr int kPagedGroups = 512;      // two workgroups a CU
 constexpr int kMaxList = 1024;
-#define PAGED_OCC 2
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kSlack = 8.f;  // the softmax's reference point moves when the maximum has grown by more (base-2 exponent)
-
+constexpr float kSlack = 8.f;          // the softmax's reference point moves when the maximum has grown by more (base-2 exponent)
 constexpr int kFew = 32, kMany = 128;  // rows of a tile
-constexpr int kPartUnits = 1;          // what beginning and ending a tile costs, in units of keys
 
-// keys a wave takes at a time
+// keys a wave of a few-row tile takes at a time
 template <typename ST>
 constexpr int kKeys = sizeof(ST) == 2 ? 32 : 16;
+// keys of a unit
+template <typename ST, bool MANY>
+constexpr int kUnit = MANY ? 128 : kKeys<ST>;
 
 struct PagedParams {
     const void *q, *k, *v;
     const int32_t *table, *len, *seq, *n_new, *share;
     void *out;
     float *lse;
-    float *cut_o, *cut_ml;      // boundary records: [2 workgroups][cut_rows] x D, x 2
-    float *row_o, *row_ml;      // row records: [shared, own][B Hq T] x D, x 2; nullptr: no segment is shared
+    float *cut_o, *cut_ml;      // boundary records: [2 shares][rows of a tile] x D, x 2; those of many-row tiles first
+    float *row_o, *row_ml;      // row records: [shared, own][B Hq T] x D, x 2
     char *plan;                 // the first workgroup's plan, for the join
-    int B, Hq, Hkv, G, S, M, N, shift, T, groups;
-    int own_rows, cut_rows;     // rows of a tile of one sequence, of a boundary record
+    long few_base;              // the first row of the few-row tiles' boundary records
+    int few_rows;               // rows that a few-row tile of this call can have
+    int own_many;               // whether a sequence's own tiles are of many rows
+    int B, Hq, Hkv, G, S, M, N, shift, T;
     float scale;
 };
 
-// The line of units of one KV head.
 struct Seq {
-    int L, n, c, first;  // tokens, new ones, pages of the run's shared part (0: none), the run's first place
+    int L, n, c, first;  // tokens, new ones, pages of the run's shared part (0: none), the run's first place in the list
 };
-// A tile of n units takes kPartUnits + n places of the line, the first of them empty; a tile without units none.
-__device__ __forceinline__ int places(int n) { return n > 0 ? n + kPartUnits : 0; }
 struct Plan {
-    Seq *seq;      // [B]
-    int *start;    // [B + 1] places of the line before this entry of the list
-    int *members;  // [B] members of the run that begins here (0: none begins, or it shares nothing)
-    int *fewest;   // [B] pages a run can share
-    int *row;      // [B] the sequence's row of the table
-    __device__ __forceinline__ Plan(char *at, int B) : seq((Seq *)at), start((int *)(seq + B)), members(start + B + 1), fewest(members + B), row(fewest + B) {}
+    Seq *seq;       // [B]
+    int *start[2];  // [B + 1] places of the line (of few-row tiles, of many-row tiles) before this entry of the list
+    int *members;   // [B] members of the run that begins here (0: none begins, or it shares nothing)
+    int *fewest;    // [B] pages a run can share
+    int *row;       // [B] the sequence's row of the table
+    __device__ __forceinline__ Plan(char *at, int B) : seq((Seq *)at)
+    {
+        start[0] = (int *)(seq + B);
+        start[1] = start[0] + B + 1;
+        members = start[1] + B + 1;
+        fewest = members + B;
+        row = fewest + B;
+    }
 };
-static size_t plan_bytes(int B) { return (size_t)B * 16 + (size_t)(4 * B + 1) * 4; }
+static size_t plan_bytes(int B) { return (size_t)B * 16 + (size_t)(5 * B + 2) * 4; }
 
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long scalar(long x)
+{
+    return (long)((uint64_t)(uint32_t)scalar((int)(x >> 32)) << 32 | (uint32_t)scalar((int)x));
+}
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 
-// units of row tile rt of sequence x over its own pages: the keys from the shared ones to the tile's last row
-template <int UNIT>
-__device__ __forceinline__ int own_units(const Seq &x, int rt, int rows, int G, int shift, int &k0, int &k1)
+// A tile of n units takes n places of its line and, before them, what beginning and ending a tile costs in units; a tile
+// without units none.
+template <bool MANY>
+constexpr int kBefore = MANY ? 1 : 2;
+template <bool MANY>
+__device__ __forceinline__ int places(int n)
 {
-    const int t0 = rt * rows / G, t1 = min(x.n - 1, (rt * rows + rows - 1) / G);
+    return n > 0 ? n + kBefore<MANY> : 0;
+}
+
+template <typename ST>
+__device__ __forceinline__ bool shared_is_many(int rows)
+{
+    return sizeof(ST) == 2 && rows > kFew;
+}
+
+// units of row tile rt of sequence x over its own pages: the keys from the shared ones to the tile's last row
+template <typename ST, bool MANY>
+__device__ __forceinline__ int own_units(const Seq &x, int rt, int G, int shift, int &k0, int &k1)
+{
+    constexpr int ROWS = MANY ? kMany : kFew, UNIT = kUnit<ST, MANY>;
+    const int t0 = rt * ROWS / G, t1 = min(x.n - 1, (rt * ROWS + ROWS - 1) / G);
     k0 = x.c << shift;
     k1 = x.L - x.n + t1 + 1;
     return (t0 >= x.n || k1 <= k0) ? 0 : (k1 - k0 + UNIT - 1) / UNIT;
 }
-// rows of a tile of a run's shared part, and its tiles
-template <typename ST>
-__device__ __forceinline__ int shared_rows(int rows) { return sizeof(ST) == 2 && rows > kFew ? kMany : kFew; }
+// an entry's places in a line: those of the run that begins there, if its tiles are of that kind, and its own
+template <typename ST, bool MANY>
+__device__ __forceinline__ int entry_places(const PagedParams &a, const Seq &x, int members)
+{
+    constexpr int ROWS = MANY ? kMany : kFew;
+    int sum = 0, k0, k1;
+    if (members > 0 && x.c > 0 && shared_is_many<ST>(members * a.T * a.G) == MANY)
+        sum = div_up(members * a.T * a.G, ROWS) * places<MANY>(div_up(x.c << a.shift, kUnit<ST, MANY>));
+    if ((a.own_many != 0) == MANY)
+        for (int rt = 0; rt * ROWS < x.n * a.G; ++rt) sum += places<MANY>(own_units<ST, MANY>(x, rt, a.G, a.shift, k0, k1));
+    return sum;
+}
 
 // Fills the plan; called by the whole workgroup.
 template <typename ST>
 __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
 {
-    constexpr int UNIT = kPagedWaves * kKeys<ST>;
     const int tid = threadIdx.x;
     for (int b = tid; b < a.B; b += kPagedThreads) {
         const int s = a.seq[b];
@@ -123,111 +161,139 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
         __syncthreads();
     }
     // (a thread's stretch of the list, so that a second pass can add what precedes it)
+    __shared__ int tot[2][kPagedWaves];
     const int each = div_up(a.B, kPagedThreads), lo = min(tid * each, a.B), hi = min(lo + each, a.B);
-    int sum = 0;
+    int sum[2] = {0, 0}, inc[2];
     for (int b = lo; b < hi; ++b) {
         Seq x = pl.seq[b];
         x.c = pl.members[x.first] ? pl.fewest[x.first] : 0;  // (nobody writes members, fewest or first here)
-        int units = 0, k0, k1;
-        if (x.first == b && x.c > 0) {
-            const int rows = pl.members[b] * a.T * a.G;
-            units += div_up(rows, shared_rows<ST>(rows)) * places(div_up(x.c << a.shift, UNIT));
-        }
-        for (int rt = 0; rt * a.own_rows < x.n * a.G; ++rt) units += places(own_units<UNIT>(x, rt, a.own_rows, a.G, a.shift, k0, k1));
-        pl.start[b] = units;
+        const int few = entry_places<ST, false>(a, x, pl.members[b]), many = entry_places<ST, true>(a, x, pl.members[b]);
         pl.seq[b].c = x.c;
-        sum += units;
+        pl.start[0][b] = few;
+        pl.start[1][b] = many;
+        sum[0] += few;
+        sum[1] += many;
     }
-    // what precedes the stretch
-    __shared__ int tot[kPagedWaves];
-    int inc = sum;
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int o = __shfl_up(inc, d, kWave);
-        if (lane_id() >= d) inc += o;
+    for (int k = 0; k < 2; ++k) {
+        inc[k] = sum[k];
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int o = __shfl_up(inc[k], d, kWave);
+            if (lane_id() >= d) inc[k] += o;
+        }
+        if (lane_id() == kWave - 1) tot[k][tid >> 6] = inc[k];
     }
-    if (lane_id() == kWave - 1) tot[tid >> 6] = inc;
     __syncthreads();
-    int at = inc - sum;
-    for (int w = 0; w < (tid >> 6); ++w) at += tot[w];
-    for (int b = lo; b < hi; ++b) {
-        const int u = pl.start[b];
-        pl.start[b] = at;
-        at += u;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        int at = inc[k] - sum[k];
+        for (int w = 0; w < (tid >> 6); ++w) at += tot[k][w];
+        for (int b = lo; b < hi; ++b) {
+            const int u = pl.start[k][b];
+            pl.start[k][b] = at;
+            at += u;
+        }
+        if (hi == a.B && lo < hi) pl.start[k][a.B] = at;
     }
-    if (hi == a.B && lo < hi) pl.start[a.B] = at;
     __syncthreads();
 }
 
-// Workgroup w of `groups` (no more than there are places) has the places [share_begin(w), share_begin(w + 1)) of the whole line.
-__device__ __forceinline__ long share_begin(long w, long all, int groups) { return w * all / groups; }
-__device__ __forceinline__ long owner_of(long place, long all, int groups) { return ((place + 1) * groups - 1) / all; }
+// A line's division into shares, equal but for one place: the first `more` have each + 1.  No more shares than places.
+template <bool MANY>
+struct Shares {
+    int line, n, more;  // places of a KV head, shares
+    long all, each;
+    double per, per1;   // 1 / each, 1 / (each + 1)
+    __device__ __forceinline__ Shares(int line, int Hkv) : line(line)
+    {
+        constexpr int MOST = MANY ? kPagedGroups : kPagedGroups * kPagedWaves;  // (a power of two)
+        all = (long)line * Hkv;
+        n = all < MOST ? (int)all : MOST;
+        each = n == MOST ? all / MOST : 1;
+        more = (int)(all - each * n);
+        per = 1. / (double)each;
+        per1 = 1. / (double)(each + 1);
+    }
+    __device__ __forceinline__ long begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int owner(long place) const
+    {
+        const long big = more * (each + 1);
+        int w = place < big ? (int)((double)place * per1) : more + (int)((double)(place - big) * per);
+        w = max(0, min(w, n - 1));
+        if (begin(w) > place) --w;  // (the quotient is within one of the true one)
+        if (begin(w + 1) <= place) ++w;
+        return w;
+    }
+};
 // where the part of a tile (its units at s0 .. s1 - 1) that lies in [wb, we) goes: 2: all of it is there; 0, 1: a boundary record
 __device__ __forceinline__ int record_of(long s0, long s1, long wb, long we) { return (s0 >= wb && s1 <= we) ? 2 : s0 <= wb ? 0 : 1; }
-
-// the last entry of the list that begins at or before off (entries without units are passed over)
-__device__ __forceinline__ int place_of(const Plan &pl, int B, int off)
+// the first row of a boundary record
+template <bool MANY>
+__device__ __forceinline__ long cut_row(const PagedParams &a, long share, int record)
 {
-    int lo = 0, hi = B;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (pl.start[mid] <= off) lo = mid;
-        else hi = mid;
-    }
-    return lo;
+    return MANY ? (2 * share + record) * kMany : a.few_base + (2 * share + record) * a.few_rows;
 }
 
 // one tile of rows over a run of keys
 struct TileWork {
-    int kvh, b, rt, rows;     // rows: of the segment (the tile takes those from rt * tile_rows on)
-    int tile_rows;
+    int kvh, b, rt, rows;     // rows: of the segment (the tile takes those from rt * (its kind's rows) on)
     bool shared;
     int row_seq;              // whose table row names the pages
     int key0, units, limit;   // first key, units of keys from there, keys that exist (later ones are nobody's)
     int record;               // record_of()
-    long slot;                // of the boundary record
+    long cut;                 // cut_row() of the boundary record
     bool direct;              // a whole tile without a second part
     int entries;              // this lane's first entry of the table (PageList)
 };
 
 // the tile that place `at` of the whole line belongs to; its units are those at s0 .. s1 - 1
-template <typename ST>
+template <typename ST, bool MANY>
 __device__ __forceinline__ void find_tile(const PagedParams &a, const Plan &pl, long at, int line, TileWork &w, long &s0, long &s1)
 {
-    constexpr int UNIT = kPagedWaves * kKeys<ST>;
+    const int *start = pl.start[MANY];
     w.kvh = (int)(at / line);
-    int off = (int)(at % line), n;
-    const int lo = w.b = place_of(pl, a.B, off);
-    off -= pl.start[lo];
+    int off = (int)(at % line), n = 0, lo = 0;
+    for (int hi = a.B; hi - lo > 1;) {  // the last entry that begins at or before off (entries without places are passed over)
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= off) lo = mid;
+        else hi = mid;
+    }
+    w.b = lo;
+    off -= start[lo];
     const Seq x = pl.seq[lo];
     w.row_seq = pl.row[lo];
-    int su = 0, st = 0;
-    if (x.first == lo && x.c > 0) {
-        w.rows = pl.members[lo] * a.T * a.G;
-        w.tile_rows = shared_rows<ST>(w.rows);
-        n = div_up(x.c << a.shift, UNIT);
-        su = places(n);
-        st = div_up(w.rows, w.tile_rows);
-    }
     w.key0 = 0;
-    w.shared = off < su * st;
-    if (w.shared) {
-        w.rt = off / su;
-        off -= w.rt * su;
+    w.shared = false;
+    const int members = pl.members[lo];
+    if (members > 0 && x.c > 0 && shared_is_many<ST>(members * a.T * a.G) == MANY) {
+        w.rows = members * a.T * a.G;
         w.limit = x.c << a.shift;
-    } else {
-        off -= su * st;
-        w.rt = 0;
-        w.rows = x.n * a.G;
-        w.tile_rows = a.own_rows;
-        for (;; ++w.rt) {
-            n = own_units<UNIT>(x, w.rt, a.own_rows, a.G, a.shift, w.key0, w.limit);
-            if (off < places(n)) break;
-            off -= places(n);
+        n = div_up(w.limit, kUnit<ST, MANY>);
+        const int su = places<MANY>(n), st = div_up(w.rows, MANY ? kMany : kFew);
+        w.shared = off < su * st;
+        if (w.shared) {
+            w.rt = off / su;
+            off -= w.rt * su;
+        } else {
+            off -= su * st;
         }
     }
-    s0 = at - off + kPartUnits;
-    s1 = s0 + n;
+    if (!w.shared) {
+        w.rows = x.n * a.G;
+        for (w.rt = 0;; ++w.rt) {
+            n = own_units<ST, MANY>(x, w.rt, a.G, a.shift, w.key0, w.limit);
+            if (off < places<MANY>(n)) break;
+            off -= places<MANY>(n);
+        }
+    }
+    s0 = scalar(at - off + kBefore<MANY>);
+    s1 = s0 + scalar(n);
+    // (what is read from LDS is the same for all lanes, which the compiler does not know: as vectors these would take the
+    // registers of the accumulators)
+    w.kvh = scalar(w.kvh), w.b = scalar(w.b), w.rt = scalar(w.rt), w.rows = scalar(w.rows), w.row_seq = scalar(w.row_seq);
+    w.key0 = scalar(w.key0), w.limit = scalar(w.limit);
+    w.shared = scalar(w.shared) != 0;
 }
 
 // the query behind row r of a segment; false: none
@@ -263,23 +329,20 @@ __device__ __forceinline__ void put4(const PagedParams &a, const TileWork &w, lo
         return;
     }
     const bool whole = w.record == 2;
-    const long at = whole ? (w.shared ? 0 : (long)a.B * a.Hq * a.T) + row : w.slot * a.cut_rows + r;
+    const long at = whole ? (w.shared ? 0 : (long)a.B * a.Hq * a.T) + row : w.cut + r;
     *reinterpret_cast<f32x4 *>((whole ? a.row_o : a.cut_o) + at * D + c) = o;
     if (c == 0) *reinterpret_cast<float2 *>((whole ? a.row_ml : a.cut_ml) + at * 2) = make_float2(m, l);
 }
 
 // ---- pages -----------------------------------------------------------------------------------------------------
-// Which rows hold a wave's keys, 16 at a time (a page is 16 keys and more): entry n is that of keys first + (n / PER) * stride +
-// 16 (n % PER).  64 entries of the table at a time, one a lane.
-template <int PER>
+// Which rows hold the keys from `first` on, 16 at a time (a page is 16 keys and more).  64 entries of the table at a time, one a lane.
 struct PageList {
     const int32_t *row;
-    int first, stride, last, limit, N, shift, listed;
-    __device__ __forceinline__ int key(int n) const { return first + n / PER * stride + n % PER * 16; }
+    int first, last, limit, N, shift, listed;  // last: groups of 16 that are asked for
     // this lane's entry of the 64 from n on, as the table has it
     __device__ __forceinline__ int fetch(int n) const
     {
-        const int m = n + lane_id(), k = key(m);
+        const int m = n + lane_id(), k = first + 16 * m;
         int page = -1;
         if (m < last && k < limit) page = row[k >> shift];
         return page;
@@ -289,33 +352,22 @@ struct PageList {
         listed = (page < 0 || page >= N) ? -1 : page;
         asm volatile("" : "+v"(listed));  // (waited for here, and not by every step)
     }
-    // before the first entry of a step after the first is asked for (64 % PER == 0): all lanes
-    __device__ __forceinline__ void fill(int n)
+    // rows that exist (0 .. 16) of group n, and the first of them; asked for in ascending order by the whole wave
+    __device__ __forceinline__ int rows(int n, long &at)
     {
-        if ((n & 63) == 0) take(fetch(n));
-    }
-    // rows that exist (0 .. 16), and the first of them
-    __device__ __forceinline__ int rows(int n, long &at) const
-    {
-        const int page = __builtin_amdgcn_readlane(listed, n & 63), k = key(n), left = limit - k;
+        if ((n & 63) == 0 && n > 0) take(fetch(n));
+        const int page = __builtin_amdgcn_readlane(listed, n & 63), k = first + 16 * n, left = limit - k;
         at = page < 0 ? 0l : ((long)page << shift) + (k & ((1 << shift) - 1));
         // (a scalar, which the compiler does not see in the clamp: the descriptors made of it would be a loop over the lanes each)
         return __builtin_amdgcn_readfirstlane(page < 0 || left < 0 ? 0 : left < 16 ? left : 16);
     }
 };
-
-// the lists of the two kinds of tile
-template <typename ST>
-__device__ __forceinline__ PageList<kKeys<ST> / 16> few_pages(const PagedParams &a, const TileWork &w)
+template <typename ST, bool MANY>
+__device__ __forceinline__ PageList page_list(const PagedParams &a, const TileWork &w)
 {
-    constexpr int KT = kKeys<ST>;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    return PageList<KT / 16>{a.table + (long)w.row_seq * a.M, w.key0 + wave * KT, kPagedWaves * KT, w.units * (KT / 16), w.limit, a.N, a.shift, -1};
-}
-__device__ __forceinline__ PageList<2> many_pages(const PagedParams &a, const TileWork &w)
-{
-    const int end = min(w.limit, w.key0 + w.units * (kPagedWaves * 32));
-    return PageList<2>{a.table + (long)w.row_seq * a.M, w.key0, 32, 2 * ((end - w.key0 + 31) / 32), w.limit, a.N, a.shift, -1};
+    constexpr int STEP = MANY ? 32 : kKeys<ST>;
+    const int end = min(w.limit, w.key0 + w.units * kUnit<ST, MANY>);
+    return PageList{a.table + (long)w.row_seq * a.M, w.key0, (end - w.key0 + STEP - 1) / STEP * (STEP / 16), w.limit, a.N, a.shift, -1};
 }
 
 __device__ __forceinline__ s16x4 paged_read_tr16(const char *p)
@@ -349,9 +401,9 @@ __device__ __forceinline__ void pin()
     asm volatile("" ::: "memory");
 }
 
-// the LDS of a workgroup: six tiles of 32 bfloat16 (16 float32) rows
+// the LDS of a workgroup: eight tiles of 32 bfloat16 (16 float32) rows
 struct Ring {
-    char *k0, *k1, *k2, *v0, *v1, *v2;
+    char *k0, *k1, *k2, *k3, *v0, *v1, *v2, *v3;
 };
 
 // whether any of `chunks` 16-byte pieces of LDS holds an infinity or NaN; every step-th from at on
@@ -371,24 +423,26 @@ __device__ __forceinline__ bool not_finite(const char *lds, int at, int step, in
 }
 
 // The same tile key by key, only the keys that a row sees: where V holds an infinity or NaN that some row is not to see, and
-// a matrix product would take 0 times it.  D / 4 lanes a row.
-template <typename ST, int D>
-__device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &pl, const TileWork &w)
+// a matrix product would take 0 times it.  D / 4 lanes a row, rows grp, grp + groups, ...
+template <typename ST, int D, bool MANY>
+__device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &pl, const TileWork &w, int grp, int groups)
 {
-    constexpr int UNIT = kPagedWaves * kKeys<ST>, C4 = D / 4, NG = kPagedThreads / C4;
-    const int c4 = threadIdx.x % C4, end = min(w.limit, w.key0 + w.units * UNIT);
+    constexpr int C4 = D / 4, ROWS = MANY ? kMany : kFew;
+    const int c4 = threadIdx.x % C4, end = min(w.limit, w.key0 + w.units * kUnit<ST, MANY>);
     const int32_t *pages = a.table + (long)w.row_seq * a.M;
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const float cs = a.scale * kLog2e;
-    for (int r = threadIdx.x / C4; r < w.tile_rows; r += NG) {
+#pragma unroll 1
+    for (int r = grp; r < ROWS; r += groups) {
         int bq, t, g;
-        if (!query_of(a, pl, w, w.rt * w.tile_rows + r, bq, t, g)) continue;
+        if (!query_of(a, pl, w, w.rt * ROWS + r, bq, t, g)) continue;
         const long row = out_row(a, w, bq, t, g);
         const int last = w.shared ? end - 1 : min(end - 1, pl.seq[bq].L - pl.seq[bq].n + t);
         float q[4], m = -INFINITY, l = 0.f;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[j] = to_f32(((const ST *)a.q)[row * D + 4 * c4 + j]);
+#pragma unroll 1
         for (int key = w.key0; key <= last; ++key) {
             const int page = pages[key >> a.shift];
             if (page < 0 || page >= a.N) continue;
@@ -405,7 +459,6 @@ __device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &
         }
         put4<ST, D>(a, w, row, r, 4 * c4, o, m, l);
     }
-    __syncthreads();
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------
@@ -434,67 +487,72 @@ struct FewRows {
 };
 
 template <typename ST, int D, int RT>
-__device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl, const TileWork &w, const Ring &lds, float *s_m, float *s_l)
+__device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl, const TileWork &w, char *const even, char *const odd_tile)
 {
     using Rows = FewRows<ST, D>;
     constexpr bool BF = sizeof(ST) == 2;
     constexpr int KT = kKeys<ST>, NH = KT / 16, ROW = Rows::ROW;
     constexpr int NDT = D / 16, NK = BF ? D / 32 : D / 16;  // 16-channel tiles of O^T; 16-byte operands of a row
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l16 = lane & 15, lg = lane >> 4;
-    char *const cV = wave == 0 ? lds.k0 : wave == 1 ? lds.k1 : wave == 2 ? lds.k2 : lds.v0;
+    const int lane = lane_id(), l16 = lane & 15, lg = lane >> 4;
 
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const ST *kb = (const ST *)a.k + pool * D, *vb = (const ST *)a.v + pool * D;
-    PageList<NH> pages = few_pages<ST>(a, w);
+    PageList pages = page_list<ST, false>(a, w);
     pages.take(w.entries);
 
     f32x4 kf[NH][NK];
-    LdsSource v_src[NH];
-    int valid[NH];
+    struct Where {
+        long at[NH];
+        int valid[NH];
+    };
     const uint32_t k_at = (uint32_t)(l16 * ROW + lg * 16);
-    auto load_k = [&](int u) __attribute__((always_inline)) {  // also looks up where the step's rows are
-        if (u > 0) pages.fill(u * NH);
+    auto look_up = [&](int u) __attribute__((always_inline)) -> Where {  // (past the last step: no rows)
+        Where x;
+#pragma unroll
+        for (int h = 0; h < NH; ++h) x.valid[h] = pages.rows(u * NH + h, x.at[h]);
+        return x;
+    };
+    auto load_k = [&](const Where &x) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
-            long at;
-            valid[h] = pages.rows(u * NH + h, at);
-            const LdsSource src = lds_source_sized(kb + at * D, valid[h] * ROW);
-            v_src[h] = lds_source_sized(vb + at * D, valid[h] * ROW);
+            const LdsSource src = lds_source_sized(kb + x.at[h] * D, x.valid[h] * ROW);
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) {
-                const auto x = __builtin_amdgcn_raw_buffer_load_b128(src, k_at + 64 * kk, 0, 2);
-                kf[h][kk] = __builtin_bit_cast(f32x4, x);
-            }
+            for (int kk = 0; kk < NK; ++kk) kf[h][kk] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(src, k_at + 64 * kk, 0, 2));
         }
         pin();
     };
-    auto load_v = [&]() __attribute__((always_inline)) {
+    auto load_v = [&](const Where &x, char *tile) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < NH; ++h) Rows::load_v(v_src[h], cV + h * 16 * ROW);
+        for (int h = 0; h < NH; ++h) Rows::load_v(lds_source_sized(vb + x.at[h] * D, x.valid[h] * ROW), tile + h * 16 * ROW);
         pin();
     };
-    load_k(0);
-    load_v();
+    // V of a step is always on its way before its K, so that K being there means V is
+    Where x0 = look_up(0);
+    load_v(x0, even);
+    load_k(x0);
+    Where x1 = look_up(1);
+    load_v(x1, odd_tile);
 
     // ---- this lane's queries ----
     f32x4 qf[RT][NK];
+    bool real[RT];
+    long row[RT];
     int last[RT];                 // the last position the row sees (-1: there is no such row)
     int first_last = 0x7fffffff;  // the smallest of the tile's rows
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         int bq, t, g;
-        const bool real = query_of(a, pl, w, w.rt * w.tile_rows + rt * 16 + l16, bq, t, g);
+        real[rt] = query_of(a, pl, w, w.rt * kFew + rt * 16 + l16, bq, t, g);
         last[rt] = -1;
-        const ST *q = (const ST *)a.q;
-        if (real) {
-            q += out_row(a, w, bq, t, g) * D;
+        row[rt] = 0;
+        if (real[rt]) {
+            row[rt] = out_row(a, w, bq, t, g);
             last[rt] = pl.seq[bq].L - pl.seq[bq].n + t;
         }
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const char *>(q) + 64 * kk + 16 * lg);
-            qf[rt][kk] = real ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const char *>((const ST *)a.q + row[rt] * D) + 64 * kk + 16 * lg);
+            qf[rt][kk] = real[rt] ? x : f32x4{0.f, 0.f, 0.f, 0.f};
         }
         first_last = min(first_last, last[rt]);
     }
@@ -516,17 +574,19 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
     // where a lane reads V of the tile's first 16 channels; of 16-channel tile dt: ^ 16 * (chunks of it)
     uint32_t v_at[BF ? 1 : 4];
     if constexpr (BF) {
-        const int row = 4 * lg + (l16 >> 2);
-        v_at[0] = (uint32_t)(row * ROW + ((((l16 & 3) >> 1) ^ Rows::v_swizzle(row)) * 16) + 8 * (l16 & 1));
+        const int r = 4 * lg + (l16 >> 2);
+        v_at[0] = (uint32_t)(r * ROW + ((((l16 & 3) >> 1) ^ Rows::v_swizzle(r)) * 16) + 8 * (l16 & 1));
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v_at[j] = (uint32_t)((4 * lg + j) * ROW + (((l16 >> 2) ^ Rows::v_swizzle(4 * lg + j)) * 16) + 4 * (l16 & 3));
     }
 
     bool odd = false;  // values that are not finite where some row may not look
+    const int n_steps = pages.last / NH;
 #pragma unroll 1
-    for (int u = 0; u < w.units; ++u) {
-        const int key = w.key0 + wave * KT + u * (kPagedWaves * KT);
+    for (int u = 0; u < n_steps; ++u) {
+        const int key = w.key0 + u * KT;
+        char *const cV = (u & 1) ? odd_tile : even;
         // ---- S^T = K Q^T ----
         f32x4 s[RT][NH];
 #pragma unroll
@@ -545,24 +605,19 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
                     }
                 }
             }
-        int here[NH];
-#pragma unroll
-        for (int h = 0; h < NH; ++h) here[h] = valid[h];
-        load_k(u + 1);  // (past the last unit: descriptors of no rows)
+        load_k(x1);
         // ---- softmax, base 2 ----
         const bool edge = key + KT - 1 > first_last;  // some row does not see some key of this step
-        const bool masked = edge || here[0] < 16 || here[NH - 1] < 16;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int h = 0; h < NH; ++h) s[rt][h] *= cs;
-        if (masked) {
+        if (edge || x0.valid[0] < 16 || x0.valid[NH - 1] < 16) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int h = 0; h < NH; ++h)
-                {
-                    const int sees = min(here[h], edge ? last[rt] + 1 - key - 16 * h : 16) - 4 * lg;  // of the lane's four
+                for (int h = 0; h < NH; ++h) {
+                    const int sees = min(x0.valid[h], edge ? last[rt] + 1 - key - 16 * h : 16) - 4 * lg;  // of the lane's four
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[rt][h][i] = i < sees ? s[rt][h][i] : -INFINITY;
                 }
@@ -592,9 +647,9 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
                     l[rt] += s[rt][h][i];
                 }
         }
-        // ---- O^T += V^T P^T ----
+        // ---- O^T += V^T P^T (weights rounded to the storage type: half a step of 2^-8 of each, of which a row has many) ----
         pin();
-        wait_loads<NH * NK>();  // V is here (the next K, issued after it, may be on its way)
+        wait_loads<NH *(NK + Rows::NL)>();  // V is here (the next V and the next K may be on their way)
         if (edge) odd |= not_finite<ST>(cV, lane, 64, KT * ROW / 16);
         if constexpr (BF) {
             bf16x8 pf[RT];
@@ -624,50 +679,19 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
                 }
         }
         wait_lds_reads();
-        load_v();
+        x0 = x1;
+        x1 = look_up(u + 2);
+        load_v(x1, cV);
     }
-
-    // ---- the four waves' parts become one ----
     wait_loads<0>();  // (nothing lands in this LDS any more)
-    if (__syncthreads_or(odd)) return attend_by_key<ST, D>(a, pl, w);
+    if (__any(odd)) return attend_by_key<ST, D, false>(a, pl, w, lane / (D / 4), 64 / (D / 4));
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const float sum = quad_sum(l[rt]);
-        if (lg == 0) {
-            s_m[wave * kFew + rt * 16 + l16] = m[rt];
-            s_l[wave * kFew + rt * 16 + l16] = sum;
+        if (real[rt]) {
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) put4<ST, D>(a, w, row[rt], rt * 16 + l16, 16 * dt + 4 * lg, oacc[rt][dt], m[rt], sum);
         }
-    }
-    constexpr int C4 = D / 4;  // 16-byte columns of an output row
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        f32x4 *mine = reinterpret_cast<f32x4 *>(cV);  // 16 rows of D floats: as large as a step's V
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) mine[l16 * C4 + ((4 * dt + lg) ^ l16)] = oacc[rt][dt];
-        __syncthreads();
-        for (int e = threadIdx.x; e < 16 * C4; e += kPagedThreads) {
-            const int r = e / C4, c4 = e % C4;
-            int bq, t, g;
-            if (!query_of(a, pl, w, w.rt * w.tile_rows + rt * 16 + r, bq, t, g)) continue;
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < kPagedWaves; ++i) top = fmaxf(top, s_m[i * kFew + rt * 16 + r]);
-            float L = 0.f;
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < kPagedWaves; ++i) {
-                const float mi = s_m[i * kFew + rt * 16 + r], li = s_l[i * kFew + rt * 16 + r];
-                if (mi == -INFINITY && li == 0.f) continue;  // saw nothing
-                const float f = mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
-                L = fmaf(f, li, L);
-                const char *tile = i == 0 ? lds.k0 : i == 1 ? lds.k1 : i == 2 ? lds.k2 : lds.v0;
-                const f32x4 x = *(reinterpret_cast<const f32x4 *>(tile) + r * C4 + (c4 ^ r));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] = fmaf(f, x[j], o[j]);
-            }
-            put4<ST, D>(a, w, out_row(a, w, bq, t, g), rt * 16 + r, 4 * c4, o, top, L);
-        }
-        __syncthreads();
     }
 }
 
@@ -681,7 +705,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     const int lq = lane & 31, h = lane >> 5;
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const bf16 *kb = (const bf16 *)a.k + pool * D, *vb = (const bf16 *)a.v + pool * D;
-    PageList<2> pages = many_pages(a, w);
+    PageList pages = page_list<bf16, true>(a, w);
     const int n_steps = pages.last / 2;
     pages.take(w.entries);
 
@@ -691,7 +715,6 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     const uint32_t gv = (uint32_t)(row0 * ROW + (((lane % CR) ^ chunk_swizzle<D>(row0 & 7)) * 16));
     LdsSource k_src[CPT], v_src[CPT];
     auto look_up = [&](int step) __attribute__((always_inline)) -> int {  // valid rows of the two groups, 8 bits each
-        if (step > 0) pages.fill(2 * step);
         long at[2];
         const int r0 = pages.rows(2 * step, at[0]), r1 = pages.rows(2 * step + 1, at[1]);
 #pragma unroll
@@ -711,11 +734,14 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     int valid1 = look_up(1);
 #pragma unroll
     for (int i = 0; i < CPT; ++i) stage_k(i, lds.k1), stage_v(i, lds.v1);
+    int valid2 = look_up(2);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) stage_k(i, lds.k2), stage_v(i, lds.v2);
 
     // ---- this lane's query ----
     int bq = 0, t = 0, g = 0;
     const int r = wave * 32 + lq;
-    const bool real = query_of(a, pl, w, w.rt * w.tile_rows + r, bq, t, g);
+    const bool real = query_of(a, pl, w, w.rt * kMany + r, bq, t, g);
     const long row = real ? out_row(a, w, bq, t, g) : 0;
     const int last = real ? pl.seq[bq].L - pl.seq[bq].n + t : -1;
     bf16x8 qf[NC];
@@ -751,22 +777,24 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
         for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
     const float cs = a.scale * kLog2e;
     float m = -INFINITY, l = 0.f;
-    wait_loads<2 * CPT>();  // the first tile has landed
+    wait_loads<4 * CPT>();  // the first tile has landed
     asm volatile("s_barrier" ::: "memory");
 
     auto step = [&](auto buf_tag, int it) __attribute__((always_inline)) {
         constexpr int BUF = decltype(buf_tag)::value;
-        const char *cK = BUF == 0 ? lds.k0 : BUF == 1 ? lds.k1 : lds.k2, *cV = BUF == 0 ? lds.v0 : BUF == 1 ? lds.v1 : lds.v2;
-        char *nK = BUF == 0 ? lds.k2 : BUF == 1 ? lds.k0 : lds.k1, *nV = BUF == 0 ? lds.v2 : BUF == 1 ? lds.v0 : lds.v1;
+        const char *cK = BUF == 0 ? lds.k0 : BUF == 1 ? lds.k1 : BUF == 2 ? lds.k2 : lds.k3, *cV = BUF == 0 ? lds.v0 : BUF == 1 ? lds.v1 : BUF == 2 ? lds.v2 : lds.v3;
+        char *nK = BUF == 0 ? lds.k3 : BUF == 1 ? lds.k0 : BUF == 2 ? lds.k1 : lds.k2, *nV = BUF == 0 ? lds.v3 : BUF == 1 ? lds.v0 : BUF == 2 ? lds.v1 : lds.v2;
         const int key = w.key0 + it * 32, here = valid0;
         valid0 = valid1;
-        valid1 = look_up(it + 2);  // (past the last step: descriptors of no rows)
-        const bool live = key <= wave_last;
+        valid1 = valid2;
+        valid2 = look_up(it + 3);  // (past the last step: descriptors of no rows)
+        const bool live = key <= wave_last && it < n_steps;
         if (key + 31 > tile_first) odd |= not_finite<bf16>(cV, threadIdx.x, kPagedThreads, 32 * ROW / 16);
         if (!live) {
 #pragma unroll
             for (int i = 0; i < CPT; ++i) stage_k(i, nK), stage_v(i, nV);
-        } else {
+        }
+        if (live) {
             f32x16 s;
 #pragma unroll
             for (int v = 0; v < 16; ++v) s[v] = 0.f;
@@ -850,20 +878,24 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
             __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
             __builtin_amdgcn_s_setprio(0);
         }
-        // the next step's tile has landed (the one after it may be on its way), and this wave has read what it needs
-        __builtin_amdgcn_s_waitcnt(0x0070 | (2 * CPT));
+        // the next step's tile has landed (the two after it may be on their way), and this wave has read what it needs
+        __builtin_amdgcn_s_waitcnt(0x0070 | (4 * CPT));
         asm volatile("s_barrier" ::: "memory");
     };
-    for (int it = 0;;) {
+    // (whole turns of the ring: steps past the last one only pass the barrier.  With ways out between the steps the compiler keeps two
+    // sets of accumulators and copies one to the other every step.)
+#pragma unroll 1
+    for (int it = 0; it < n_steps; it += 4) {
         step(std::integral_constant<int, 0>{}, it);
-        if (++it >= n_steps) break;
-        step(std::integral_constant<int, 1>{}, it);
-        if (++it >= n_steps) break;
-        step(std::integral_constant<int, 2>{}, it);
-        if (++it >= n_steps) break;
+        step(std::integral_constant<int, 1>{}, it + 1);
+        step(std::integral_constant<int, 2>{}, it + 2);
+        step(std::integral_constant<int, 3>{}, it + 3);
     }
     wait_loads<0>();  // (nothing lands in the ring any more)
-    if (__syncthreads_or(odd)) return attend_by_key<bf16, D>(a, pl, w);
+    if (__syncthreads_or(odd)) {
+        attend_by_key<bf16, D, true>(a, pl, w, threadIdx.x / (D / 4), kPagedThreads / (D / 4));
+        return;
+    }
     const float sum = half_pair_sum(l);
     if (real) {
 #pragma unroll
@@ -879,7 +911,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
 }
 
 template <typename ST, int D>
-__global__ __launch_bounds__(kPagedThreads, PAGED_OCC) void paged_attend_kernel(const PagedParams a)
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const PagedParams a)
 {
     constexpr int TILE = kKeys<ST> * D * (int)sizeof(ST);
     __shared__ __attribute__((aligned(1024))) char k0[TILE];
@@ -888,68 +920,89 @@ __global__ __launch_bounds__(kPagedThreads, PAGED_OCC) void paged_attend_kernel(
     __shared__ __attribute__((aligned(1024))) char v0[TILE];
     __shared__ __attribute__((aligned(1024))) char v1[TILE];
     __shared__ __attribute__((aligned(1024))) char v2[TILE];
-    __shared__ float s_m[kPagedWaves * kFew], s_l[kPagedWaves * kFew];
+    __shared__ __attribute__((aligned(1024))) char k3[TILE];
+    __shared__ __attribute__((aligned(1024))) char v3[TILE];
     extern __shared__ __attribute__((aligned(16))) char lds_plan[];
-    const Ring ring{k0, k1, k2, v0, v1, v2};
+    const Ring ring{k0, k1, k2, k3, v0, v1, v2, v3};
     const Plan pl(lds_plan, a.B);
     make_plan<ST>(a, pl);
     if (blockIdx.x == 0) {  // for the join
         const Plan to(a.plan, a.B);
-        for (int b = threadIdx.x; b < a.B; b += kPagedThreads) {
+        for (int b = threadIdx.x; b <= a.B; b += kPagedThreads) {
+            to.start[0][b] = pl.start[0][b];
+            to.start[1][b] = pl.start[1][b];
+            if (b == a.B) break;
             to.seq[b] = pl.seq[b];
-            to.start[b] = pl.start[b];
             to.members[b] = pl.members[b];
             to.row[b] = pl.row[b];
         }
-        if (threadIdx.x == 0) to.start[a.B] = pl.start[a.B];
     }
-    const int line = pl.start[a.B];
-    const long all = (long)line * a.Hkv;
-    const int groups = (int)min((long)gridDim.x, all);
-    // Workgroups are dealt to the eight XCDs in turn: those of one XCD take neighbouring shares of the line, tiles of one KV head
-    // as a rule, whose rows they find in their L2; less work than workgroups goes to all XCDs.
-    const int me = groups < (int)gridDim.x ? (int)blockIdx.x : (int)(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8);
-    if (me >= groups) return;
-    const long wb = share_begin(me, all, groups), we = share_begin(me + 1, all, groups);
-    long at = wb;
-    // the next part of this workgroup's, with the first entries of its table row on their way
-    auto next = [&](TileWork &w) __attribute__((always_inline)) -> bool {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // the next part of a share, with the first entries of its table row on their way
+    auto next = [&](auto many_tag, TileWork &w, long &at, long wb, long we, int line, int share) __attribute__((always_inline)) -> bool {
+        constexpr bool MANY = decltype(many_tag)::value;
         while (at < we) {
             long s0, s1;
-            find_tile<ST>(a, pl, at, line, w, s0, s1);
+            find_tile<ST, MANY>(a, pl, at, line, w, s0, s1);
             const long from = max(at, s0), to = min(we, s1);
             at = s1;
-            if (from >= to) continue;  // only the place before the units
-            w.key0 += (int)(from - s0) * (kPagedWaves * kKeys<ST>);
+            if (from >= to) continue;  // only places before the units
+            w.key0 += (int)(from - s0) * kUnit<ST, MANY>;
             w.units = (int)(to - from);
             w.record = record_of(s0, s1, wb, we);
-            w.slot = 2l * me + (w.record & 1);
-            w.direct = w.record == 2 && !w.shared && pl.seq[w.b].c == 0;
-            if (sizeof(ST) == 2 && w.tile_rows == kMany) w.entries = many_pages(a, w).fetch(0);
-            else w.entries = few_pages<ST>(a, w).fetch(0);
+            w.cut = cut_row<MANY>(a, share, w.record & 1);
+            w.direct = w.record == 2 && !w.shared && scalar(pl.seq[w.b].c) == 0;
+            w.entries = page_list<ST, MANY>(a, w).fetch(0);
             return true;
         }
         return false;
     };
-    TileWork w;
-    bool more = next(w);
+    // Workgroups are dealt to the eight XCDs in turn: those of one XCD take neighbouring shares of a line, tiles of one KV head
+    // as a rule, whose rows they find in their L2; less work than workgroups goes to all XCDs.
+    const int spread = (int)(blockIdx.x % 8 * (kPagedGroups / 8) + blockIdx.x / 8);
+    const Shares<false> few(scalar(pl.start[0][a.B]), a.Hkv);
+    const int few_me = few.n < kPagedGroups * kPagedWaves ? wave * kPagedGroups + (int)blockIdx.x : spread * kPagedWaves + wave;
+    const long few_end = few_me < few.n ? few.begin(few_me + 1) : 0, few_begin = few_me < few.n ? few.begin(few_me) : 0;
+    long few_at = few_begin;
+    TileWork first;  // of this wave's few-row tiles
+    bool few_more = next(std::false_type{}, first, few_at, few_begin, few_end, few.line, few_me);
 #pragma unroll 1
-    while (more) {
-        TileWork then;
-        more = next(then);
-        if (sizeof(ST) == 2 && w.tile_rows == kMany) {
-            if constexpr (sizeof(ST) == 2) attend_many<D>(a, pl, w, ring);
-        } else if (w.rows - w.rt * kFew <= 16) {
-            attend_few<ST, D, 1>(a, pl, w, ring, s_m, s_l);
+    for (int phase = 0; phase < 2; ++phase) {
+        if ((phase ^ (blockIdx.x >> 3)) & 1) {
+            if constexpr (sizeof(ST) == 2) {
+                const Shares<true> many(scalar(pl.start[1][a.B]), a.Hkv);
+                const int me = many.n < kPagedGroups ? (int)blockIdx.x : spread;
+                if (me < many.n) {
+                    const long wb = many.begin(me), we = many.begin(me + 1);
+                    long at = wb;
+                    TileWork w, then;
+                    bool more = next(std::true_type{}, w, at, wb, we, many.line, me);
+#pragma unroll 1
+                    while (more) {
+                        more = next(std::true_type{}, then, at, wb, we, many.line, me);
+                        attend_many<D>(a, pl, w, ring);
+                        w = then;
+                    }
+                }
+            }
         } else {
-            attend_few<ST, D, 2>(a, pl, w, ring, s_m, s_l);
+            char *const even = wave == 0 ? k0 : wave == 1 ? k2 : wave == 2 ? v0 : v2, *const odd = wave == 0 ? k1 : wave == 1 ? k3 : wave == 2 ? v1 : v3;
+            TileWork w = first;
+#pragma unroll 1
+            while (few_more) {
+                TileWork then;
+                few_more = next(std::false_type{}, then, few_at, few_begin, few_end, few.line, few_me);
+                if (w.rows - w.rt * kFew <= 16) attend_few<ST, D, 1>(a, pl, w, even, odd);
+                else attend_few<ST, D, 2>(a, pl, w, even, odd);
+                w = then;
+            }
         }
-        w = then;
+        __syncthreads();  // (the other phase uses the same LDS)
     }
 }
 
 // ---- the join --------------------------------------------------------------------------------------------------
-// Records are joined by a workgroup's 4 x 64 / (D / 4) groups of D / 4 threads, 16 bytes of the row a thread.
+// Records are joined by groups of D / 4 threads, 16 bytes of the row a thread.
 template <typename ST, int D>
 struct Join {
     static constexpr int C4 = D / 4, NG = kPagedThreads / C4;
@@ -965,14 +1018,28 @@ struct Join {
         for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + v[j] * f1;
     }
     // every step-th record of a tile's row, from the lo-th on: its units are at s0 .. s1 - 1; row r of the tile; whole: its row record
-    __device__ __forceinline__ void add_tile(const PagedParams &a, long s0, long s1, long all, int groups, int r, long whole, int lo, int step, int c4)
+    template <bool MANY>
+    __device__ __forceinline__ void add_tile(const PagedParams &a, const Shares<MANY> &sh, long s0, long s1, int r, long whole, int lo, int step, int c4)
     {
-        const long w0 = owner_of(s0, all, groups), w1 = owner_of(s1 - 1, all, groups);
-        for (long w = w0 + lo; w <= w1; w += step) {
-            const int rec = record_of(s0, s1, share_begin(w, all, groups), share_begin(w + 1, all, groups));
-            const long at = rec == 2 ? whole : (2 * w + rec) * a.cut_rows + r;
-            const float2 ml = *reinterpret_cast<const float2 *>((rec == 2 ? a.row_ml : a.cut_ml) + at * 2);
-            add(ml.x, ml.y, *reinterpret_cast<const f32x4 *>((rec == 2 ? a.row_o : a.cut_o) + at * D + 4 * c4));
+        constexpr int AHEAD = 4;  // records on their way together
+        const int w0 = sh.owner(s0), w1 = sh.owner(s1 - 1);
+        for (int w = w0 + lo; w <= w1; w += AHEAD * step) {
+            float2 ml[AHEAD];
+            f32x4 v[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int x = w + i * step;
+                ml[i] = make_float2(-INFINITY, 0.f);
+                v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (x <= w1) {
+                    const int rec = record_of(s0, s1, sh.begin(x), sh.begin(x + 1));
+                    const long at = rec == 2 ? whole : cut_row<MANY>(a, x, rec) + r;
+                    ml[i] = *reinterpret_cast<const float2 *>((rec == 2 ? a.row_ml : a.cut_ml) + at * 2);
+                    v[i] = *reinterpret_cast<const f32x4 *>((rec == 2 ? a.row_o : a.cut_o) + at * D + 4 * c4);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) add(ml[i].x, ml[i].y, v[i]);
         }
     }
     __device__ __forceinline__ void put(const PagedParams &a, long row, int c4) const
@@ -983,39 +1050,54 @@ struct Join {
     }
 };
 
-// Where sequences share pages: every row has its shared and its own part, and at most kMany rows of a sequence are one tile.
+// Where a sequence's rows are one tile: a workgroup for every row, its records divided among the thread groups.
+template <typename ST, int D, bool OWN>
+__device__ __forceinline__ bool own_part(const PagedParams &a, const Plan &pl, const Shares<OWN> &sh, Join<ST, D> &j, const Seq &x, int b, int kvh,
+                                         long row, int r, int grp, int c4)
+{
+    int k0, k1;
+    const int n = own_units<ST, OWN>(x, 0, a.G, a.shift, k0, k1);
+    if (n == 0) return false;
+    long s0 = (long)kvh * sh.line + pl.start[OWN][b] + kBefore<OWN>;
+    const int rows = pl.members[b] * a.T * a.G;
+    if (rows > 0 && x.c > 0 && shared_is_many<ST>(rows) == OWN) s0 += (long)div_up(rows, OWN ? kMany : kFew) * places<OWN>(div_up(x.c << a.shift, kUnit<ST, OWN>));
+    if (x.c == 0 && sh.owner(s0) == sh.owner(s0 + n - 1)) return true;  // written as it is
+    j.template add_tile<OWN>(a, sh, s0, s0 + n, r, (long)a.B * a.Hq * a.T + row, j.NG - 1 - grp, j.NG, c4);
+    return false;
+}
+template <typename ST, int D, bool MANY>
+__device__ __forceinline__ void shared_part(const PagedParams &a, const Plan &pl, const Shares<MANY> &sh, Join<ST, D> &j, int c, int lead, int kvh,
+                                            long row, int r, int grp, int c4)
+{
+    constexpr int ROWS = MANY ? kMany : kFew;
+    const int n = div_up(c << a.shift, kUnit<ST, MANY>);
+    const long s0 = (long)kvh * sh.line + pl.start[MANY][lead] + (long)(r / ROWS) * places<MANY>(n) + kBefore<MANY>;
+    j.template add_tile<MANY>(a, sh, s0, s0 + n, r % ROWS, row, grp, j.NG, c4);
+}
 template <typename ST, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join_rows_kernel(const PagedParams a)
 {
-    constexpr int UNIT = kPagedWaves * kKeys<ST>;
     using J = Join<ST, D>;
     __shared__ float s_m[J::NG], s_l[J::NG];
     __shared__ f32x4 s_o[J::NG][J::C4];
     const Plan pl(a.plan, a.B);
     const int c4 = threadIdx.x % J::C4, grp = threadIdx.x / J::C4;
     const long rows = (long)a.B * a.Hq * a.T;
-    const int line = pl.start[a.B];
-    const long all = (long)line * a.Hkv;
-    const int groups = (int)min((long)a.groups, all);
+    const Shares<false> few(pl.start[0][a.B], a.Hkv);
+    const Shares<true> many(pl.start[1][a.B], a.Hkv);
     for (long row = blockIdx.x; row < rows; row += gridDim.x) {
         const int t = (int)(row % a.T), hq = (int)(row / a.T % a.Hq), b = (int)(row / a.T / a.Hq);
         const Seq x = pl.seq[b];
         if (t >= x.n) continue;
-        const int kvh = hq / a.G, g = hq % a.G;
+        const int kvh = hq / a.G, r = t * a.G + hq % a.G;
         J j;
-        int k0, k1;
-        const int own = own_units<UNIT>(x, 0, a.own_rows, a.G, a.shift, k0, k1);
-        long s0 = (long)kvh * line + pl.start[b] + kPartUnits;
+        if (a.own_many ? own_part<ST, D, true>(a, pl, many, j, x, b, kvh, row, r, grp, c4) : own_part<ST, D, false>(a, pl, few, j, x, b, kvh, row, r, grp, c4))
+            continue;  // (the same for the whole workgroup)
         if (x.c > 0) {
-            const int lead = x.first, su = div_up(x.c << a.shift, UNIT), all_rows = pl.members[lead] * a.T * a.G, tile = shared_rows<ST>(all_rows);
-            const int r = ((b - lead) * a.T + t) * a.G + g;
-            const long t0 = (long)kvh * line + pl.start[lead] + (long)(r / tile) * places(su) + kPartUnits;
-            j.add_tile(a, t0, t0 + su, all, groups, r % tile, row, grp, J::NG, c4);
-            if (lead == b) s0 += (long)places(su) * div_up(all_rows, tile);
-        } else if (own > 0 && owner_of(s0, all, groups) == owner_of(s0 + own - 1, all, groups)) {
-            continue;  // written as it is (the same for the whole workgroup)
+            const int lead = x.first, at = (b - lead) * a.T * a.G + r;
+            if (shared_is_many<ST>(pl.members[lead] * a.T * a.G)) shared_part<ST, D, true>(a, pl, many, j, x.c, lead, kvh, row, at, grp, c4);
+            else shared_part<ST, D, false>(a, pl, few, j, x.c, lead, kvh, row, at, grp, c4);
         }
-        if (own > 0) j.add_tile(a, s0, s0 + own, all, groups, t * a.G + g, rows + row, J::NG - 1 - grp, J::NG, c4);
         if (c4 == 0) {
             s_m[grp] = j.m;
             s_l[grp] = j.l;
@@ -1032,12 +1114,13 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_rows_kernel(const Pa
     }
 }
 
-// Where they do not: only the tiles that the line's cuts go through, workgroup i looking at the end of the i-th share; and the rows that see
+// Where they are many: only the tiles that the line's cuts go through, workgroup i looking at the end of the i-th share; and the rows that see
 // nothing, which may have no tile.
-template <typename ST, int D>
+template <typename ST, int D, bool MANY>
 __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const PagedParams a)
 {
     using J = Join<ST, D>;
+    constexpr int ROWS = MANY ? kMany : kFew;
     const Plan pl(a.plan, a.B);
     const int c4 = threadIdx.x % J::C4, grp = threadIdx.x / J::C4;
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
@@ -1047,46 +1130,46 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const Pa
             j.put(a, (long)(b * a.Hq + e / none) * a.T + e % none, c4);
         }
     }
-    const int line = pl.start[a.B];
-    const long all = (long)line * a.Hkv;
-    const int groups = (int)min((long)a.groups, all);
-    if ((int)blockIdx.x + 1 >= groups) return;
-    const long cut = share_begin(blockIdx.x + 1, all, groups);
+    const Shares<MANY> sh(pl.start[MANY][a.B], a.Hkv);
+    if ((int)blockIdx.x + 1 >= sh.n) return;
+    const long cut = sh.begin(blockIdx.x + 1);
     TileWork w;
     long s0, s1;
-    find_tile<ST>(a, pl, cut, line, w, s0, s1);
-    if (cut <= s0 || share_begin(blockIdx.x, all, groups) > s0) return;  // not through its units; not its first
-    const int rows = min(w.rows - w.rt * w.tile_rows, w.tile_rows);
+    find_tile<ST, MANY>(a, pl, cut, sh.line, w, s0, s1);
+    if (cut <= s0 || sh.begin(blockIdx.x) > s0) return;  // not through its units; not its first
+    const int rows = min(w.rows - w.rt * ROWS, ROWS);
     for (int r = grp; r < rows; r += J::NG) {
         int bq, t, g;
-        w.shared = false;
-        if (!query_of(a, pl, w, w.rt * w.tile_rows + r, bq, t, g)) continue;
+        if (!query_of(a, pl, w, w.rt * ROWS + r, bq, t, g)) continue;
         J j;
-        j.add_tile(a, s0, s1, all, groups, r, 0, 0, 1, c4);
+        j.template add_tile<MANY>(a, sh, s0, s1, r, 0, 0, 1, c4);
         j.put(a, out_row(a, w, bq, t, g), c4);
     }
 }
 
 int check_pool(const rs_pool *p);  // pool.hip
 
-constexpr int kPagedGroups = 256 * PAGED_OCC;
-
-static bool many_rows(const rs_shape *s, long rows) { return s->dtype == RS_BF16 && rows > kFew; }
-static int unit_keys(int dtype) { return kPagedWaves * (dtype == RS_BF16 ? kKeys<bf16> : kKeys<float>); }
-
-// Whether the rows of several sequences are put together: only where one sequence's rows leave room in a tile; else a
-// tile's rows come from one sequence anyway and its keys are one segment, without records to join.
-static bool rows_are_shared(const rs_shape *s, int T_new) { return (long)T_new * (s->Hq / s->Hkv) < (s->dtype == RS_BF16 ? kMany : kFew); }
+static int tile_rows(const rs_shape *s) { return s->dtype == RS_BF16 ? kMany : kFew; }
 
 struct PagedLayout {
-    size_t cut, rows, off_ml, off_plan, total;  // records of each kind
+    bool own_many, shares;   // a sequence's own tiles are of many rows; rows of several sequences may be put together
+    int few_rows;            // rows of a few-row tile, at most
+    size_t many, cut, rows;  // boundary records' rows of many-row tiles, of both kinds; row records
+    size_t off_ml, off_plan, total;
 };
 static PagedLayout paged_layout(const rs_shape *s, int T_new)
 {
     PagedLayout x;
-    const long most = rows_are_shared(s, T_new) ? (long)s->B * T_new * (s->Hq / s->Hkv) : (long)T_new * (s->Hq / s->Hkv);
-    x.cut = (size_t)2 * kPagedGroups * (many_rows(s, most) ? kMany : kFew);
-    x.rows = rows_are_shared(s, T_new) ? (size_t)s->B * s->Hq * T_new * 2 : 0;
+    const long own = (long)T_new * (s->Hq / s->Hkv);
+    // Rows of several sequences are put together only where one sequence's rows leave room in a tile; else a
+    // tile's rows come from one sequence anyway and its keys are one segment, without records to join.
+    x.shares = own < tile_rows(s);
+    const long most = x.shares ? own * s->B : own;
+    x.own_many = s->dtype == RS_BF16 && own > kFew;
+    x.few_rows = (int)(most < kFew ? most : kFew);
+    x.many = (s->dtype == RS_BF16 && most > kFew) ? (size_t)2 * kPagedGroups * kMany : 0;
+    x.cut = x.many + (size_t)2 * kPagedGroups * kPagedWaves * x.few_rows;
+    x.rows = x.shares ? (size_t)s->B * s->Hq * T_new * 2 : 0;
     x.off_ml = RS_WS_CTRL_BYTES + align256((x.cut + x.rows) * s->D * 4);
     x.off_plan = x.off_ml + align256((x.cut + x.rows) * 8);
     x.total = x.off_plan + align256(plan_bytes(s->B));
@@ -1100,19 +1183,22 @@ static int check_paged(const rs_shape *s, const rs_pool *p, int T_new)
     if (st != RS_OK) return st;
     if (p->P != s->P || (long)p->N * p->P != s->Tcap || T_new < 1) return RS_INVALID_ARG;
     if (s->B > kMaxList) return RS_UNSUPPORTED;
-    // units of a KV head's line, at most: they are counted in 32 bits
-    const double tiles = (double)s->B * ((double)T_new * (s->Hq / s->Hkv) / kFew + 2);
-    if (tiles * ((double)p->M * p->P / unit_keys(s->dtype) + 1) * 2 > 2e9 || (double)s->B * s->Hq * T_new > 2e9) return RS_UNSUPPORTED;
+    // places of a KV head's line, at most: they are counted in 32 bits
+    const double own = (double)T_new * (s->Hq / s->Hkv), tokens = (double)p->M * p->P;
+    const double few = s->B * (own / kFew + 2) * (tokens / (s->dtype == RS_BF16 ? kKeys<bf16> : kKeys<float>) + 3);
+    const double many = s->B * (own / kMany + 2) * (tokens / 128 + 2);
+    if ((paged_layout(s, T_new).own_many ? many : few) * 2 > 2e9 || (double)s->B * s->Hq * T_new > 2e9) return RS_UNSUPPORTED;
     return RS_OK;
 }
 
 template <typename ST, int D>
-static void paged_launch(const PagedParams &a, hipStream_t stream)
+static void paged_launch(const PagedParams &a, bool one_tile, hipStream_t stream)
 {
-    paged_attend_kernel<ST, D><<<(unsigned)a.groups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
+    paged_attend_kernel<ST, D><<<kPagedGroups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
     const long rows = (long)a.B * a.Hq * a.T;
-    if (a.share) paged_join_rows_kernel<ST, D><<<(unsigned)(rows < 2048 ? rows : 2048), kPagedThreads, 0, stream>>>(a);
-    else paged_join_cuts_kernel<ST, D><<<(unsigned)a.groups, kPagedThreads, 0, stream>>>(a);
+    if (one_tile) paged_join_rows_kernel<ST, D><<<(unsigned)(rows < 2048 ? rows : 2048), kPagedThreads, 0, stream>>>(a);
+    else if (sizeof(ST) == 2) paged_join_cuts_kernel<ST, D, true><<<kPagedGroups, kPagedThreads, 0, stream>>>(a);
+    else paged_join_cuts_kernel<ST, D, false><<<kPagedGroups * kPagedWaves, kPagedThreads, 0, stream>>>(a);
 }
 
 }  // namespace rs
@@ -1141,22 +1227,21 @@ int32_t attn_paged(const rs_shape *s, const rs_pool *p, const void *q, const voi
     PagedParams a;
     a.q = q, a.k = k_pool, a.v = v_pool;
     a.table = table, a.len = len, a.seq = seq, a.n_new = n_new;
-    a.share = x.rows > 0 ? share : nullptr;
+    a.share = x.shares ? share : nullptr;
     a.out = out, a.lse = lse_out;
     a.cut_o = (float *)((char *)ws + RS_WS_CTRL_BYTES), a.row_o = a.cut_o + x.cut * s->D;
     a.cut_ml = (float *)((char *)ws + x.off_ml), a.row_ml = a.cut_ml + x.cut * 2;
     a.plan = (char *)ws + x.off_plan;
+    a.few_base = (long)x.many, a.few_rows = x.few_rows, a.own_many = x.own_many;
     a.B = s->B, a.Hq = s->Hq, a.Hkv = s->Hkv, a.G = s->Hq / s->Hkv;
-    a.S = p->S, a.M = p->M, a.N = p->N, a.shift = __builtin_ctz((unsigned)p->P), a.T = T_new, a.groups = kPagedGroups;
-    a.own_rows = many_rows(s, (long)T_new * a.G) ? kMany : kFew;
-    a.cut_rows = (int)(x.cut / (2 * kPagedGroups));
+    a.S = p->S, a.M = p->M, a.N = p->N, a.shift = __builtin_ctz((unsigned)p->P), a.T = T_new;
     a.scale = scale;
     if (s->dtype == RS_BF16) {
-        if (s->D == 128) paged_launch<bf16, 128>(a, (hipStream_t)stream);
-        else paged_launch<bf16, 64>(a, (hipStream_t)stream);
+        if (s->D == 128) paged_launch<bf16, 128>(a, x.shares, (hipStream_t)stream);
+        else paged_launch<bf16, 64>(a, x.shares, (hipStream_t)stream);
     } else {
-        if (s->D == 128) paged_launch<float, 128>(a, (hipStream_t)stream);
-        else paged_launch<float, 64>(a, (hipStream_t)stream);
+        if (s->D == 128) paged_launch<float, 128>(a, x.shares, (hipStream_t)stream);
+        else paged_launch<float, 64>(a, x.shares, (hipStream_t)stream);
     }
     return launch_status();
 }
