@@ -17,8 +17,8 @@
 // second product as it is.
 //
 // Work.  The tiles of each kind, cut into units of keys, form a line: of every segment (a run's shared pages, a sequence's own) its
-// tiles, per KV head.  Every wave takes an equal share of the line of few-row tiles and every workgroup one of the line of many-row
-// tiles, whatever the lengths are (every other workgroup the one first, so that a CU has both at hand).  Where a line is cut follows from the
+// tiles, per KV head.  The workgroups are divided between the kinds by the bytes of their keys, side by side on the CUs; every wave takes an
+// equal share of the line of few-row tiles, every workgroup one of the line of many-row tiles, whatever the lengths are.  Where a line is cut follows from the
 // lengths alone: each workgroup works it out for itself, by a prefix sum over the list, so lengths live on the device and nothing has to
 // be planned by the host.  What a share holds of a tile goes to one of its two boundary records if the tile goes on in another
 // share, to the row's record if the row has a second part (shared and own), else straight to the output; a second launch joins the records.
@@ -199,26 +199,38 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
     __syncthreads();
 }
 
+// How many of the workgroups take many-row tiles: by the bytes of both kinds' keys, a multiple of the eight XCDs, at least eight for
+// each kind that there is.
+__device__ __forceinline__ int many_groups(int few_line, int many_line)
+{
+    if (many_line == 0 || few_line == 0) return many_line > 0 ? kPagedGroups : 0;
+    const float many = (float)many_line * 4.f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
+    return 8 * max(1, min(kPagedGroups / 8 - 1, (int)(part * (kPagedGroups / 8) + 0.5f)));
+}
 // A line's division into shares, equal but for one place: the first `more` have each + 1.  No more shares than places.
 template <bool MANY>
 struct Shares {
     int line, n, more;  // places of a KV head, shares
-    long all, each;
+    int each;
+    long all;
     double per, per1;   // 1 / each, 1 / (each + 1)
-    __device__ __forceinline__ Shares(int line, int Hkv) : line(line)
+    __device__ __forceinline__ Shares(const Plan &pl, int B, int Hkv)
     {
-        constexpr int MOST = MANY ? kPagedGroups : kPagedGroups * kPagedWaves;  // (a power of two)
+        const int f = scalar(pl.start[0][B]), m = scalar(pl.start[1][B]), groups = many_groups(f, m);
+        line = MANY ? m : f;
         all = (long)line * Hkv;
-        n = all < MOST ? (int)all : MOST;
-        each = n == MOST ? all / MOST : 1;
-        more = (int)(all - each * n);
+        const int most = MANY ? groups : (kPagedGroups - groups) * kPagedWaves;
+        n = all < most ? (int)all : most;
+        each = n > 0 ? (int)((double)all / (double)n) : 1;
+        if ((long)each * n > all) --each;  // (the quotient may be rounded up)
+        more = (int)(all - (long)each * n);
         per = 1. / (double)each;
         per1 = 1. / (double)(each + 1);
     }
-    __device__ __forceinline__ long begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ long begin(int w) const { return (long)w * each + min(w, more); }
     __device__ __forceinline__ int owner(long place) const
     {
-        const long big = more * (each + 1);
+        const long big = (long)more * (each + 1);
         int w = place < big ? (int)((double)place * per1) : more + (int)((double)(place - big) * per);
         w = max(0, min(w, n - 1));
         if (begin(w) > place) --w;  // (the quotient is within one of the true one)
@@ -957,47 +969,46 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
         }
         return false;
     };
-    // Workgroups are dealt to the eight XCDs in turn: those of one XCD take neighbouring shares of a line, tiles of one KV head
-    // as a rule, whose rows they find in their L2; less work than workgroups goes to all XCDs.
-    const int spread = (int)(blockIdx.x % 8 * (kPagedGroups / 8) + blockIdx.x / 8);
-    const Shares<false> few(scalar(pl.start[0][a.B]), a.Hkv);
-    const int few_me = few.n < kPagedGroups * kPagedWaves ? wave * kPagedGroups + (int)blockIdx.x : spread * kPagedWaves + wave;
-    const long few_end = few_me < few.n ? few.begin(few_me + 1) : 0, few_begin = few_me < few.n ? few.begin(few_me) : 0;
-    long few_at = few_begin;
-    TileWork first;  // of this wave's few-row tiles
-    bool few_more = next(std::false_type{}, first, few_at, few_begin, few_end, few.line, few_me);
+    // Workgroups are dealt to the eight XCDs in turn, and there in turn to the CUs.  On every XCD the two kinds are spread evenly, and
+    // those of one XCD take neighbouring shares of a line, tiles of one KV head as a rule, whose rows they find in their L2; less
+    // work than workgroups goes to all XCDs.
+    const int xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8, groups = many_groups(scalar(pl.start[0][a.B]), scalar(pl.start[1][a.B]));
+    const int each = groups / 8, before = in_xcd * each / (kPagedGroups / 8);  // many-row workgroups of an XCD, those before this one
+    if ((in_xcd + 1) * each / (kPagedGroups / 8) > before) {
+        if constexpr (sizeof(ST) == 2) {
+            const Shares<true> sh(pl, a.B, a.Hkv);
+            const int me = sh.n < groups ? before * 8 + xcd : xcd * each + before;
+            if (me < sh.n) {
+                const long wb = sh.begin(me), we = sh.begin(me + 1);
+                long at = wb;
+                TileWork w, then;
+                bool more = next(std::true_type{}, w, at, wb, we, sh.line, me);
 #pragma unroll 1
-    for (int phase = 0; phase < 2; ++phase) {
-        if ((phase ^ (blockIdx.x >> 3)) & 1) {
-            if constexpr (sizeof(ST) == 2) {
-                const Shares<true> many(scalar(pl.start[1][a.B]), a.Hkv);
-                const int me = many.n < kPagedGroups ? (int)blockIdx.x : spread;
-                if (me < many.n) {
-                    const long wb = many.begin(me), we = many.begin(me + 1);
-                    long at = wb;
-                    TileWork w, then;
-                    bool more = next(std::true_type{}, w, at, wb, we, many.line, me);
-#pragma unroll 1
-                    while (more) {
-                        more = next(std::true_type{}, then, at, wb, we, many.line, me);
-                        attend_many<D>(a, pl, w, ring);
-                        w = then;
-                    }
+                while (more) {
+                    more = next(std::true_type{}, then, at, wb, we, sh.line, me);
+                    attend_many<D>(a, pl, w, ring);
+                    w = then;
                 }
             }
-        } else {
-            char *const even = wave == 0 ? k0 : wave == 1 ? k2 : wave == 2 ? v0 : v2, *const odd = wave == 0 ? k1 : wave == 1 ? k3 : wave == 2 ? v1 : v3;
-            TileWork w = first;
+        }
+    } else {
+        char *const even = wave == 0 ? k0 : wave == 1 ? k2 : wave == 2 ? v0 : v2, *const odd = wave == 0 ? k1 : wave == 1 ? k3 : wave == 2 ? v1 : v3;
+        const Shares<false> sh(pl, a.B, a.Hkv);
+        const int mine = in_xcd - before, of = kPagedGroups / 8 - each;  // few-row workgroups of the XCD
+        const int me = sh.n < of * 8 * kPagedWaves ? (wave * of + mine) * 8 + xcd : (xcd * of + mine) * kPagedWaves + wave;
+        if (me < sh.n) {
+            const long wb = sh.begin(me), we = sh.begin(me + 1);
+            long at = wb;
+            TileWork w, then;
+            bool more = next(std::false_type{}, w, at, wb, we, sh.line, me);
 #pragma unroll 1
-            while (few_more) {
-                TileWork then;
-                few_more = next(std::false_type{}, then, few_at, few_begin, few_end, few.line, few_me);
+            while (more) {
+                more = next(std::false_type{}, then, at, wb, we, sh.line, me);
                 if (w.rows - w.rt * kFew <= 16) attend_few<ST, D, 1>(a, pl, w, even, odd);
                 else attend_few<ST, D, 2>(a, pl, w, even, odd);
                 w = then;
             }
         }
-        __syncthreads();  // (the other phase uses the same LDS)
     }
 }
 
@@ -1083,8 +1094,8 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_rows_kernel(const Pa
     const Plan pl(a.plan, a.B);
     const int c4 = threadIdx.x % J::C4, grp = threadIdx.x / J::C4;
     const long rows = (long)a.B * a.Hq * a.T;
-    const Shares<false> few(pl.start[0][a.B], a.Hkv);
-    const Shares<true> many(pl.start[1][a.B], a.Hkv);
+    const Shares<false> few(pl, a.B, a.Hkv);
+    const Shares<true> many(pl, a.B, a.Hkv);
     for (long row = blockIdx.x; row < rows; row += gridDim.x) {
         const int t = (int)(row % a.T), hq = (int)(row / a.T % a.Hq), b = (int)(row / a.T / a.Hq);
         const Seq x = pl.seq[b];
@@ -1130,7 +1141,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const Pa
             j.put(a, (long)(b * a.Hq + e / none) * a.T + e % none, c4);
         }
     }
-    const Shares<MANY> sh(pl.start[MANY][a.B], a.Hkv);
+    const Shares<MANY> sh(pl, a.B, a.Hkv);
     if ((int)blockIdx.x + 1 >= sh.n) return;
     const long cut = sh.begin(blockIdx.x + 1);
     TileWork w;
