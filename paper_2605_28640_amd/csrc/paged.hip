@@ -56,6 +56,7 @@ struct PagedParams {
     float *cut_o, *cut_ml;      // boundary records: [2 shares][rows of a tile] x D, x 2; those of many-row tiles first
     float *row_o, *row_ml;      // row records: [shared, own][B Hq T] x D, x 2
     char *plan;                 // the first workgroup's plan, for the join
+    struct JoinEntry *entries;  // [B][Hkv], for the join where a sequence's rows are one tile, else nullptr
     long few_base;              // the first row of the few-row tiles' boundary records
     int few_rows;               // rows that a few-row tile of this call can have
     int own_many;               // whether a sequence's own tiles are of many rows
@@ -82,6 +83,8 @@ struct Plan {
     }
 };
 static size_t plan_bytes(int B) { return (size_t)B * 16 + (size_t)(5 * B + 2) * 4; }
+constexpr size_t plan_room(int B) { return ((size_t)B * 16 + (size_t)(5 * B + 2) * 4 + 255) & ~(size_t)255; }
+constexpr int kPlanShares = 256;  // bytes before the plan in the workspace: how both lines are divided
 
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ long scalar(long x)
@@ -93,7 +96,7 @@ __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 // A tile of n units takes n places of its line and, before them, what beginning and ending a tile costs in units; a tile
 // without units none.
 template <bool MANY>
-constexpr int kBefore = MANY ? 1 : 2;
+constexpr int kBefore = MANY ? 2 : 3;
 template <bool MANY>
 __device__ __forceinline__ int places(int n)
 {
@@ -204,37 +207,66 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
 __device__ __forceinline__ int many_groups(int few_line, int many_line)
 {
     if (many_line == 0 || few_line == 0) return many_line > 0 ? kPagedGroups : 0;
-    const float many = (float)many_line * 4.f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
+    const float many = (float)many_line * 5.f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
     return 8 * max(1, min(kPagedGroups / 8 - 1, (int)(part * (kPagedGroups / 8) + 0.5f)));
 }
-// A line's division into shares, equal but for one place: the first `more` have each + 1.  No more shares than places.
+// A line's division into shares.  With few places, equal ones, no more than there are places.  Else shares by the eight XCDs, in each those of
+// its first 32 workgroups 11 places for every 9 of the others': two workgroups are on a CU, and the one that came first is served
+// first by its memory path (four sequences of 65536 tokens, 8 heads, with equal shares: every one of the first 256 workgroups done after
+// 131-145 us, every other after 157-171).
 template <bool MANY>
 struct Shares {
-    int line, n, more;  // places of a KV head, shares
-    int each;
+    static constexpr int kOlder = 11, kNewer = 9;
+    int line, n;             // places of a KV head, shares
+    int of_xcd, older, sum;  // shares of an XCD, those of its first workgroups, their places' weights together (0: equal shares)
+    int each, more;          // equal shares: the first `more` have each + 1
     long all;
-    double per, per1;   // 1 / each, 1 / (each + 1)
+    double unit, per_unit;   // places for each unit of weight (equal shares: of a share), and 1 / unit
+    Shares() = default;
     __device__ __forceinline__ Shares(const Plan &pl, int B, int Hkv)
     {
+        static_assert(sizeof(Shares) <= kPlanShares / 2, "room in the workspace");
         const int f = scalar(pl.start[0][B]), m = scalar(pl.start[1][B]), groups = many_groups(f, m);
         line = MANY ? m : f;
         all = (long)line * Hkv;
-        const int most = MANY ? groups : (kPagedGroups - groups) * kPagedWaves;
-        n = all < most ? (int)all : most;
-        each = n > 0 ? (int)((double)all / (double)n) : 1;
-        if ((long)each * n > all) --each;  // (the quotient may be rounded up)
-        more = (int)(all - (long)each * n);
-        per = 1. / (double)each;
-        per1 = 1. / (double)(each + 1);
+        const int half = groups / 16;  // many-row workgroups among an XCD's first 32
+        of_xcd = MANY ? groups / 8 : (kPagedGroups - groups) / 8 * kPagedWaves;
+        older = MANY ? half : (kPagedGroups / 16 - half) * kPagedWaves;
+        n = 8 * of_xcd;
+        sum = 0;
+        each = 1, more = 0, unit = 1.;
+        if (all >= 4l * n) {
+            sum = older * kOlder + (of_xcd - older) * kNewer;
+            unit = n > 0 ? (double)all / (8. * sum) : 1.;
+        } else {
+            n = (int)min((long)n, all);
+            if (n > 0) {
+                each = (int)all / n;
+                more = (int)all - each * n;
+                unit = (double)all / n;
+            }
+        }
+        per_unit = 1. / unit;
     }
-    __device__ __forceinline__ long begin(int w) const { return (long)w * each + min(w, more); }
+    __device__ __forceinline__ long begin(int w) const
+    {
+        if (sum == 0) return w * each + min(w, more);
+        if (w >= n) return all;
+        const int x = w / of_xcd, i = w - x * of_xcd;
+        return (long)((double)(x * sum + min(i, older) * kOlder + max(i - older, 0) * kNewer) * unit);
+    }
     __device__ __forceinline__ int owner(long place) const
     {
-        const long big = (long)more * (each + 1);
-        int w = place < big ? (int)((double)place * per1) : more + (int)((double)(place - big) * per);
+        int w;
+        if (sum == 0) {
+            w = (int)((double)place * per_unit);
+        } else {
+            const int at = (int)((double)place * per_unit), x = at / sum, r = at - x * sum;
+            w = x * of_xcd + (r < older * kOlder ? r / kOlder : older + (r - older * kOlder) / kNewer);
+        }
         w = max(0, min(w, n - 1));
-        if (begin(w) > place) --w;  // (the quotient is within one of the true one)
-        if (begin(w + 1) <= place) ++w;
+        while (w > 0 && begin(w) > place) --w;  // (at most a step or two: the quotients are rounded)
+        while (w + 1 < n && begin(w + 1) <= place) ++w;
         return w;
     }
 };
@@ -922,6 +954,64 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     }
 }
 
+// The shares that a tile's records come from: w0 .. w1 (none: w1 < w0).  One share: the row's record; else boundary records, the second one
+// of share w0 where that began before the tile.
+struct Span {
+    int w0, w1, begun;
+};
+template <bool MANY>
+__device__ __forceinline__ Span span_of(const Shares<MANY> &sh, long s0, int units)
+{
+    if (units == 0) return Span{0, -1, 0};
+    const int w0 = sh.owner(s0), w1 = s0 + units <= sh.begin(w0 + 1) ? w0 : sh.owner(s0 + units - 1);
+    return Span{w0, w1, s0 > sh.begin(w0) ? 1 : 0};
+}
+// What the join of the rows of a list's entry and KV head goes by, where they are one tile of their own.  Worked out by a wave of each of the
+// first launch's workgroups, so that the second launch has nothing to do but to fetch.
+struct JoinEntry {
+    Span own, shared[2];  // of the own tile; of the run's tiles that hold the entry's rows (they may go on in a second one)
+    int n, row0, many;    // new tokens; the first row in the run's tile; whether that is of many rows
+};
+template <typename ST, bool MANY>
+__device__ __forceinline__ Span shared_span(const PagedParams &a, const Plan &pl, const Shares<MANY> &sh, const Seq &x, int tile, int kvh)
+{
+    const int units = div_up(x.c << a.shift, kUnit<ST, MANY>), rows = pl.members[x.first] * a.T * a.G;
+    const long s0 = (long)kvh * sh.line + pl.start[MANY][x.first] + (long)tile * places<MANY>(units) + kBefore<MANY>;
+    return span_of<MANY>(sh, s0, tile * (MANY ? kMany : kFew) < rows ? units : 0);
+}
+template <typename ST, bool MANY>
+__device__ __forceinline__ Span own_span(const PagedParams &a, const Plan &pl, const Shares<MANY> &sh, const Seq &x, int b, int kvh)
+{
+    int k0, k1;
+    const int units = own_units<ST, MANY>(x, 0, a.G, a.shift, k0, k1), rows = pl.members[b] * a.T * a.G;
+    long s0 = (long)kvh * sh.line + pl.start[MANY][b] + kBefore<MANY>;
+    if (rows > 0 && x.c > 0 && shared_is_many<ST>(rows) == MANY)
+        s0 += (long)div_up(rows, MANY ? kMany : kFew) * places<MANY>(div_up(x.c << a.shift, kUnit<ST, MANY>));
+    return span_of<MANY>(sh, s0, units);
+}
+// a part of the entry: 0: its own tile and the numbers, 1, 2: the run's tiles (a thread each: the divisions take their time)
+template <typename ST>
+__device__ __forceinline__ void fill_join_entry(const PagedParams &a, const Plan &pl, const Shares<false> &few, const Shares<true> &many, int b, int kvh,
+                                                int part, JoinEntry &e)
+{
+    const Seq x = pl.seq[b];
+    const bool shared_many = x.c > 0 && shared_is_many<ST>(pl.members[x.first] * a.T * a.G);
+    const int rows = shared_many ? kMany : kFew, row = (b - x.first) * a.T * a.G;
+    if (part == 0) {
+        if (sizeof(ST) == 2 && a.own_many) e.own = own_span<ST, true>(a, pl, many, x, b, kvh);
+        else e.own = own_span<ST, false>(a, pl, few, x, b, kvh);
+        e.n = x.n;
+        e.row0 = row % rows;
+        e.many = shared_many;
+    } else if (x.c == 0) {
+        e.shared[part - 1] = Span{0, -1, 0};
+    } else if (shared_many) {
+        e.shared[part - 1] = shared_span<ST, true>(a, pl, many, x, row / rows + part - 1, kvh);
+    } else {
+        e.shared[part - 1] = shared_span<ST, false>(a, pl, few, x, row / rows + part - 1, kvh);
+    }
+}
+
 template <typename ST, int D>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const PagedParams a)
 {
@@ -938,8 +1028,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
     const Ring ring{k0, k1, k2, k3, v0, v1, v2, v3};
     const Plan pl(lds_plan, a.B);
     make_plan<ST>(a, pl);
+    const Shares<false> few(pl, a.B, a.Hkv);
+    const Shares<true> many(pl, a.B, a.Hkv);
     if (blockIdx.x == 0) {  // for the join
-        const Plan to(a.plan, a.B);
+        const Plan to(a.plan + kPlanShares, a.B);
+        if (threadIdx.x == 0) {
+            *reinterpret_cast<Shares<false> *>(a.plan) = few;
+            *reinterpret_cast<Shares<true> *>(a.plan + kPlanShares / 2) = many;
+        }
         for (int b = threadIdx.x; b <= a.B; b += kPagedThreads) {
             to.start[0][b] = pl.start[0][b];
             to.start[1][b] = pl.start[1][b];
@@ -950,6 +1046,10 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
         }
     }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (a.entries && wave == kPagedWaves - 1) {  // (here, and not when all is done: what it needs would have to be kept in registers until then)
+        for (int p = blockIdx.x + kPagedGroups * (lane_id() / 4); p < a.B * a.Hkv; p += kPagedGroups * 16)
+            if (lane_id() % 4 < 3) fill_join_entry<ST>(a, pl, few, many, p / a.Hkv, p % a.Hkv, lane_id() % 4, a.entries[p]);
+    }
     // the next part of a share, with the first entries of its table row on their way
     auto next = [&](auto many_tag, TileWork &w, long &at, long wb, long we, int line, int share) __attribute__((always_inline)) -> bool {
         constexpr bool MANY = decltype(many_tag)::value;
@@ -976,7 +1076,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
     const int each = groups / 8, before = in_xcd * each / (kPagedGroups / 8);  // many-row workgroups of an XCD, those before this one
     if ((in_xcd + 1) * each / (kPagedGroups / 8) > before) {
         if constexpr (sizeof(ST) == 2) {
-            const Shares<true> sh(pl, a.B, a.Hkv);
+            const Shares<true> &sh = many;
             const int me = sh.n < groups ? before * 8 + xcd : xcd * each + before;
             if (me < sh.n) {
                 const long wb = sh.begin(me), we = sh.begin(me + 1);
@@ -993,7 +1093,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
         }
     } else {
         char *const even = wave == 0 ? k0 : wave == 1 ? k2 : wave == 2 ? v0 : v2, *const odd = wave == 0 ? k1 : wave == 1 ? k3 : wave == 2 ? v1 : v3;
-        const Shares<false> sh(pl, a.B, a.Hkv);
+        const Shares<false> &sh = few;
         const int mine = in_xcd - before, of = kPagedGroups / 8 - each;  // few-row workgroups of the XCD
         const int me = sh.n < of * 8 * kPagedWaves ? (wave * of + mine) * 8 + xcd : (xcd * of + mine) * kPagedWaves + wave;
         if (me < sh.n) {
@@ -1016,7 +1116,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
 // Records are joined by groups of D / 4 threads, 16 bytes of the row a thread.
 template <typename ST, int D>
 struct Join {
-    static constexpr int C4 = D / 4, NG = kPagedThreads / C4;
+    static constexpr int C4 = D / 4;
     float m = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     __device__ __forceinline__ void add(float m1, float l1, const f32x4 &v)
@@ -1028,13 +1128,13 @@ struct Join {
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + v[j] * f1;
     }
-    // every step-th record of a tile's row, from the lo-th on: its units are at s0 .. s1 - 1; row r of the tile; whole: its row record
+    // every step-th record of row r of a tile, from the lo-th on; whole: the row's own record
     template <bool MANY>
-    __device__ __forceinline__ void add_tile(const PagedParams &a, const Shares<MANY> &sh, long s0, long s1, int r, long whole, int lo, int step, int c4)
+    __device__ __forceinline__ void add_tile(const PagedParams &a, const Span &s, int r, long whole, int lo, int step, int c4)
     {
         constexpr int AHEAD = 4;  // records on their way together
-        const int w0 = sh.owner(s0), w1 = sh.owner(s1 - 1);
-        for (int w = w0 + lo; w <= w1; w += AHEAD * step) {
+        const bool one = s.w0 == s.w1;
+        for (int w = s.w0 + lo; w <= s.w1; w += AHEAD * step) {
             float2 ml[AHEAD];
             f32x4 v[AHEAD];
 #pragma unroll
@@ -1042,11 +1142,10 @@ struct Join {
                 const int x = w + i * step;
                 ml[i] = make_float2(-INFINITY, 0.f);
                 v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (x <= w1) {
-                    const int rec = record_of(s0, s1, sh.begin(x), sh.begin(x + 1));
-                    const long at = rec == 2 ? whole : cut_row<MANY>(a, x, rec) + r;
-                    ml[i] = *reinterpret_cast<const float2 *>((rec == 2 ? a.row_ml : a.cut_ml) + at * 2);
-                    v[i] = *reinterpret_cast<const f32x4 *>((rec == 2 ? a.row_o : a.cut_o) + at * D + 4 * c4);
+                if (x <= s.w1) {
+                    const long at = one ? whole : cut_row<MANY>(a, x, x == s.w0 ? s.begun : 0) + r;
+                    ml[i] = *reinterpret_cast<const float2 *>((one ? a.row_ml : a.cut_ml) + at * 2);
+                    v[i] = *reinterpret_cast<const f32x4 *>((one ? a.row_o : a.cut_o) + at * D + 4 * c4);
                 }
             }
 #pragma unroll
@@ -1061,87 +1160,59 @@ struct Join {
     }
 };
 
-// Where a sequence's rows are one tile: a workgroup for every row, its records divided among the thread groups.
-template <typename ST, int D, bool OWN>
-__device__ __forceinline__ bool own_part(const PagedParams &a, const Plan &pl, const Shares<OWN> &sh, Join<ST, D> &j, const Seq &x, int b, int kvh,
-                                         long row, int r, int grp, int c4)
-{
-    int k0, k1;
-    const int n = own_units<ST, OWN>(x, 0, a.G, a.shift, k0, k1);
-    if (n == 0) return false;
-    long s0 = (long)kvh * sh.line + pl.start[OWN][b] + kBefore<OWN>;
-    const int rows = pl.members[b] * a.T * a.G;
-    if (rows > 0 && x.c > 0 && shared_is_many<ST>(rows) == OWN) s0 += (long)div_up(rows, OWN ? kMany : kFew) * places<OWN>(div_up(x.c << a.shift, kUnit<ST, OWN>));
-    if (x.c == 0 && sh.owner(s0) == sh.owner(s0 + n - 1)) return true;  // written as it is
-    j.template add_tile<OWN>(a, sh, s0, s0 + n, r, (long)a.B * a.Hq * a.T + row, j.NG - 1 - grp, j.NG, c4);
-    return false;
-}
-template <typename ST, int D, bool MANY>
-__device__ __forceinline__ void shared_part(const PagedParams &a, const Plan &pl, const Shares<MANY> &sh, Join<ST, D> &j, int c, int lead, int kvh,
-                                            long row, int r, int grp, int c4)
-{
-    constexpr int ROWS = MANY ? kMany : kFew;
-    const int n = div_up(c << a.shift, kUnit<ST, MANY>);
-    const long s0 = (long)kvh * sh.line + pl.start[MANY][lead] + (long)(r / ROWS) * places<MANY>(n) + kBefore<MANY>;
-    j.template add_tile<MANY>(a, sh, s0, s0 + n, r % ROWS, row, grp, j.NG, c4);
-}
+// Where a sequence's rows are one tile: a wave for every row, the records divided among its 2 or 4 groups.  Nothing but trips to memory
+// (the entry, the records), so many waves and little arithmetic: with the spans worked out here by every wave the join of 2048 rows took 16 us
+// instead of 7.
 template <typename ST, int D>
-__global__ __launch_bounds__(kPagedThreads) void paged_join_rows_kernel(const PagedParams a)
+__global__ __launch_bounds__(64) void paged_join_rows_kernel(const PagedParams a)
 {
     using J = Join<ST, D>;
-    __shared__ float s_m[J::NG], s_l[J::NG];
-    __shared__ f32x4 s_o[J::NG][J::C4];
-    const Plan pl(a.plan, a.B);
+    constexpr int NG = 64 / J::C4;
     const int c4 = threadIdx.x % J::C4, grp = threadIdx.x / J::C4;
-    const long rows = (long)a.B * a.Hq * a.T;
-    const Shares<false> few(pl, a.B, a.Hkv);
-    const Shares<true> many(pl, a.B, a.Hkv);
-    for (long row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int t = (int)(row % a.T), hq = (int)(row / a.T % a.Hq), b = (int)(row / a.T / a.Hq);
-        const Seq x = pl.seq[b];
-        if (t >= x.n) continue;
-        const int kvh = hq / a.G, r = t * a.G + hq % a.G;
+    const int rows = a.B * a.Hq * a.T;
+    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
+        const int bh = row / a.T, t = row - bh * a.T, b = bh / a.Hq, hq = bh - b * a.Hq, kvh = hq / a.G, r = t * a.G + hq - kvh * a.G;
+        const JoinEntry e = a.entries[b * a.Hkv + kvh];
+        if (t >= e.n) continue;
+        const bool none = e.shared[0].w1 < e.shared[0].w0;
+        if (none && e.own.w0 == e.own.w1) continue;  // written as it is
         J j;
-        if (a.own_many ? own_part<ST, D, true>(a, pl, many, j, x, b, kvh, row, r, grp, c4) : own_part<ST, D, false>(a, pl, few, j, x, b, kvh, row, r, grp, c4))
-            continue;  // (the same for the whole workgroup)
-        if (x.c > 0) {
-            const int lead = x.first, at = (b - lead) * a.T * a.G + r;
-            if (shared_is_many<ST>(pl.members[lead] * a.T * a.G)) shared_part<ST, D, true>(a, pl, many, j, x.c, lead, kvh, row, at, grp, c4);
-            else shared_part<ST, D, false>(a, pl, few, j, x.c, lead, kvh, row, at, grp, c4);
+        if (a.own_many) j.template add_tile<true>(a, e.own, r, (long)rows + row, NG - 1 - grp, NG, c4);
+        else j.template add_tile<false>(a, e.own, r, (long)rows + row, NG - 1 - grp, NG, c4);
+        if (!none) {
+            const int in = e.row0 + r;
+            if (e.many) j.template add_tile<true>(a, e.shared[in >= kMany], in % kMany, row, grp, NG, c4);
+            else j.template add_tile<false>(a, e.shared[in >= kFew], in % kFew, row, grp, NG, c4);
         }
-        if (c4 == 0) {
-            s_m[grp] = j.m;
-            s_l[grp] = j.l;
-        }
-        s_o[grp][c4] = j.o;
-        __syncthreads();
-        if (grp == 0) {
-            J sum;
+        J sum;  // in the order of the groups, the same in all of them
 #pragma unroll
-            for (int i = 0; i < J::NG; ++i) sum.add(s_m[i], s_l[i], s_o[i][c4]);
-            sum.put(a, row, c4);
+        for (int i = 0; i < NG; ++i) {
+            f32x4 o;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = shfl_f(j.o[k], i * J::C4 + c4);
+            sum.add(shfl_f(j.m, i * J::C4), shfl_f(j.l, i * J::C4), o);
         }
-        __syncthreads();
+        if (grp == 0) sum.put(a, row, c4);
     }
 }
 
-// Where they are many: only the tiles that the line's cuts go through, workgroup i looking at the end of the i-th share; and the rows that see
+// Where they are many: only the tiles that the line's cuts go through, workgroups i looking at the end of the i-th share; and the rows that see
 // nothing, which may have no tile.
 template <typename ST, int D, bool MANY>
 __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const PagedParams a)
 {
     using J = Join<ST, D>;
-    constexpr int ROWS = MANY ? kMany : kFew;
-    const Plan pl(a.plan, a.B);
+    constexpr int ROWS = MANY ? kMany : kFew, NG = kPagedThreads / J::C4;
+    const Plan pl(a.plan + kPlanShares, a.B);
     const int c4 = threadIdx.x % J::C4, grp = threadIdx.x / J::C4;
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    for (int b = blockIdx.x; blockIdx.y == 0 && b < a.B; b += gridDim.x) {
         const int none = min(pl.seq[b].n - pl.seq[b].L, pl.seq[b].n);
-        for (int e = grp; e < none * a.Hq; e += J::NG) {
+        for (int e = grp; e < none * a.Hq; e += NG) {
             J j;
             j.put(a, (long)(b * a.Hq + e / none) * a.T + e % none, c4);
         }
     }
-    const Shares<MANY> sh(pl, a.B, a.Hkv);
+    const Shares<MANY> sh = *reinterpret_cast<const Shares<MANY> *>(a.plan + (MANY ? kPlanShares / 2 : 0));
     if ((int)blockIdx.x + 1 >= sh.n) return;
     const long cut = sh.begin(blockIdx.x + 1);
     TileWork w;
@@ -1149,11 +1220,12 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const Pa
     find_tile<ST, MANY>(a, pl, cut, sh.line, w, s0, s1);
     if (cut <= s0 || sh.begin(blockIdx.x) > s0) return;  // not through its units; not its first
     const int rows = min(w.rows - w.rt * ROWS, ROWS);
-    for (int r = grp; r < rows; r += J::NG) {
+    const Span span = span_of<MANY>(sh, s0, (int)(s1 - s0));
+    for (int r = blockIdx.y * NG + grp; r < rows; r += gridDim.y * NG) {
         int bq, t, g;
         if (!query_of(a, pl, w, w.rt * ROWS + r, bq, t, g)) continue;
         J j;
-        j.template add_tile<MANY>(a, sh, s0, s1, r, 0, 0, 1, c4);
+        j.template add_tile<MANY>(a, span, r, 0, 0, 1, c4);
         j.put(a, out_row(a, w, bq, t, g), c4);
     }
 }
@@ -1183,7 +1255,7 @@ static PagedLayout paged_layout(const rs_shape *s, int T_new)
     x.rows = x.shares ? (size_t)s->B * s->Hq * T_new * 2 : 0;
     x.off_ml = RS_WS_CTRL_BYTES + align256((x.cut + x.rows) * s->D * 4);
     x.off_plan = x.off_ml + align256((x.cut + x.rows) * 8);
-    x.total = x.off_plan + align256(plan_bytes(s->B));
+    x.total = x.off_plan + kPlanShares + plan_room(s->B) + align256((size_t)s->B * s->Hkv * sizeof(JoinEntry));
     return x;
 }
 
@@ -1203,12 +1275,12 @@ static int check_paged(const rs_shape *s, const rs_pool *p, int T_new)
 }
 
 template <typename ST, int D>
-static void paged_launch(const PagedParams &a, bool one_tile, hipStream_t stream)
+static void paged_launch(const PagedParams &a, hipStream_t stream)
 {
     paged_attend_kernel<ST, D><<<kPagedGroups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
     const long rows = (long)a.B * a.Hq * a.T;
-    if (one_tile) paged_join_rows_kernel<ST, D><<<(unsigned)(rows < 2048 ? rows : 2048), kPagedThreads, 0, stream>>>(a);
-    else if (sizeof(ST) == 2) paged_join_cuts_kernel<ST, D, true><<<kPagedGroups, kPagedThreads, 0, stream>>>(a);
+    if (a.entries) paged_join_rows_kernel<ST, D><<<(unsigned)(rows < 8192 ? rows : 8192), 64, 0, stream>>>(a);
+    else if (sizeof(ST) == 2) paged_join_cuts_kernel<ST, D, true><<<dim3(kPagedGroups, 4), kPagedThreads, 0, stream>>>(a);
     else paged_join_cuts_kernel<ST, D, false><<<kPagedGroups * kPagedWaves, kPagedThreads, 0, stream>>>(a);
 }
 
@@ -1243,16 +1315,17 @@ int32_t attn_paged(const rs_shape *s, const rs_pool *p, const void *q, const voi
     a.cut_o = (float *)((char *)ws + RS_WS_CTRL_BYTES), a.row_o = a.cut_o + x.cut * s->D;
     a.cut_ml = (float *)((char *)ws + x.off_ml), a.row_ml = a.cut_ml + x.cut * 2;
     a.plan = (char *)ws + x.off_plan;
+    a.entries = x.shares ? (JoinEntry *)(a.plan + kPlanShares + plan_room(s->B)) : nullptr;
     a.few_base = (long)x.many, a.few_rows = x.few_rows, a.own_many = x.own_many;
     a.B = s->B, a.Hq = s->Hq, a.Hkv = s->Hkv, a.G = s->Hq / s->Hkv;
     a.S = p->S, a.M = p->M, a.N = p->N, a.shift = __builtin_ctz((unsigned)p->P), a.T = T_new;
     a.scale = scale;
     if (s->dtype == RS_BF16) {
-        if (s->D == 128) paged_launch<bf16, 128>(a, x.shares, (hipStream_t)stream);
-        else paged_launch<bf16, 64>(a, x.shares, (hipStream_t)stream);
+        if (s->D == 128) paged_launch<bf16, 128>(a, (hipStream_t)stream);
+        else paged_launch<bf16, 64>(a, (hipStream_t)stream);
     } else {
-        if (s->D == 128) paged_launch<float, 128>(a, x.shares, (hipStream_t)stream);
-        else paged_launch<float, 64>(a, x.shares, (hipStream_t)stream);
+        if (s->D == 128) paged_launch<float, 128>(a, (hipStream_t)stream);
+        else paged_launch<float, 64>(a, (hipStream_t)stream);
     }
     return launch_status();
 }
