@@ -430,7 +430,8 @@ int32_t rat_state_copy(const rs_shape *s, float *state_k, float *state_v, int32_
  * (positions len - n_new[i] .. len - 1).  Sequences may hold different numbers of them.
  *   k, v [B, Hkv, T_new, D] dtype, g [B, Hkv, T_new, D] float32, B = s->B listed sequences; what lies past n_new[i] tokens is not read
  *   state_k, state_v [S, Hkv, D] float32, rows by sequence number, as in rat_scan
- *   meta: the bounds of every page that gets a row are brought up to date, or NULL
+ *   meta: every page that gets a row has its bounds formed anew from its rows so far (they need not have been current
+ *         before), or NULL
  *   n_new [B] int32 or NULL: T_new for each; counts above T_new are taken as T_new, below 0 as 0
  * Nothing is done for a sequence out of range, listed before, or with fewer than n_new tokens; rows whose table entry names
  * no page are not written.  Long prompts are better scanned as contiguous rows (rat_scan) and copied into their pages. */

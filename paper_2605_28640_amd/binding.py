@@ -89,6 +89,11 @@ SIGNATURES = {
 }
 
 
+# those of them that native.cpp takes apart too, in the order in which it is told their addresses
+_POOL_CALLS = ("page_pool_reserve", "page_pool_fork", "page_pool_free", "page_pool_compact", "page_pool_share", "page_copy",
+               "rat_state_copy", "rat_append_paged", "attn_paged")
+
+
 def load():
     """Load libratsparse.so; raises if it has not been built (no fallback exists)."""
     global _lib, _native
@@ -107,6 +112,7 @@ def load():
             raise RatsparseError("_native.so is not built: run `python -m paper_2605_28640_amd.build`") from e
         native.setup(*(ctypes.cast(getattr(lib, name), _vp).value for name in ("rat_scan", "sparse_attn_decode", "rat_decode_step")),
                      _check, torch._C._cuda_getCurrentRawStream, torch.cuda.current_device, rs_shape, Workspace)
+        native.setup_pool(*(ctypes.cast(getattr(lib, name), _vp).value for name in _POOL_CALLS), rs_pool)
         _native = native
         _lib = lib  # last: another thread that finds it set goes on without a look at the rest
     return _lib
@@ -339,6 +345,8 @@ def page_pool_workspace_bytes(p):
 
 
 def page_pool_reserve(p, table, len, refs, seq, want, T_new, granted, ws):
+    if _calls().page_pool_reserve(p, table, len, refs, seq, want, T_new, granted, ws):
+        return
     n = seq.numel()
     _check(load().page_pool_reserve(ctypes.byref(p), *_sequences(p, table, len, refs), _need(seq, torch.int32, n), n,
                                     _need(want, torch.int32, n), T_new, _need(granted, torch.int32, n), ws.ptr, ws.nbytes,
@@ -346,6 +354,8 @@ def page_pool_reserve(p, table, len, refs, seq, want, T_new, granted, ws):
 
 
 def page_pool_fork(p, table, len, refs, src, dst, pairs_out, carry_out, ws):
+    if _calls().page_pool_fork(p, table, len, refs, src, dst, pairs_out, carry_out, ws):
+        return
     n = src.numel()
     _check(load().page_pool_fork(ctypes.byref(p), *_sequences(p, table, len, refs), _need(src, torch.int32, n),
                                  _need(dst, torch.int32, n), n, _need(pairs_out, torch.int32, n, 2),
@@ -353,24 +363,32 @@ def page_pool_fork(p, table, len, refs, src, dst, pairs_out, carry_out, ws):
 
 
 def page_pool_free(p, table, len, refs, seq, ws):
+    if _calls().page_pool_free(p, table, len, refs, seq, ws):
+        return
     n = seq.numel()
     _check(load().page_pool_free(ctypes.byref(p), *_sequences(p, table, len, refs), _need(seq, torch.int32, n), n, ws.ptr,
                                  ws.nbytes, _stream()))
 
 
 def page_pool_compact(p, table, len, refs, pairs_out, n_pairs_out, ws):
+    if _calls().page_pool_compact(p, table, len, refs, pairs_out, n_pairs_out, ws):
+        return
     _check(load().page_pool_compact(ctypes.byref(p), *_sequences(p, table, len, refs),
                                     _need(pairs_out, torch.int32, max(p.N // 2, 1), 2), _need(n_pairs_out, torch.int32, 1),
                                     ws.ptr, ws.nbytes, _stream()))
 
 
 def page_pool_share(p, table, len, seq, min_pages, share_out):
+    if _calls().page_pool_share(p, table, len, seq, min_pages, share_out):
+        return
     n = seq.numel()
     _check(load().page_pool_share(ctypes.byref(p), _need(table, torch.int32, p.S, p.M), _need(len, torch.int32, p.S),
                                   _need(seq, torch.int32, n), n, min_pages, _need(share_out, torch.int32, n, 3), _stream()))
 
 
 def page_copy(s_src, k_src, v_src, meta_src, s_dst, k_dst, v_dst, meta_dst, pairs, n_pairs):
+    if _calls().page_copy(s_src, k_src, v_src, meta_src, s_dst, k_dst, v_dst, meta_dst, pairs, n_pairs):
+        return
     n = pairs.shape[0]
     _check(load().page_copy(ctypes.byref(s_src), *_rows(s_src, k_src, v_src, meta_src), ctypes.byref(s_dst),
                             *_rows(s_dst, k_dst, v_dst, meta_dst), _need(pairs, torch.int32, n, 2), n,
@@ -378,12 +396,17 @@ def page_copy(s_src, k_src, v_src, meta_src, s_dst, k_dst, v_dst, meta_dst, pair
 
 
 def rat_state_copy(s, state_k, state_v, pairs):
+    if _calls().rat_state_copy(s, state_k, state_v, pairs):
+        return
     S, n = state_k.shape[0], pairs.shape[0]
     _check(load().rat_state_copy(ctypes.byref(s), _need(state_k, torch.float32, S, s.Hkv, s.D),
                                  _need(state_v, torch.float32, S, s.Hkv, s.D), S, _need(pairs, torch.int32, n, 2), n, _stream()))
 
 
 def rat_append_paged(s, p, k, v, g, state_k, state_v, k_pool, v_pool, meta, table, len, seq, n_new, T_new):
+    if _calls().rat_append_paged(s, p, k, v, g, state_k, state_v, k_pool, v_pool, meta, table, len, seq, n_new,
+                                 T_new):
+        return
     dt, new, carry = k.dtype, (s.B, s.Hkv, T_new, s.D), (p.S, s.Hkv, s.D)
     if _dtype_code(k) != s.dtype:
         raise RatsparseError("k is not of the shape's type")
@@ -400,6 +423,8 @@ def attn_paged_workspace_bytes(s, p, T_new):
 
 
 def attn_paged(s, p, q, k_pool, v_pool, table, len, seq, n_new, T_new, share, scale, out, lse_out, ws):
+    if _calls().attn_paged(s, p, q, k_pool, v_pool, table, len, seq, n_new, T_new, share, scale, out, lse_out, ws):
+        return
     dt, rows = q.dtype, (s.B, s.Hq, T_new)
     if _dtype_code(q) != s.dtype:
         raise RatsparseError("q is not of the shape's type")

@@ -422,64 +422,282 @@ struct AppendParams {
     int Hkv, S, M, N, shift, T_new;
 };
 
-// The recurrence over a sequence's new tokens, a thread for every (sequence, KV head, channel): s = g s + (1 - g) x in float32, the
-// rounded state to the token's row, its key into the page's bounds.
+// What an append's workgroup works on: 64 channels of one KV head of one listed sequence, 8 of them a lane, `slice` being the lane's place among those
+// that hold the same channels.
 template <typename ST, int D>
-__global__ __launch_bounds__(256) void append_paged_kernel(const AppendParams a)
-{
-    const int b = blockIdx.x, s = a.seq[b];
-    if (s < 0 || s >= a.S) return;
-    int again = 0;  // listed before: nothing is appended twice
-    for (int o = threadIdx.x; o < b; o += 256) again |= a.seq[o] == s;
-    if (__syncthreads_or(again)) return;
-    int n = a.n_new ? a.n_new[b] : a.T_new;
-    n = n < 0 ? 0 : n > a.T_new ? a.T_new : n;
-    const int L = a.len[s], P = 1 << a.shift;
-    if (n == 0 || L < n || L > (long)a.M << a.shift) return;
-    const int e = blockIdx.y * 256 + threadIdx.x;  // head * D + channel
-    if (e >= a.Hkv * D) return;
-    const int h = e / D, c = e % D;
-    const long st = (long)s * a.Hkv * D + e;
-    float sk = a.state_k[st], sv = a.state_v[st];
-    const long in0 = ((long)(b * a.Hkv + h) * a.T_new) * D + c;
-    const ST *k = (const ST *)a.k + in0, *v = (const ST *)a.v + in0;
-    const float *g = a.g + in0;
-    const int32_t *row = a.table + (long)s * a.M;
-    const long rows = (long)a.N << a.shift;
-    ST *kp = (ST *)a.k_pool + (long)h * rows * D + c, *vp = (ST *)a.v_pool + (long)h * rows * D + c;
-    ST *mt = a.meta ? (ST *)a.meta + (long)h * a.N * 2 * D + c : nullptr;
-    int page = -1;
-    float lo = 0.f, hi = 0.f;
-    for (int t = 0; t < n; ++t) {
-        const int pos = L - n + t, in_page = pos & (P - 1);
-        if (t == 0 || in_page == 0) {
-            page = row[pos >> a.shift];
-            if (page < 0 || page >= a.N) page = -1;
+struct AppendPiece {
+    int b, s, L, n;     // list entry, sequence, its tokens, the new ones among them (0: nothing to do)
+    int h, c;           // KV head, the lane's first channel
+    long state, in;     // of the lane's channels: offset of the carry, of token 0's inputs
+    const int32_t *row;
+    ST *k_rows, *v_rows, *bounds;
+
+    // the same for the whole workgroup but for c, state, in, and the row pointers
+    __device__ __forceinline__ AppendPiece(const AppendParams &a)
+    {
+        b = blockIdx.x;
+        s = a.seq[b];
+        const int piece = blockIdx.y;
+        h = piece / (D / 64);
+        c = piece % (D / 64) * 64 + 8 * (threadIdx.x & 7);
+        n = a.n_new ? a.n_new[b] : a.T_new;
+        n = n < 0 ? 0 : n > a.T_new ? a.T_new : n;
+        int again = 0;  // listed before: nothing is appended twice
+        for (int o = threadIdx.x; o < b; o += blockDim.x) again |= a.seq[o] == s;
+        again = __syncthreads_or(again);
+        L = 0;
+        if (again || s < 0 || s >= a.S) {
+            n = 0;
+            s = 0;
+        } else {
+            L = a.len[s];
+            if (L < n || L > (long)a.M << a.shift) n = 0;
         }
-        const float gg = g[(long)t * D], om = 1.f - gg;
-        sk = fmaf(gg, sk, om * to_f32(k[(long)t * D]));
-        sv = fmaf(gg, sv, om * to_f32(v[(long)t * D]));
-        ST ks, vs;
-        from_f32(ks, sk);
-        from_f32(vs, sv);
-        if (page < 0) continue;
-        const long at = (((long)page << a.shift) + in_page) * D;
-        kp[at] = ks;
-        vp[at] = vs;
-        if (mt) {
-            const float x = to_f32(ks);
-            ST *m = mt + (long)page * 2 * D;
-            if (in_page == 0) lo = hi = x;
-            else if (t == 0) lo = fminf(to_f32(m[0]), x), hi = fmaxf(to_f32(m[D]), x);
-            else lo = fminf(lo, x), hi = fmaxf(hi, x);
-            if (t + 1 == n || in_page == P - 1) {
-                from_f32(m[0], lo);
-                from_f32(m[D], hi);
+        state = ((long)s * a.Hkv + h) * D + c;
+        in = ((long)(b * a.Hkv + h) * a.T_new) * D + c;
+        row = a.table + (long)s * a.M;
+        const long rows = (long)a.N << a.shift;
+        k_rows = (ST *)a.k_pool + (long)h * rows * D + c;
+        v_rows = (ST *)a.v_pool + (long)h * rows * D + c;
+        bounds = a.meta ? (ST *)a.meta + (long)h * a.N * 2 * D + c : nullptr;
+    }
+    // the row that holds a position; below 0: the table names no page for it
+    __device__ __forceinline__ long row_of(const AppendParams &a, int pos) const
+    {
+        const int page = row[pos >> a.shift];
+        return (page < 0 || page >= a.N) ? -1 : ((long)page << a.shift) + (pos & ((1 << a.shift) - 1));
+    }
+};
+
+// bounds of rows first, first + STEP, ... below `rows` of a page into lo and hi
+template <typename ST, int D, int STEP>
+__device__ __forceinline__ void fold_rows(const ST *page, int first, int rows, float (&lo)[8], float (&hi)[8])
+{
+    constexpr int AHEAD = STEP == 1 ? 16 : 4;  // on their way together
+    for (int r = first; r < rows; r += STEP * AHEAD) {
+        typename Row8<ST>::raw_t raw[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) raw[i] = Row8<ST>::load_raw(page + (long)(r + STEP * i < rows ? r + STEP * i : r) * D);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            float x[8];
+            Row8<ST>::unpack(raw[i], x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lo[j] = fminf(lo[j], x[j]), hi[j] = fmaxf(hi[j], x[j]);
+        }
+    }
+}
+// over the wave's eight slices, written by the first
+template <typename ST, int D>
+__device__ __forceinline__ void put_bounds(ST *bounds, int slice, float (&lo)[8], float (&hi)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int m = 8; m < 64; m <<= 1) lo[j] = fminf(lo[j], shfl_xor_f(lo[j], m)), hi[j] = fmaxf(hi[j], shfl_xor_f(hi[j], m));
+    if (slice == 0) {
+        Row8<ST>::store(bounds, lo);
+        Row8<ST>::store(bounds + D, hi);
+    }
+}
+
+// One token a sequence: s = g s + (1 - g) x in float32, the rounded state to the token's row, its page's bounds from the page's rows so
+// far, which need not have been current before.  Nothing but trips to memory: the list, then length and table, then the rows of the
+// page, everything else beside them; a wave for 64 channels, its eight slices reading the page's rows side by side.
+template <typename ST, int D>
+__global__ __launch_bounds__(64) void append_token_kernel(const AppendParams a)
+{
+    const AppendPiece<ST, D> x(a);
+    const int slice = threadIdx.x >> 3;
+    float sk[8], sv[8], k[8], v[8], g[8];
+    Row8<float>::load(a.state_k + x.state, sk);
+    Row8<float>::load(a.state_v + x.state, sv);
+    Row8<ST>::load((const ST *)a.k + x.in, k);
+    Row8<ST>::load((const ST *)a.v + x.in, v);
+    Row8<float>::load(a.g + x.in, g);
+    if (x.n == 0) return;
+    const long row = x.row_of(a, x.L - 1);
+    float lo[8], hi[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float om = 1.f - g[j];
+        sk[j] = fmaf(g[j], sk[j], om * k[j]);
+        sv[j] = fmaf(g[j], sv[j], om * v[j]);
+        ST y;
+        from_f32(y, sk[j]);
+        lo[j] = hi[j] = to_f32(y);
+    }
+    if (slice == 0) {
+        Row8<float>::store(a.state_k + x.state, sk);
+        Row8<float>::store(a.state_v + x.state, sv);
+        if (row >= 0) {
+            Row8<ST>::store(x.k_rows + row * D, sk);
+            Row8<ST>::store(x.v_rows + row * D, sv);
+        }
+    }
+    if (x.bounds && row >= 0) {
+        const int in_page = (int)(row & ((1 << a.shift) - 1));
+        fold_rows<ST, D, 8>(x.k_rows + (row - in_page) * D, slice, in_page, lo, hi);
+        put_bounds<ST, D>(x.bounds + (row >> a.shift) * 2 * D, slice, lo, hi);
+    }
+}
+
+// Several tokens a sequence.  The recurrence is linear, so a run of tokens is (A, S): s -> A s + S, and runs compose: a workgroup takes 32 W tokens at a
+// time, 4 a slice; every slice forms its run's (A, S), a scan over the slices (shuffles in a wave, LDS between waves) gives each
+// its first state, from which it goes through its 4 tokens as written.  The next tokens' inputs are on their way meanwhile.  Then the bounds
+// of the pages touched, from their rows.
+template <typename ST, int D, int W>
+__global__ __launch_bounds__(64 * W) void append_run_kernel(const AppendParams a)
+{
+    constexpr int R = 4, CHUNK = 8 * W * R;
+    __shared__ float s_run[2][W][3][64];
+    const AppendPiece<ST, D> x(a);
+    const int slice = (threadIdx.x & 63) >> 3, lane8 = threadIdx.x & 7, wave = threadIdx.x >> 6, n = x.n;
+    if (n == 0) return;  // (the whole workgroup)
+    struct Inputs {
+        typename Row8<ST>::raw_t k[R], v[R];
+        typename Row8<float>::raw_t g[R];
+        long row[R];
+    };
+    auto load = [&](int c0, Inputs &in) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int t = c0 + (wave * 8 + slice) * R + r, u = t < n ? t : n - 1;
+            in.k[r] = Row8<ST>::load_raw((const ST *)a.k + x.in + (long)u * D);
+            in.v[r] = Row8<ST>::load_raw((const ST *)a.v + x.in + (long)u * D);
+            in.g[r] = Row8<float>::load_raw(a.g + x.in + (long)u * D);
+            in.row[r] = t < n ? x.row_of(a, x.L - n + t) : -1;
+        }
+    };
+    float sk[8], sv[8];  // the carry before the chunk
+    Row8<float>::load(a.state_k + x.state, sk);
+    Row8<float>::load(a.state_v + x.state, sv);
+    Inputs in;
+    load(0, in);
+#pragma unroll 1
+    for (int c0 = 0, buf = 0; c0 < n; c0 += CHUNK, buf ^= 1) {
+        const Inputs cur = in;
+        if (c0 + CHUNK < n) load(c0 + CHUNK, in);
+        const int t0 = c0 + (wave * 8 + slice) * R;
+        float A[8], Sk[8], Sv[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) A[j] = 1.f, Sk[j] = Sv[j] = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float g[8], k[8], v[8];
+            Row8<float>::unpack(cur.g[r], g);
+            Row8<ST>::unpack(cur.k[r], k);
+            Row8<ST>::unpack(cur.v[r], v);
+            if (t0 + r < n) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float om = 1.f - g[j];
+                    A[j] *= g[j];
+                    Sk[j] = fmaf(g[j], Sk[j], om * k[j]);
+                    Sv[j] = fmaf(g[j], Sv[j], om * v[j]);
+                }
+            }
+        }
+        // up to and with this slice, within the wave
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float pA = __shfl_up(A[j], 8 * d, kWave), pk = __shfl_up(Sk[j], 8 * d, kWave), pv = __shfl_up(Sv[j], 8 * d, kWave);
+                if (slice >= d) {
+                    Sk[j] = fmaf(A[j], pk, Sk[j]);
+                    Sv[j] = fmaf(A[j], pv, Sv[j]);
+                    A[j] *= pA;
+                }
+            }
+        if (slice == 7) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s_run[buf][wave][0][lane8 * 8 + j] = A[j];
+                s_run[buf][wave][1][lane8 * 8 + j] = Sk[j];
+                s_run[buf][wave][2][lane8 * 8 + j] = Sv[j];
+            }
+        }
+        // before this slice, within the wave
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float pA = __shfl_up(A[j], 8, kWave), pk = __shfl_up(Sk[j], 8, kWave), pv = __shfl_up(Sv[j], 8, kWave);
+            A[j] = slice ? pA : 1.f;
+            Sk[j] = slice ? pk : 0.f;
+            Sv[j] = slice ? pv : 0.f;
+        }
+        __syncthreads();  // (two buffers: the one after next is written only after everyone has passed the next barrier)
+        float yk[8], yv[8];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (w == wave) {
+                    yk[j] = fmaf(A[j], sk[j], Sk[j]);
+                    yv[j] = fmaf(A[j], sv[j], Sv[j]);
+                }
+                const float wA = s_run[buf][w][0][lane8 * 8 + j];
+                sk[j] = fmaf(wA, sk[j], s_run[buf][w][1][lane8 * 8 + j]);
+                sv[j] = fmaf(wA, sv[j], s_run[buf][w][2][lane8 * 8 + j]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float g[8], k[8], v[8];
+            Row8<float>::unpack(cur.g[r], g);
+            Row8<ST>::unpack(cur.k[r], k);
+            Row8<ST>::unpack(cur.v[r], v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float om = 1.f - g[j];
+                yk[j] = fmaf(g[j], yk[j], om * k[j]);
+                yv[j] = fmaf(g[j], yv[j], om * v[j]);
+            }
+            if (t0 + r < n) {
+                if (cur.row[r] >= 0) {
+                    Row8<ST>::store(x.k_rows + cur.row[r] * D, yk);
+                    Row8<ST>::store(x.v_rows + cur.row[r] * D, yv);
+                }
+                if (t0 + r == n - 1) {  // (as this slice has it: the same bits as one token after the other from its first state)
+                    Row8<float>::store(a.state_k + x.state, yk);
+                    Row8<float>::store(a.state_v + x.state, yv);
+                }
             }
         }
     }
-    a.state_k[st] = sk;
-    a.state_v[st] = sv;
+    if (!x.bounds) return;
+    __syncthreads();  // all rows are written
+    const int j0 = (x.L - n) >> a.shift, j1 = (x.L - 1) >> a.shift;
+    float lo[8], hi[8];
+    if (a.shift <= 6) {  // small pages, many of them: one a slice
+        for (int j = j0 + wave * 8 + slice; j <= j1; j += 8 * W) {
+            const int page = x.row[j], rows = min(1 << a.shift, x.L - (j << a.shift));
+            if (page < 0 || page >= a.N) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
+            fold_rows<ST, D, 1>(x.k_rows + ((long)page << a.shift) * D, 0, rows, lo, hi);
+            Row8<ST>::store(x.bounds + (long)page * 2 * D, lo);
+            Row8<ST>::store(x.bounds + (long)page * 2 * D + D, hi);
+        }
+        return;
+    }
+    for (int j = j0 + wave; j <= j1; j += W) {
+        const int page = x.row[j], rows = min(1 << a.shift, x.L - (j << a.shift));
+        if (page < 0 || page >= a.N) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
+        fold_rows<ST, D, 8>(x.k_rows + ((long)page << a.shift) * D, slice, rows, lo, hi);
+        put_bounds<ST, D>(x.bounds + (long)page * 2 * D, slice, lo, hi);
+    }
+}
+
+template <typename ST, int D>
+static void append_launch(const AppendParams &a, int B, hipStream_t stream)
+{
+    const dim3 grid((unsigned)B, (unsigned)(a.Hkv * (D / 64)));
+    if (a.T_new == 1) append_token_kernel<ST, D><<<grid, 64, 0, stream>>>(a);
+    else if (a.T_new <= 32) append_run_kernel<ST, D, 1><<<grid, 64, 0, stream>>>(a);
+    else append_run_kernel<ST, D, 4><<<grid, 256, 0, stream>>>(a);
 }
 
 static PoolView view(const rs_pool *p, int32_t *table, int32_t *len, int32_t *refs)
@@ -656,13 +874,12 @@ int32_t rat_append_paged(const rs_shape *s, const rs_pool *p, const void *k, con
         if (!aligned16(x)) return RS_INVALID_ARG;
     const AppendParams a{k, v, g, state_k, state_v, k_pool, v_pool, meta, table, len, seq, n_new, s->Hkv, p->S, p->M, p->N,
                          __builtin_ctz((unsigned)p->P), T_new};
-    const dim3 grid((unsigned)s->B, (unsigned)((s->Hkv * s->D + 255) / 256));
     if (s->dtype == RS_BF16) {
-        if (s->D == 128) append_paged_kernel<bf16, 128><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-        else append_paged_kernel<bf16, 64><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+        if (s->D == 128) append_launch<bf16, 128>(a, s->B, (hipStream_t)stream);
+        else append_launch<bf16, 64>(a, s->B, (hipStream_t)stream);
     } else {
-        if (s->D == 128) append_paged_kernel<float, 128><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-        else append_paged_kernel<float, 64><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+        if (s->D == 128) append_launch<float, 128>(a, s->B, (hipStream_t)stream);
+        else append_launch<float, 64>(a, s->B, (hipStream_t)stream);
     }
     return launch_status();
 }

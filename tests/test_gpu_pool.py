@@ -210,10 +210,6 @@ def test_append(rs, case, dtype):
     sk, sv = rnd(S, Hkv, D), rnd(S, Hkv, D)
     kp, vp = rnd(Hkv, S * M * P, D).to(dt), rnd(Hkv, S * M * P, D).to(dt)
     meta = rnd(Hkv, S * M, 2, D).to(dt)
-    for i in range(B):  # bounds are current before
-        for j in range(d.m.held(seq[i])):
-            rows = kp[:, d.m.rows(seq[i])[j * P:(j + 1) * P]].float()
-            meta[:, d.m.table[seq[i]][j], 0], meta[:, d.m.table[seq[i]][j], 1] = rows.amin(1).to(dt), rows.amax(1).to(dt)
     olds = [x.clone() for x in (sk, sv, kp, vp, meta)]
     assert d.reserve(seq, cut)
     rs.rat_append_paged(s, d.p, k, v, g, sk, sv, kp, vp, meta, d.table, d.len, ints(seq), ints(counts) if counts else None, T)
