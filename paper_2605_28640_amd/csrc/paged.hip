@@ -138,23 +138,21 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
 {
     const int tid = threadIdx.x;
     for (int b = tid; b < a.B; b += kPagedThreads) {
-        const int s = a.seq[b];
-        int L = (s >= 0 && s < a.S) ? a.len[s] : 0, n = a.n_new ? a.n_new[b] : a.T;
+        // (two trips to memory: the list's entries, then length and the run's entry side by side)
+        const int s = a.seq[b], f = a.share ? a.share[3 * b] : -1;
+        int n = a.n_new ? a.n_new[b] : a.T;
+        const int *run = a.share + 3 * (f >= 0 && f <= b ? f : b);
+        const int begins = a.share ? run[0] : 0, cnt = a.share ? run[1] : 0, shared = a.share ? run[2] : 0;
+        int L = (s >= 0 && s < a.S) ? a.len[s] : 0;
         L = L < 0 ? 0 : min(L, a.M << a.shift);
         n = n < 0 ? 0 : min(n, a.T);
         int first = b, c = 0;
-        if (a.share) {
-            const int f = a.share[3 * b];
-            if (f >= 0 && f <= b) {
-                const int cnt = a.share[3 * f + 1];
-                if (a.share[3 * f] == f && cnt > b - f && cnt <= a.B - f && cnt > 1) {
-                    first = f;
-                    c = min(max(a.share[3 * f + 2], 0), max(L - n, 0) >> a.shift);
-                }
-            }
+        if (f >= 0 && f <= b && begins == f && cnt > b - f && cnt <= a.B - f && cnt > 1) {
+            first = f;
+            c = min(max(shared, 0), max(L - n, 0) >> a.shift);
         }
         pl.seq[b] = Seq{L, n, c, first};
-        pl.members[b] = (c > 0 && first == b) ? a.share[3 * b + 1] : 0;
+        pl.members[b] = (c > 0 && first == b) ? cnt : 0;
         pl.fewest[b] = 0x7fffffff;
         pl.row[b] = s;
     }

@@ -51,19 +51,18 @@ __device__ __forceinline__ int block_scan_i(int v, int *tot, int &total)
     return before + inc - v;
 }
 
-// The pages of [lo, hi) that are free (FREE) or held, ascending, to emit(rank, page) for ranks below `most`; returns how many
-// there are, but stops looking once there are `most`.  Called by the whole workgroup.
-template <bool FREE, typename Emit>
-__device__ __forceinline__ int collect_pages(const int32_t *refs, int lo, int hi, int most, int *tot, Emit emit)
+// The free pages, ascending, to list, `most` of them; returns how many were found (more perhaps, fewer if there are no more).  Called by
+// the whole workgroup.
+__device__ __forceinline__ int free_pages(const int32_t *refs, int N, int most, int *tot, int32_t *list)
 {
     constexpr int EACH = 16;
     int found = 0;
-    for (long base = lo & ~3; base < hi && found < most; base += kPoolThreads * EACH) {
+    for (long base = 0; base < N && found < most; base += kPoolThreads * EACH) {
         const long p0 = base + (long)threadIdx.x * EACH;
         uint32_t mask = 0u;
-        if (p0 < hi) {
+        if (p0 < N) {
             int r[EACH];
-            if (p0 + EACH <= hi) {
+            if (p0 + EACH <= N) {
 #pragma unroll
                 for (int u = 0; u < EACH / 4; ++u) {
                     const int4 x = *reinterpret_cast<const int4 *>(refs + p0 + 4 * u);
@@ -71,15 +70,15 @@ __device__ __forceinline__ int collect_pages(const int32_t *refs, int lo, int hi
                 }
             } else {
 #pragma unroll
-                for (int u = 0; u < EACH; ++u) r[u] = refs[p0 + u < hi ? p0 + u : hi - 1];
+                for (int u = 0; u < EACH; ++u) r[u] = refs[p0 + u < N ? p0 + u : N - 1];
             }
 #pragma unroll
             for (int u = 0; u < EACH; ++u)
-                if (p0 + u >= lo && p0 + u < hi && (r[u] <= 0) == FREE) mask |= 1u << u;
+                if (p0 + u < N && r[u] <= 0) mask |= 1u << u;
         }
         int total;
         int at = found + block_scan_i(__popc(mask), tot, total);
-        for (; mask && at < most; mask &= mask - 1, ++at) emit(at, (int)(p0 + __builtin_ctz(mask)));
+        for (; mask && at < most; mask &= mask - 1, ++at) list[at] = (int)(p0 + __builtin_ctz(mask));
         found += total;
     }
     return found;
@@ -138,7 +137,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_reserve_kernel(PoolView p, 
     bad = __syncthreads_or(bad);
     const int total = (int)needed;
     if (!bad && total > 0)
-        bad = collect_pages<true>(p.refs, 0, p.N, total, tot, [&](int r, int page) { list[r] = page; }) < total;
+        bad = free_pages(p.refs, p.N, total, tot, list) < total;
     __syncthreads();
     if (bad) {
         if (granted)
@@ -190,7 +189,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_fork_kernel(PoolView p, con
         needed += total;
     }
     if (!bad && needed > 0)
-        bad = collect_pages<true>(p.refs, 0, p.N, needed, tot, [&](int r, int page) { list[r] = page; }) < needed;
+        bad = free_pages(p.refs, p.N, needed, tot, list) < needed;
     __syncthreads();
     for (int i = tid; i < n; i += kPoolThreads) {
         int2 pr = make_int2(-1, -1), cr = make_int2(-1, -1);
@@ -261,28 +260,56 @@ __global__ __launch_bounds__(256) void pool_free_rows_kernel(PoolView p, const i
 }
 
 // L pages are held: those among them with numbers from L on go, in order, to the free ones below L.  to[page]: where page goes
-// (pages from L on that are held); holes: N words; count[0] = L.
-__global__ __launch_bounds__(kPoolThreads) void pool_compact_kernel(PoolView p, int32_t *to, int32_t *holes, int32_t *count, int2 *pairs,
-                                                                    int32_t *n_pairs)
+// (pages from L on that are held); holes, movers: N words; count[0] = L.  Two passes over the counts (how many are held; which are which), every
+// thread on 16 of them at a time, and one over the moves.
+__global__ __launch_bounds__(kPoolThreads) void pool_compact_kernel(PoolView p, int32_t *to, int32_t *holes, int32_t *movers, int32_t *count,
+                                                                    int2 *pairs, int32_t *n_pairs)
 {
+    constexpr int EACH = 16;
     __shared__ int tot[kPoolThreads / kWave];
-    const int L = collect_pages<false>(p.refs, 0, p.N, p.N, tot, [](int, int) {});
-    const int n = collect_pages<true>(p.refs, 0, L, L, tot, [&](int r, int page) { holes[r] = page; });
+    // which of the 16 counts from p0 on are held
+    auto held_mask = [&](long p0) __attribute__((always_inline)) -> uint32_t {
+        uint32_t mask = 0u;
+        if (p0 + EACH <= p.N) {
+#pragma unroll
+            for (int u = 0; u < EACH / 4; ++u) {
+                const int4 x = *reinterpret_cast<const int4 *>(p.refs + p0 + 4 * u);
+                mask |= (uint32_t)((x.x > 0) | (x.y > 0) << 1 | (x.z > 0) << 2 | (x.w > 0) << 3) << (4 * u);
+            }
+        } else {
+            for (int u = 0; p0 + u < p.N; ++u) mask |= (uint32_t)(p.refs[p0 + u] > 0) << u;
+        }
+        return mask;
+    };
+    int mine = 0, L;
+    for (long base = (long)threadIdx.x * EACH; base < p.N; base += kPoolThreads * EACH) mine += __popc(held_mask(base));
+    (void)block_scan_i(mine, tot, L);
+    int n_holes = 0, n_movers = 0;
+    for (long base = 0; base < p.N; base += kPoolThreads * EACH) {
+        const long p0 = base + (long)threadIdx.x * EACH;
+        const uint32_t held = p0 < p.N ? held_mask(p0) : 0u;
+        const long below = p0 >= L ? 0 : min((long)EACH, (long)L - p0), in = p0 >= p.N ? 0 : min((long)EACH, (long)p.N - p0);
+        const uint32_t low = (1u << below) - 1u, all = (1u << in) - 1u;
+        uint32_t hole = ~held & low & all, mover = held & ~low;
+        int total;  // (both numbers in one scan: at most 16384 of each a turn)
+        const int at = block_scan_i(__popc(hole) | __popc(mover) << 16, tot, total);
+        int h = n_holes + (at & 0xffff), m = n_movers + (at >> 16);
+        for (; hole; hole &= hole - 1) holes[h++] = (int)(p0 + __builtin_ctz(hole));
+        for (; mover; mover &= mover - 1) movers[m++] = (int)(p0 + __builtin_ctz(mover));
+        n_holes += total & 0xffff;
+        n_movers += total >> 16;
+    }
     __syncthreads();
-    collect_pages<false>(p.refs, L, p.N, n, tot, [&](int r, int page) {
-        const int hole = holes[r];
-        to[page] = hole;
-        pairs[r] = make_int2(page, hole);
-    });
-    __syncthreads();
-    for (int r = threadIdx.x; r < n; r += kPoolThreads) {
-        const int2 pr = pairs[r];
-        p.refs[pr.y] = p.refs[pr.x];
-        p.refs[pr.x] = 0;
+    for (int r = threadIdx.x; r < n_holes; r += kPoolThreads) {  // (as many movers as holes)
+        const int from = movers[r], hole = holes[r];
+        to[from] = hole;
+        pairs[r] = make_int2(from, hole);
+        p.refs[hole] = p.refs[from];
+        p.refs[from] = 0;
     }
     if (threadIdx.x == 0) {
         count[0] = L;
-        n_pairs[0] = n;
+        n_pairs[0] = n_holes;
     }
 }
 
@@ -713,15 +740,15 @@ int check_pool(const rs_pool *p)
     return RS_OK;
 }
 
-// scratch behind the control words: a word for every listed sequence, two for every page, one more
+// scratch behind the control words: a word for every listed sequence, three for every page, one more
 static size_t pool_ws_bytes(const rs_pool *p)
 {
-    return RS_WS_CTRL_BYTES + align256((size_t)p->S * 4) + 2 * align256((size_t)p->N * 4) + 256;
+    return RS_WS_CTRL_BYTES + align256((size_t)p->S * 4) + 3 * align256((size_t)p->N * 4) + 256;
 }
 
 struct PoolScratch {
     uint32_t *err;
-    int32_t *seqs, *pages, *pages2, *word;
+    int32_t *seqs, *pages, *pages2, *pages3, *word;
 };
 static PoolScratch scratch(const rs_pool *p, void *ws)
 {
@@ -731,7 +758,8 @@ static PoolScratch scratch(const rs_pool *p, void *ws)
     x.seqs = (int32_t *)w;
     x.pages = (int32_t *)(w + align256((size_t)p->S * 4));
     x.pages2 = (int32_t *)((char *)x.pages + align256((size_t)p->N * 4));
-    x.word = (int32_t *)((char *)x.pages2 + align256((size_t)p->N * 4));
+    x.pages3 = (int32_t *)((char *)x.pages2 + align256((size_t)p->N * 4));
+    x.word = (int32_t *)((char *)x.pages3 + align256((size_t)p->N * 4));
     return x;
 }
 
@@ -805,7 +833,7 @@ int32_t page_pool_compact(const rs_pool *p, int32_t *table, int32_t *len, int32_
     if (!pairs_out || !n_pairs_out || !aligned16(pairs_out) || !aligned16(n_pairs_out)) return RS_INVALID_ARG;
     const PoolScratch x = scratch(p, ws);
     const PoolView v = view(p, table, len, refs);
-    pool_compact_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, x.pages, x.pages2, x.word, (int2 *)pairs_out, n_pairs_out);
+    pool_compact_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, x.pages, x.pages2, x.pages3, x.word, (int2 *)pairs_out, n_pairs_out);
     const long cells = (long)p->S * p->M;
     const unsigned groups = (unsigned)(cells >= 2048l * 256 ? 2048 : (cells + 255) / 256);
     pool_renumber_kernel<<<groups, 256, 0, (hipStream_t)stream>>>(v, x.pages, x.word, (int2 *)pairs_out, n_pairs_out, p->N / 2);
