@@ -158,10 +158,32 @@ __global__ __launch_bounds__(kPoolThreads) void pool_reserve_kernel(PoolView p, 
     }
 }
 
+// a fork's row: the source's first `n` pages, one more reference each; a release's: the same taken back.  By `step` threads from `at` on.
+__device__ __forceinline__ void fork_row(const PoolView &p, int src, int dst, int n, int at, int step)
+{
+    const long s = (long)src * p.M, d = (long)dst * p.M;
+    for (int j = at; j < n; j += step) {
+        const int page = p.table[s + j];
+        p.table[d + j] = page;
+        if (page >= 0 && page < p.N) atomicAdd(&p.refs[page], 1);
+    }
+}
+__device__ __forceinline__ void free_row(const PoolView &p, int seq, int n, int at, int step)
+{
+    const long row = (long)seq * p.M;
+    for (int j = at; j < n; j += step) {
+        const int page = p.table[row + j];
+        p.table[row + j] = -1;
+        if (page >= 0 && page < p.N) atomicSub(&p.refs[page], 1);
+    }
+}
+// Rows of so few entries in all are done by the workgroup that decides (a wave a row), others by a launch of their own.
+constexpr long kRowsHere = 8192;
+
 // full: n words, the pages that entry i takes over from its source (none where the call is refused)
 __global__ __launch_bounds__(kPoolThreads) void pool_fork_kernel(PoolView p, const int32_t *__restrict__ src,
                                                                  const int32_t *__restrict__ dst, int n, int2 *pairs, int2 *carry,
-                                                                 int32_t *full, int32_t *list, uint32_t *err)
+                                                                 int32_t *full, int32_t *list, uint32_t *err, bool rows_here)
 {
     __shared__ uint32_t seen[kMaxSeqs / 32];
     __shared__ int tot[kPoolThreads / kWave];
@@ -210,25 +232,21 @@ __global__ __launch_bounds__(kPoolThreads) void pool_fork_kernel(PoolView p, con
         if (carry) carry[i] = cr;
     }
     if (bad && tid == 0) *err = kErrPages;
+    if (!rows_here || bad) return;
+    __syncthreads();
+    for (int i = tid >> 6; i < n; i += kPoolThreads / kWave) fork_row(p, src[i], dst[i], full[i], lane_id(), kWave);
 }
 
-// the rows of a fork: the source's full pages, one more reference each
 __global__ __launch_bounds__(256) void pool_fork_rows_kernel(PoolView p, const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
                                                              const int32_t *__restrict__ full)
 {
     const int i = blockIdx.x, n = full[i];
-    if (n == 0) return;
-    const long s = (long)src[i] * p.M, d = (long)dst[i] * p.M;
-    for (int j = blockIdx.y * 256 + threadIdx.x; j < n; j += gridDim.y * 256) {
-        const int page = p.table[s + j];
-        p.table[d + j] = page;
-        if (page >= 0 && page < p.N) atomicAdd(&p.refs[page], 1);
-    }
+    if (n > 0) fork_row(p, src[i], dst[i], n, blockIdx.y * 256 + threadIdx.x, gridDim.y * 256);
 }
 
 // held: n words, the pages that entry i gives up (none where the call is refused)
 __global__ __launch_bounds__(kPoolThreads) void pool_free_kernel(PoolView p, const int32_t *__restrict__ seq, int n, int32_t *held,
-                                                                 uint32_t *err)
+                                                                 uint32_t *err, bool rows_here)
 {
     __shared__ uint32_t seen[kMaxSeqs / 32];
     const int tid = threadIdx.x;
@@ -245,18 +263,15 @@ __global__ __launch_bounds__(kPoolThreads) void pool_free_kernel(PoolView p, con
         if (!bad) p.len[seq[i]] = 0;
     }
     if (bad && tid == 0) *err = kErrPages;
+    if (!rows_here || bad) return;
+    __syncthreads();
+    for (int i = tid >> 6; i < n; i += kPoolThreads / kWave) free_row(p, seq[i], held[i], lane_id(), kWave);
 }
 
 __global__ __launch_bounds__(256) void pool_free_rows_kernel(PoolView p, const int32_t *__restrict__ seq, const int32_t *__restrict__ held)
 {
     const int i = blockIdx.x, n = held[i];
-    if (n == 0) return;
-    const long row = (long)seq[i] * p.M;
-    for (int j = blockIdx.y * 256 + threadIdx.x; j < n; j += gridDim.y * 256) {
-        const int page = p.table[row + j];
-        p.table[row + j] = -1;
-        if (page >= 0 && page < p.N) atomicSub(&p.refs[page], 1);
-    }
+    if (n > 0) free_row(p, seq[i], n, blockIdx.y * 256 + threadIdx.x, gridDim.y * 256);
 }
 
 // L pages are held: those among them with numbers from L on go, in order, to the free ones below L.  to[page]: where page goes
@@ -300,12 +315,25 @@ __global__ __launch_bounds__(kPoolThreads) void pool_compact_kernel(PoolView p, 
         n_movers += total >> 16;
     }
     __syncthreads();
-    for (int r = threadIdx.x; r < n_holes; r += kPoolThreads) {  // (as many movers as holes)
-        const int from = movers[r], hole = holes[r];
-        to[from] = hole;
-        pairs[r] = make_int2(from, hole);
-        p.refs[hole] = p.refs[from];
-        p.refs[from] = 0;
+    constexpr int AHEAD = 4;  // moves on their way together
+    for (int r0 = threadIdx.x; r0 < n_holes; r0 += AHEAD * kPoolThreads) {  // (as many movers as holes)
+        int from[AHEAD], hole[AHEAD], held[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int r = min(r0 + i * kPoolThreads, n_holes - 1);
+            from[i] = movers[r], hole[i] = holes[r];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) held[i] = p.refs[from[i]];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int r = r0 + i * kPoolThreads;
+            if (r >= n_holes) break;
+            to[from[i]] = hole[i];
+            pairs[r] = make_int2(from[i], hole[i]);
+            p.refs[hole[i]] = held[i];
+            p.refs[from[i]] = 0;
+        }
     }
     if (threadIdx.x == 0) {
         count[0] = L;
@@ -365,18 +393,18 @@ __global__ __launch_bounds__(256) void pool_common_kernel(PoolView p, const int3
     if (tid == 0) share[3 * i + 1] = n;
 }
 
-// runs of neighbours with at least `least` pages in common; a run's pages are the fewest that two neighbours in it share
-__global__ __launch_bounds__(kMaxShared) void pool_runs_kernel(int32_t *share, int n, int least)
+// Runs of neighbours with at least `least` pages in common; a run's pages are the fewest that two neighbours in it share.  common: of this
+// thread's place of the list with the one before it.
+__device__ __forceinline__ void put_runs(int32_t *share, int n, int least, int common)
 {
     __shared__ int first[kMaxShared], size[kMaxShared], pages[kMaxShared];
     const int i = threadIdx.x;
-    const int common = i < n ? share[3 * i + 1] : 0;
     const bool begins = i == 0 || common < least;
     size[i] = 0;
     pages[i] = 0x7fffffff;
     first[i] = begins ? i : 0;
     __syncthreads();
-    for (int d = 1; d < kMaxShared; d <<= 1) {  // running maximum
+    for (int d = 1; d < n; d <<= 1) {  // running maximum
         const int o = i >= d ? first[i - d] : 0;
         __syncthreads();
         if (o > first[i]) first[i] = o;
@@ -393,6 +421,47 @@ __global__ __launch_bounds__(kMaxShared) void pool_runs_kernel(int32_t *share, i
         share[3 * i + 1] = size[f];
         share[3 * i + 2] = size[f] > 1 ? pages[f] : 0;
     }
+}
+__global__ __launch_bounds__(kMaxShared) void pool_runs_kernel(int32_t *share, int n, int least)
+{
+    put_runs(share, n, least, (int)threadIdx.x < n ? share[3 * threadIdx.x + 1] : 0);
+}
+// both at once, for lists of few entries: a wave a pair of neighbours
+__global__ __launch_bounds__(kMaxShared) void pool_share_kernel(PoolView p, const int32_t *__restrict__ seq, int32_t *share, int n, int least)
+{
+    __shared__ int common[kMaxShared];
+    if (threadIdx.x == 0) common[0] = 0;
+    for (int i = 1 + (threadIdx.x >> 6); i < n; i += kMaxShared / kWave) {
+        const int a = seq[i - 1], b = seq[i];
+        int same = 0;
+        if (a >= 0 && a < p.S && b >= 0 && b < p.S) {
+            const int most = min(min(p.len[a] >> p.shift, p.len[b] >> p.shift), p.M);
+            const int32_t *ra = p.table + (long)a * p.M, *rb = p.table + (long)b * p.M;
+            while (same < most) {
+                constexpr int AHEAD = 4;
+                int x[AHEAD], y[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int j = min(same + u * kWave + lane_id(), most - 1);
+                    x[u] = ra[j], y[u] = rb[j];
+                }
+                int step = AHEAD * kWave;
+#pragma unroll
+                for (int u = AHEAD - 1; u >= 0; --u) {
+                    const uint64_t differ = __ballot(x[u] != y[u] || x[u] < 0);
+                    if (differ) step = u * kWave + __builtin_ctzll(differ);
+                }
+                if (step < AHEAD * kWave) {
+                    same = min(same + step, most);
+                    break;
+                }
+                same = min(same + step, most);
+            }
+        }
+        if (lane_id() == 0) common[i] = max(same, 0);
+    }
+    __syncthreads();
+    put_runs(share, n, least, (int)threadIdx.x < n ? common[threadIdx.x] : 0);
 }
 
 struct CopyView {
@@ -806,9 +875,10 @@ int32_t page_pool_fork(const rs_pool *p, int32_t *table, int32_t *len, int32_t *
         return RS_INVALID_ARG;
     const PoolScratch x = scratch(p, ws);
     const PoolView v = view(p, table, len, refs);
+    const bool rows_here = (long)n * p->M <= kRowsHere;
     pool_fork_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, src, dst, n, (int2 *)pairs_out, (int2 *)carry_out, x.seqs, x.pages,
-                                                                  x.err);
-    pool_fork_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, src, dst, x.seqs);
+                                                                  x.err, rows_here);
+    if (!rows_here) pool_fork_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, src, dst, x.seqs);
     return launch_status();
 }
 
@@ -820,8 +890,9 @@ int32_t page_pool_free(const rs_pool *p, int32_t *table, int32_t *len, int32_t *
     if (!seq || !aligned16(seq)) return RS_INVALID_ARG;
     const PoolScratch x = scratch(p, ws);
     const PoolView v = view(p, table, len, refs);
-    pool_free_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, seq, n, x.seqs, x.err);
-    pool_free_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, seq, x.seqs);
+    const bool rows_here = (long)n * p->M <= kRowsHere;
+    pool_free_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, seq, n, x.seqs, x.err, rows_here);
+    if (!rows_here) pool_free_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, seq, x.seqs);
     return launch_status();
 }
 
@@ -850,6 +921,10 @@ int32_t page_pool_share(const rs_pool *p, const int32_t *table, const int32_t *l
     if (n < 1 || min_pages < 1) return RS_INVALID_ARG;
     if (n > kMaxShared) return RS_UNSUPPORTED;
     const PoolView v = view(p, const_cast<int32_t *>(table), const_cast<int32_t *>(len), nullptr);
+    if ((long)n * p->M <= 4 * kRowsHere) {
+        pool_share_kernel<<<1, kMaxShared, 0, (hipStream_t)stream>>>(v, seq, share_out, n, min_pages);
+        return launch_status();
+    }
     pool_common_kernel<<<(unsigned)n, 256, 0, (hipStream_t)stream>>>(v, seq, share_out);
     pool_runs_kernel<<<1, kMaxShared, 0, (hipStream_t)stream>>>(share_out, n, min_pages);
     return launch_status();

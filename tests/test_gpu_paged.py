@@ -375,3 +375,63 @@ def test_serving_eagerly_and_from_a_graph(rs, dtype):
     assert len(eager) == len(replayed) == 39
     for (o, l), (o2, l2) in zip(eager, replayed):
         assert torch.equal(o, o2) and torch.equal(l, l2)
+
+
+def test_the_longest_list(rs):
+    r = np.random.default_rng(8)
+    lens = [int(x) for x in r.integers(0, 40, 1024)]
+    for i in range(500, 700):
+        lens[i] = 16 + int(r.integers(1, 20))
+    b = Batch(rs, 2, 1, 128, 16, lens, [1] * 500 + [200], 16, 1, None, "bf16", seed=9)
+    b.check(*b.run())
+
+
+def test_nothing_new(rs):
+    b = Batch(rs, 2, 2, 64, 16, [40, 35], (2,), 32, 3, [0, -5])
+    out, lse = b.run()
+    assert out.eq(7.0).all() and lse.eq(7.0).all()
+
+
+def test_two_calls_at_once(rs):
+    """On two streams, each with a workspace of its own."""
+    one, two = Batch(rs, 8, 2, 128, 16, [3000, 3010, 5000], (2,), 2992, 1, seed=1), Batch(rs, 4, 4, 64, 32, [900, 700], (), 0, 9, seed=2)
+    want = one.run(), two.run()
+    side = [torch.cuda.Stream() for _ in range(2)]
+    got = [(torch.full_like(o, 7.0), torch.full_like(l, 7.0)) for o, l in want]
+    shares = [ints(b.share) for b in (one, two)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, st, (o, l), sh in zip((one, two), side, got, shares):
+            with torch.cuda.stream(st):
+                rs.attn_paged(b.s, b.p, b.q, b.k, b.v, b.table, b.len, b.seq, None, b.T, sh, b.scale, o, l, b.ws)
+    torch.cuda.synchronize()
+    for (o, l), (wo, wl) in zip(got, want):
+        assert torch.equal(o, wo) and torch.equal(l, wl)
+
+
+@pytest.mark.parametrize("case", [3, 4, 9, 10])
+def test_a_workspace_used_for_other_calls_in_between(rs, case):
+    """Two captured graphs and eager calls of another shape share one workspace."""
+    Hq, Hkv, D, P, lens, runs, shared, T, counts = CASES[case]
+    one, two = Batch(rs, Hq, Hkv, D, P, lens, runs, shared, T, counts, seed=case), Batch(rs, 4, 2, 64, 16, [130, 140, 129], (3,), 128, 1, seed=2)
+    ws = rs.Workspace(max(one.ws.nbytes, two.ws.nbytes))
+    one.ws = two.ws = ws
+    want = one.run(), two.run()
+    outs = [(torch.full_like(o, 7.0), torch.full_like(l, 7.0)) for o, l in want]
+    graphs, extra = [], [(ints(b.counts) if b.counts else None, ints(b.share)) for b in (one, two)]
+    for b, (o, l), (n_new, share) in zip((one, two), outs, extra):
+        g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+            rs.attn_paged(b.s, b.p, b.q, b.k, b.v, b.table, b.len, b.seq, n_new, b.T, share, b.scale, o, l, ws)
+        graphs.append(g)
+    for rep in range(3):
+        for o, l in outs:
+            o.fill_(7.0), l.fill_(7.0)
+        graphs[0].replay()
+        two.run()
+        graphs[1].replay()
+        one.run(share=False)
+        torch.cuda.synchronize()
+        for (o, l), (wo, wl) in zip(outs, want):
+            assert torch.equal(o, wo) and torch.equal(l, wl), rep

@@ -299,3 +299,46 @@ def test_as_the_contiguous_append_does_it(rs):
         rows = torch.from_numpy(d.m.rows(b)).cuda()
         assert torch.equal(kp[:, rows], kc[b, :, :T0 + steps]) and torch.equal(vp[:, rows], vc[b, :, :T0 + steps])
         assert torch.equal(pm[:, d.m.table[b][:3]], meta[b, :, :3])
+
+
+def test_plain_and_other_arguments_make_the_same_call(rs):
+    """Through native.cpp, and (a subclass of torch.Tensor is not of the plain type) through ctypes."""
+    class Other(torch.Tensor):
+        pass
+    for kind in (lambda x: x, lambda x: x.as_subclass(Other)):
+        d = Device(rs, 20, 4, 5, 16)
+        granted = ints([9, 9])
+        rs.page_pool_reserve(d.p, kind(d.table), d.len, d.refs, ints([3, 1]), None, 20, granted, d.ws)
+        assert d.m.reserve([3, 1], [20, 20]) and granted.tolist() == [20, 20]
+        d.check("reserve")
+        pairs, carry, share = ints([[0, 0]]), ints([[0, 0]]), ints([[9] * 3] * 2)
+        rs.page_pool_fork(d.p, d.table, kind(d.len), d.refs, ints([3]), ints([0]), pairs, carry, d.ws)
+        d.m.fork([3], [0])
+        d.check("fork")
+        rs.page_pool_share(d.p, d.table, d.len, kind(ints([3, 0])), 1, share)
+        assert share.tolist() == d.m.share([3, 0], 1) == [[0, 2, 1]] * 2
+        rs.page_pool_free(d.p, d.table, d.len, d.refs, kind(ints([3])), d.ws)
+        d.m.free([3])
+        d.check("free")
+        moves, n = ints([[0, 0]] * 10), ints([0])
+        rs.page_pool_compact(d.p, d.table, d.len, kind(d.refs), moves, n, d.ws)
+        assert moves[:n.item()].tolist() == d.m.compact()
+        d.check("compact")
+        s = rs.make_shape(1, 1, 1, 64, 320, 16, torch.float32)
+        k, v, sk = torch.randn(1, 320, 64, device="cuda"), torch.randn(1, 320, 64, device="cuda"), torch.randn(4, 1, 64, device="cuda")
+        want, ws = k.clone(), sk.clone()
+        want[:, 32:48], ws[2] = k[:, 16:32], sk[1]
+        rs.page_copy(s, k, kind(v), None, s, k, v, None, ints([[1, 2]]), None)
+        rs.rat_state_copy(s, kind(sk), sk.clone(), ints([[1, 2]]))
+        assert torch.equal(k, want) and torch.equal(sk, ws)
+        x = torch.ones(1, 1, 1, 64, device="cuda")
+        rs.rat_append_paged(s, d.p, kind(x), x, torch.zeros_like(x), sk, sk.clone(), k, v, None, d.table, d.len, ints([1]), None, 1)
+        assert k[0, d.m.rows(1)[-1]].eq(1).all() and sk[1].eq(1).all()
+        out, lse = torch.zeros(1, 1, 1, 64, device="cuda"), torch.zeros(1, 1, 1, device="cuda")
+        rs.attn_paged(s, d.p, kind(x), k, v, d.table, d.len, ints([1]), None, 1, None, 0.0, out, lse, rs.Workspace(rs.attn_paged_workspace_bytes(s, d.p, 1)))
+        assert (out[0, 0, 0] - v[0, d.m.rows(1)].mean(0)).abs().max() < 1e-5
+        for bad in (lambda: rs.page_pool_free(d.p, d.table[:2], d.len, d.refs, ints([1]), d.ws),
+                    lambda: rs.page_pool_free(d.p, d.table.long(), d.len, d.refs, ints([1]), d.ws),
+                    lambda: rs.attn_paged(s, d.p, x.to(torch.bfloat16), k, v, d.table, d.len, ints([1]), None, 1, None, 0.0, out, lse, d.ws)):
+            with pytest.raises(rs.RatsparseError):
+                bad()

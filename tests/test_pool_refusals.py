@@ -136,3 +136,25 @@ def test_the_model():
     assert p.free([0]) and p.refs == [2, 2, 0, 1, 1, 0, 0, 0]
     assert p.compact() == [[4, 2]] and p.table[1] == [0, 1, 2, -1] and p.refs == [2, 2, 1, 1, 0, 0, 0, 0]
     assert p.reserve([1], [15]) and p.len[1] == 48 and p.table[1] == [0, 1, 2, -1]
+
+
+@pytest.mark.parametrize("name,names", [
+    ("page_pool_reserve", "p table len refs seq want T_new granted ws"),
+    ("page_pool_fork", "p table len refs src dst pairs_out carry_out ws"),
+    ("page_pool_free", "p table len refs seq ws"),
+    ("page_pool_compact", "p table len refs pairs_out n_pairs_out ws"),
+    ("page_pool_share", "p table len seq min_pages share_out"),
+    ("page_copy", "s_src k_src v_src meta_src s_dst k_dst v_dst meta_dst pairs n_pairs"),
+    ("rat_state_copy", "s state_k state_v pairs"),
+    ("rat_append_paged", "s p k v g state_k state_v k_pool v_pool meta table len seq n_new T_new"),
+    ("attn_paged", "s p q k_pool v_pool table len seq n_new T_new share scale out lse_out ws"),
+])
+def test_signatures(name, names):
+    """And the calls as native.cpp takes them: the same number of arguments; what is not of its plain type is left unmade."""
+    import inspect
+    assert list(inspect.signature(getattr(rs, name)).parameters) == names.split()
+    fast, n = getattr(rs._calls(), name), len(names.split())
+    assert fast(*[0.5] * n) is False
+    for wrong in (n - 1, n + 1):
+        with pytest.raises(TypeError):
+            fast(*[None] * wrong)
