@@ -416,4 +416,17 @@ __device__ __forceinline__ uint32_t float_to_key(float f)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// inclusive prefix sum over the wave: within rows of 16 lanes, then their ends to the rows after them; shifts inside the adds, where shuffles
+// would be six trips to LDS and six lane masks held in registers
+__device__ __forceinline__ int wave_scan_i(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // from 1, 2, 4, 8 lanes before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 to the second row, lane 47 to the fourth
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the third and fourth
+    return x;
+}
+
 }  // namespace rs

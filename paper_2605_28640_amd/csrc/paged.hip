@@ -44,9 +44,6 @@ constexpr int kFew = 32, kMany = 128;  // rows of a tile
 // keys a wave of a few-row tile takes at a time
 template <typename ST>
 constexpr int kKeys = sizeof(ST) == 2 ? 32 : 16;
-// keys of a unit
-template <typename ST, bool MANY>
-constexpr int kUnit = MANY ? 128 : kKeys<ST>;
 
 struct PagedParams {
     const void *q, *k, *v;
@@ -93,14 +90,22 @@ __device__ __forceinline__ long scalar(long x)
 }
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 
-// A tile of n units takes n places of its line and, before them, what beginning and ending a tile costs in units; a tile
-// without units none.
-template <bool MANY>
-constexpr int kBefore = MANY ? 2 : 3;
-template <bool MANY>
-__device__ __forceinline__ int places(int n)
+// What the two kinds of tile differ in; a value, and not a template's argument, so that there is one way through the code for both (more code
+// than the 64 KB of the CUs' instruction caches costs every launch the fetching of it).
+struct Kind {
+    bool many;
+    int rows, unit;  // log2 of a tile's rows, of a unit's keys
+    int before;      // what beginning and ending a tile costs, in units
+    // a tile of n units takes n places of its line and those before them; a tile without units none
+    __device__ __forceinline__ int places(int n) const { return n > 0 ? n + before : 0; }
+    __device__ __forceinline__ int tiles(int r) const { return (int)(((unsigned)r + (1u << rows) - 1) >> rows); }
+    __device__ __forceinline__ int units(int keys) const { return (int)(((unsigned)keys + (1u << unit) - 1) >> unit); }
+};
+template <typename ST>
+__device__ __forceinline__ Kind kind_of(bool many)
 {
-    return n > 0 ? n + kBefore<MANY> : 0;
+    if (sizeof(ST) == 2 && many) return Kind{true, __builtin_ctz(kMany), 7, 2};
+    return Kind{false, __builtin_ctz(kFew), __builtin_ctz(kKeys<ST>), 3};
 }
 
 template <typename ST>
@@ -110,25 +115,18 @@ __device__ __forceinline__ bool shared_is_many(int rows)
 }
 
 // units of row tile rt of sequence x over its own pages: the keys from the shared ones to the tile's last row
-template <typename ST, bool MANY>
-__device__ __forceinline__ int own_units(const Seq &x, int rt, int G, int shift, int &k0, int &k1)
+__device__ __forceinline__ int own_units(const Kind &kind, const Seq &x, int rt, int G, int shift, int &k0, int &k1)
 {
-    constexpr int ROWS = MANY ? kMany : kFew, UNIT = kUnit<ST, MANY>;
-    const int t0 = rt * ROWS / G, t1 = min(x.n - 1, (rt * ROWS + ROWS - 1) / G);
+    const int t0 = (rt << kind.rows) / G, t1 = min(x.n - 1, ((rt << kind.rows) + (1 << kind.rows) - 1) / G);
     k0 = x.c << shift;
     k1 = x.L - x.n + t1 + 1;
-    return (t0 >= x.n || k1 <= k0) ? 0 : (k1 - k0 + UNIT - 1) / UNIT;
+    return (t0 >= x.n || k1 <= k0) ? 0 : kind.units(k1 - k0);
 }
-// an entry's places in a line: those of the run that begins there, if its tiles are of that kind, and its own
-template <typename ST, bool MANY>
-__device__ __forceinline__ int entry_places(const PagedParams &a, const Seq &x, int members)
+// places of a sequence's own row tiles rt, rt + step, ...
+__device__ __forceinline__ int own_places(const PagedParams &a, const Kind &kind, const Seq &x, int rt, int step)
 {
-    constexpr int ROWS = MANY ? kMany : kFew;
     int sum = 0, k0, k1;
-    if (members > 0 && x.c > 0 && shared_is_many<ST>(members * a.T * a.G) == MANY)
-        sum = div_up(members * a.T * a.G, ROWS) * places<MANY>(div_up(x.c << a.shift, kUnit<ST, MANY>));
-    if ((a.own_many != 0) == MANY)
-        for (int rt = 0; rt * ROWS < x.n * a.G; ++rt) sum += places<MANY>(own_units<ST, MANY>(x, rt, a.G, a.shift, k0, k1));
+    for (; rt < kind.tiles(x.n * a.G); rt += step) sum += kind.places(own_units(kind, x, rt, a.G, a.shift, k0, k1));
     return sum;
 }
 
@@ -165,10 +163,35 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
     __shared__ int tot[2][kPagedWaves];
     const int each = div_up(a.B, kPagedThreads), lo = min(tid * each, a.B), hi = min(lo + each, a.B);
     int sum[2] = {0, 0}, inc[2];
-    for (int b = lo; b < hi; ++b) {
+    auto settled = [&](int b) __attribute__((always_inline)) -> Seq {  // with the pages its run shares
         Seq x = pl.seq[b];
         x.c = pl.members[x.first] ? pl.fewest[x.first] : 0;  // (nobody writes members, fewest or first here)
-        const int few = entry_places<ST, false>(a, x, pl.members[b]), many = entry_places<ST, true>(a, x, pl.members[b]);
+        return x;
+    };
+    // entries of many tiles: a wave each (a prompt of 32768 tokens has 1024 and more)
+    const Kind own_kind = kind_of<ST>(a.own_many);
+    const bool by_wave = a.T * a.G > 8 * kFew;
+    if (by_wave) {
+        for (int b = tid >> 6; b < a.B; b += kPagedWaves) {
+            const Seq x = settled(b);
+            int own = own_places(a, own_kind, x, lane_id(), kWave);
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) own += __shfl_xor(own, d, kWave);
+            if (lane_id() == 0) pl.start[0][b] = own;
+        }
+        __syncthreads();
+    }
+    for (int b = lo; b < hi; ++b) {
+        const Seq x = settled(b);
+        const int own = by_wave ? pl.start[0][b] : own_places(a, own_kind, x, 0, 1);
+        int few = a.own_many ? 0 : own, many = a.own_many ? own : 0;
+        const int rows = x.c > 0 ? pl.members[b] * a.T * a.G : 0;  // of the run that begins here
+        if (rows > 0) {
+            const Kind run = kind_of<ST>(shared_is_many<ST>(rows));
+            const int more = run.tiles(rows) * run.places(run.units(x.c << a.shift));
+            if (run.many) many += more;
+            else few += more;
+        }
         pl.seq[b].c = x.c;
         pl.start[0][b] = few;
         pl.start[1][b] = many;
@@ -177,12 +200,7 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        inc[k] = sum[k];
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int o = __shfl_up(inc[k], d, kWave);
-            if (lane_id() >= d) inc[k] += o;
-        }
+        inc[k] = wave_scan_i(sum[k]);
         if (lane_id() == kWave - 1) tot[k][tid >> 6] = inc[k];
     }
     __syncthreads();
@@ -212,16 +230,18 @@ __device__ __forceinline__ int many_groups(int few_line, int many_line)
 // its first 32 workgroups 11 places for every 9 of the others': two workgroups are on a CU, and the one that came first is served
 // first by its memory path (four sequences of 65536 tokens, 8 heads, with equal shares: every one of the first 256 workgroups done after
 // 131-145 us, every other after 157-171).
-template <bool MANY>
 struct Shares {
     static constexpr int kOlder = 11, kNewer = 9;
     int line, n;             // places of a KV head, shares
     int of_xcd, older, sum;  // shares of an XCD, those of its first workgroups, their places' weights together (0: equal shares)
     int each, more;          // equal shares: the first `more` have each + 1
     long all;
-    double unit, per_unit;   // places for each unit of weight (equal shares: of a share), and 1 / unit
+    double unit;             // places for each unit of weight
+    // reciprocals: a division of integers, or one in 64 bits, costs the beginning of every launch as much as 30 other instructions
+    float per_unit;          // of unit; equal shares: of a share's places
+    float per_xcd, per_sum;  // of of_xcd, of sum
     Shares() = default;
-    __device__ __forceinline__ Shares(const Plan &pl, int B, int Hkv)
+    __device__ __forceinline__ Shares(const Plan &pl, int B, int Hkv, bool MANY)
     {
         static_assert(sizeof(Shares) <= kPlanShares / 2, "room in the workspace");
         const int f = scalar(pl.start[0][B]), m = scalar(pl.start[1][B]), groups = many_groups(f, m);
@@ -232,34 +252,38 @@ struct Shares {
         older = MANY ? half : (kPagedGroups / 16 - half) * kPagedWaves;
         n = 8 * of_xcd;
         sum = 0;
-        each = 1, more = 0, unit = 1.;
-        if (all >= 4l * n) {
+        each = 1, more = 0, unit = 0., per_unit = per_xcd = per_sum = 0.f;
+        if (n > 0 && all >= 4l * n) {
             sum = older * kOlder + (of_xcd - older) * kNewer;
-            unit = n > 0 ? (double)all / (8. * sum) : 1.;
+            per_sum = __builtin_amdgcn_rcpf((float)sum);
+            per_xcd = __builtin_amdgcn_rcpf((float)of_xcd);
+            unit = (double)all * (double)(0.125f * per_sum);  // (off by 2^-22 of it: begin() rounds a whole number back up)
+            per_unit = (float)(8 * sum) * __builtin_amdgcn_rcpf((float)all);
         } else {
             n = (int)min((long)n, all);
             if (n > 0) {
                 each = (int)all / n;
                 more = (int)all - each * n;
-                unit = (double)all / n;
+                per_unit = (float)n * __builtin_amdgcn_rcpf((float)all);
             }
         }
-        per_unit = 1. / unit;
     }
+    // w / d for small whole numbers, from 1 / d: half a unit away from the next one, which is more than the rounding
+    __device__ __forceinline__ static int quotient(int w, float per_d) { return (int)(((float)w + 0.5f) * per_d); }
     __device__ __forceinline__ long begin(int w) const
     {
         if (sum == 0) return w * each + min(w, more);
         if (w >= n) return all;
-        const int x = w / of_xcd, i = w - x * of_xcd;
-        return (long)((double)(x * sum + min(i, older) * kOlder + max(i - older, 0) * kNewer) * unit);
+        const int x = quotient(w, per_xcd), i = w - x * of_xcd;
+        return (long)((double)(x * sum + min(i, older) * kOlder + max(i - older, 0) * kNewer) * unit + 0.0625);
     }
     __device__ __forceinline__ int owner(long place) const
     {
         int w;
         if (sum == 0) {
-            w = (int)((double)place * per_unit);
+            w = (int)((float)place * per_unit);
         } else {
-            const int at = (int)((double)place * per_unit), x = at / sum, r = at - x * sum;
+            const int at = (int)((float)place * per_unit), x = quotient(at, per_sum), r = at - x * sum;
             w = x * of_xcd + (r < older * kOlder ? r / kOlder : older + (r - older * kOlder) / kNewer);
         }
         w = max(0, min(w, n - 1));
@@ -271,10 +295,9 @@ struct Shares {
 // where the part of a tile (its units at s0 .. s1 - 1) that lies in [wb, we) goes: 2: all of it is there; 0, 1: a boundary record
 __device__ __forceinline__ int record_of(long s0, long s1, long wb, long we) { return (s0 >= wb && s1 <= we) ? 2 : s0 <= wb ? 0 : 1; }
 // the first row of a boundary record
-template <bool MANY>
-__device__ __forceinline__ long cut_row(const PagedParams &a, long share, int record)
+__device__ __forceinline__ long cut_row(const PagedParams &a, bool many, long share, int record)
 {
-    return MANY ? (2 * share + record) * kMany : a.few_base + (2 * share + record) * a.few_rows;
+    return many ? (2 * share + record) * kMany : a.few_base + (2 * share + record) * a.few_rows;
 }
 
 // one tile of rows over a run of keys
@@ -290,10 +313,10 @@ struct TileWork {
 };
 
 // the tile that place `at` of the whole line belongs to; its units are those at s0 .. s1 - 1
-template <typename ST, bool MANY>
-__device__ __forceinline__ void find_tile(const PagedParams &a, const Plan &pl, long at, int line, TileWork &w, long &s0, long &s1)
+template <typename ST>
+__device__ __forceinline__ void find_tile(const PagedParams &a, const Plan &pl, const Kind &kind, long at, int line, TileWork &w, long &s0, long &s1)
 {
-    const int *start = pl.start[MANY];
+    const int *start = pl.start[kind.many];
     w.kvh = (int)(at / line);
     int off = (int)(at % line), n = 0, lo = 0;
     for (int hi = a.B; hi - lo > 1;) {  // the last entry that begins at or before off (entries without places are passed over)
@@ -307,12 +330,12 @@ __device__ __forceinline__ void find_tile(const PagedParams &a, const Plan &pl, 
     w.row_seq = pl.row[lo];
     w.key0 = 0;
     w.shared = false;
-    const int members = pl.members[lo];
-    if (members > 0 && x.c > 0 && shared_is_many<ST>(members * a.T * a.G) == MANY) {
-        w.rows = members * a.T * a.G;
+    const int run_rows = x.c > 0 ? pl.members[lo] * a.T * a.G : 0;
+    if (run_rows > 0 && shared_is_many<ST>(run_rows) == kind.many) {
+        w.rows = run_rows;
         w.limit = x.c << a.shift;
-        n = div_up(w.limit, kUnit<ST, MANY>);
-        const int su = places<MANY>(n), st = div_up(w.rows, MANY ? kMany : kFew);
+        n = kind.units(w.limit);
+        const int su = kind.places(n), st = kind.tiles(w.rows);
         w.shared = off < su * st;
         if (w.shared) {
             w.rt = off / su;
@@ -323,13 +346,23 @@ __device__ __forceinline__ void find_tile(const PagedParams &a, const Plan &pl, 
     }
     if (!w.shared) {
         w.rows = x.n * a.G;
-        for (w.rt = 0;; ++w.rt) {
-            n = own_units<ST, MANY>(x, w.rt, a.G, a.shift, w.key0, w.limit);
-            if (off < places<MANY>(n)) break;
-            off -= places<MANY>(n);
+        for (w.rt = 0;; w.rt += kWave) {  // 64 tiles at a time, one a lane
+            int k1, i = 0;
+            const int p = kind.places(own_units(kind, x, w.rt + lane_id(), a.G, a.shift, w.key0, k1));
+            if (scalar(w.rows) >> kind.rows) {  // which of them
+                const int inc = wave_scan_i(p);
+                const uint64_t past = __ballot(off < inc);
+                i = past ? __builtin_ctzll(past) : kWave - 1;
+                off -= __builtin_amdgcn_readlane(past ? inc - p : inc, i);
+                if (!past) continue;
+            }
+            n = __builtin_amdgcn_readlane(p, i) - kind.before;
+            w.limit = __builtin_amdgcn_readlane(k1, i);
+            w.rt += i;
+            break;
         }
     }
-    s0 = scalar(at - off + kBefore<MANY>);
+    s0 = scalar(at - off + kind.before);
     s1 = s0 + scalar(n);
     // (what is read from LDS is the same for all lanes, which the compiler does not know: as vectors these would take the
     // registers of the accumulators)
@@ -350,7 +383,8 @@ __device__ __forceinline__ bool query_of(const PagedParams &a, const Plan &pl, c
     }
     t = r / a.G;
     g = r % a.G;
-    return t < pl.seq[bq].n;
+    const Seq x = pl.seq[bq];
+    return t < x.n && (!w.shared || x.first == w.b);  // (of runs that overlap, an entry belongs to the one that it names)
 }
 __device__ __forceinline__ long out_row(const PagedParams &a, const TileWork &w, int bq, int t, int g)
 {
@@ -404,11 +438,11 @@ struct PageList {
         return __builtin_amdgcn_readfirstlane(page < 0 || left < 0 ? 0 : left < 16 ? left : 16);
     }
 };
-template <typename ST, bool MANY>
-__device__ __forceinline__ PageList page_list(const PagedParams &a, const TileWork &w)
+template <typename ST>
+__device__ __forceinline__ PageList page_list(const PagedParams &a, const Kind &kind, const TileWork &w)
 {
-    constexpr int STEP = MANY ? 32 : kKeys<ST>;
-    const int end = min(w.limit, w.key0 + w.units * kUnit<ST, MANY>);
+    constexpr int STEP = kKeys<ST>;  // (of both kinds)
+    const int end = min(w.limit, w.key0 + (w.units << kind.unit));
     return PageList{a.table + (long)w.row_seq * a.M, w.key0, (end - w.key0 + STEP - 1) / STEP * (STEP / 16), w.limit, a.N, a.shift, -1};
 }
 
@@ -465,19 +499,20 @@ __device__ __forceinline__ bool not_finite(const char *lds, int at, int step, in
 }
 
 // The same tile key by key, only the keys that a row sees: where V holds an infinity or NaN that some row is not to see, and
-// a matrix product would take 0 times it.  D / 4 lanes a row, rows grp, grp + groups, ...
-template <typename ST, int D, bool MANY>
-__device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &pl, const TileWork &w, int grp, int groups)
+// a matrix product would take 0 times it.  D / 4 lanes a row, of the wave (few rows) or the workgroup.
+template <typename ST, int D>
+__device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &pl, const Kind &kind, const TileWork &w)
 {
-    constexpr int C4 = D / 4, ROWS = MANY ? kMany : kFew;
-    const int c4 = threadIdx.x % C4, end = min(w.limit, w.key0 + w.units * kUnit<ST, MANY>);
+    constexpr int C4 = D / 4;
+    const int c4 = threadIdx.x % C4, end = min(w.limit, w.key0 + (w.units << kind.unit)), n_rows = 1 << kind.rows;
+    const int grp = (kind.many ? threadIdx.x : lane_id()) / C4, groups = (kind.many ? kPagedThreads : kWave) / C4;
     const int32_t *pages = a.table + (long)w.row_seq * a.M;
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const float cs = a.scale * kLog2e;
 #pragma unroll 1
-    for (int r = grp; r < ROWS; r += groups) {
+    for (int r = grp; r < n_rows; r += groups) {
         int bq, t, g;
-        if (!query_of(a, pl, w, w.rt * ROWS + r, bq, t, g)) continue;
+        if (!query_of(a, pl, w, (w.rt << kind.rows) + r, bq, t, g)) continue;
         const long row = out_row(a, w, bq, t, g);
         const int last = w.shared ? end - 1 : min(end - 1, pl.seq[bq].L - pl.seq[bq].n + t);
         float q[4], m = -INFINITY, l = 0.f;
@@ -539,7 +574,7 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
 
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const ST *kb = (const ST *)a.k + pool * D, *vb = (const ST *)a.v + pool * D;
-    PageList pages = page_list<ST, false>(a, w);
+    PageList pages = page_list<ST>(a, kind_of<ST>(false), w);
     pages.take(w.entries);
 
     f32x4 kf[NH][NK];
@@ -726,7 +761,7 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
         load_v(x1, cV);
     }
     wait_loads<0>();  // (nothing lands in this LDS any more)
-    if (__any(odd)) return attend_by_key<ST, D, false>(a, pl, w, lane / (D / 4), 64 / (D / 4));
+    if (__any(odd)) return attend_by_key<ST, D>(a, pl, kind_of<ST>(false), w);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const float sum = quad_sum(l[rt]);
@@ -747,7 +782,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     const int lq = lane & 31, h = lane >> 5;
     const long pool = (long)w.kvh * ((long)a.N << a.shift);
     const bf16 *kb = (const bf16 *)a.k + pool * D, *vb = (const bf16 *)a.v + pool * D;
-    PageList pages = page_list<bf16, true>(a, w);
+    PageList pages = page_list<bf16>(a, kind_of<bf16>(true), w);
     const int n_steps = pages.last / 2;
     pages.take(w.entries);
 
@@ -817,7 +852,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
-    const float cs = a.scale * kLog2e;
+    const float cs = __int_as_float(scalar(__float_as_int(a.scale * kLog2e)));
     float m = -INFINITY, l = 0.f;
     wait_loads<4 * CPT>();  // the first tile has landed
     asm volatile("s_barrier" ::: "memory");
@@ -934,12 +969,13 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
         step(std::integral_constant<int, 3>{}, it + 3);
     }
     wait_loads<0>();  // (nothing lands in the ring any more)
-    if (__syncthreads_or(odd)) {
-        attend_by_key<bf16, D, true>(a, pl, w, threadIdx.x / (D / 4), kPagedThreads / (D / 4));
-        return;
-    }
+    if (__syncthreads_or(odd)) return attend_by_key<bf16, D>(a, pl, kind_of<bf16>(true), w);
     const float sum = half_pair_sum(l);
-    if (real) {
+    int again = threadIdx.x;  // (the row is found again: kept through the loop it would take more registers than there are)
+    asm volatile("" : "+v"(again));
+    const int r_out = wave * 32 + (again & 31);
+    if (query_of(a, pl, w, w.rt * kMany + r_out, bq, t, g)) {
+        const long row_out = out_row(a, w, bq, t, g);
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
@@ -947,7 +983,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
                 f32x4 o;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[j] = oacc[dt][4 * i + j];
-                put4<bf16, D>(a, w, row, r, 32 * dt + 8 * i + 4 * h, o, m, sum);
+                put4<bf16, D>(a, w, row_out, r_out, 32 * dt + 8 * i + 4 * h, o, m, sum);
             }
     }
 }
@@ -957,8 +993,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
 struct Span {
     int w0, w1, begun;
 };
-template <bool MANY>
-__device__ __forceinline__ Span span_of(const Shares<MANY> &sh, long s0, int units)
+__device__ __forceinline__ Span span_of(const Shares &sh, long s0, int units)
 {
     if (units == 0) return Span{0, -1, 0};
     const int w0 = sh.owner(s0), w1 = s0 + units <= sh.begin(w0 + 1) ? w0 : sh.owner(s0 + units - 1);
@@ -970,43 +1005,35 @@ struct JoinEntry {
     Span own, shared[2];  // of the own tile; of the run's tiles that hold the entry's rows (they may go on in a second one)
     int n, row0, many;    // new tokens; the first row in the run's tile; whether that is of many rows
 };
-template <typename ST, bool MANY>
-__device__ __forceinline__ Span shared_span(const PagedParams &a, const Plan &pl, const Shares<MANY> &sh, const Seq &x, int tile, int kvh)
-{
-    const int units = div_up(x.c << a.shift, kUnit<ST, MANY>), rows = pl.members[x.first] * a.T * a.G;
-    const long s0 = (long)kvh * sh.line + pl.start[MANY][x.first] + (long)tile * places<MANY>(units) + kBefore<MANY>;
-    return span_of<MANY>(sh, s0, tile * (MANY ? kMany : kFew) < rows ? units : 0);
-}
-template <typename ST, bool MANY>
-__device__ __forceinline__ Span own_span(const PagedParams &a, const Plan &pl, const Shares<MANY> &sh, const Seq &x, int b, int kvh)
-{
-    int k0, k1;
-    const int units = own_units<ST, MANY>(x, 0, a.G, a.shift, k0, k1), rows = pl.members[b] * a.T * a.G;
-    long s0 = (long)kvh * sh.line + pl.start[MANY][b] + kBefore<MANY>;
-    if (rows > 0 && x.c > 0 && shared_is_many<ST>(rows) == MANY)
-        s0 += (long)div_up(rows, MANY ? kMany : kFew) * places<MANY>(div_up(x.c << a.shift, kUnit<ST, MANY>));
-    return span_of<MANY>(sh, s0, units);
-}
-// a part of the entry: 0: its own tile and the numbers, 1, 2: the run's tiles (a thread each: the divisions take their time)
+// a part of the entry: 0: its own tile and the numbers, 1, 2: the run's tiles (a thread each: the divisions take their time).  One way
+// through for all of them and both kinds: as a way each this was a quarter of the kernel's code, more than the CUs' instruction
+// caches hold (64 KB), which every launch began by fetching.
 template <typename ST>
-__device__ __forceinline__ void fill_join_entry(const PagedParams &a, const Plan &pl, const Shares<false> &few, const Shares<true> &many, int b, int kvh,
+__device__ __forceinline__ void fill_join_entry(const PagedParams &a, const Plan &pl, const Shares &few, const Shares &many, int b, int kvh,
                                                 int part, JoinEntry &e)
 {
     const Seq x = pl.seq[b];
-    const bool shared_many = x.c > 0 && shared_is_many<ST>(pl.members[x.first] * a.T * a.G);
-    const int rows = shared_many ? kMany : kFew, row = (b - x.first) * a.T * a.G;
-    if (part == 0) {
-        if (sizeof(ST) == 2 && a.own_many) e.own = own_span<ST, true>(a, pl, many, x, b, kvh);
-        else e.own = own_span<ST, false>(a, pl, few, x, b, kvh);
-        e.n = x.n;
-        e.row0 = row % rows;
-        e.many = shared_many;
-    } else if (x.c == 0) {
-        e.shared[part - 1] = Span{0, -1, 0};
-    } else if (shared_many) {
-        e.shared[part - 1] = shared_span<ST, true>(a, pl, many, x, row / rows + part - 1, kvh);
+    const bool own = part == 0;
+    const int head = own ? b : x.first, run_rows = x.c > 0 ? pl.members[head] * a.T * a.G : 0;  // (0 too: no run begins at b)
+    const Kind run = kind_of<ST>(shared_is_many<ST>(run_rows)), kind = own ? kind_of<ST>(a.own_many) : run;
+    const int row = (b - x.first) * a.T * a.G, run_units = run.units(x.c << a.shift);
+    int units, tile, k0, k1;  // of the tile; tiles of the run before it among the entry's places
+    if (own) {
+        units = own_units(kind, x, 0, a.G, a.shift, k0, k1);
+        tile = run.many == kind.many ? run.tiles(run_rows) : 0;
     } else {
-        e.shared[part - 1] = shared_span<ST, false>(a, pl, few, x, row / rows + part - 1, kvh);
+        tile = (row >> run.rows) + part - 1;
+        units = tile < run.tiles(run_rows) ? run_units : 0;
+    }
+    const Shares sh = kind.many ? many : few;
+    const long s0 = (long)kvh * sh.line + pl.start[kind.many][head] + (long)tile * run.places(run_units) + kind.before;
+    const Span span = span_of(sh, s0, units);
+    if (own) {
+        e.own = span;
+        e.n = x.n;
+    } else {
+        e.shared[part - 1] = span;
+        if (part == 1) e.row0 = row & ((1 << run.rows) - 1), e.many = run.many;
     }
 }
 
@@ -1026,13 +1053,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
     const Ring ring{k0, k1, k2, k3, v0, v1, v2, v3};
     const Plan pl(lds_plan, a.B);
     make_plan<ST>(a, pl);
-    const Shares<false> few(pl, a.B, a.Hkv);
-    const Shares<true> many(pl, a.B, a.Hkv);
+    const Shares few(pl, a.B, a.Hkv, false), many(pl, a.B, a.Hkv, true);
     if (blockIdx.x == 0) {  // for the join
         const Plan to(a.plan + kPlanShares, a.B);
         if (threadIdx.x == 0) {
-            *reinterpret_cast<Shares<false> *>(a.plan) = few;
-            *reinterpret_cast<Shares<true> *>(a.plan + kPlanShares / 2) = many;
+            *reinterpret_cast<Shares *>(a.plan) = few;
+            *reinterpret_cast<Shares *>(a.plan + kPlanShares / 2) = many;
         }
         for (int b = threadIdx.x; b <= a.B; b += kPagedThreads) {
             to.start[0][b] = pl.start[0][b];
@@ -1048,64 +1074,61 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
         for (int p = blockIdx.x + kPagedGroups * (lane_id() / 4); p < a.B * a.Hkv; p += kPagedGroups * 16)
             if (lane_id() % 4 < 3) fill_join_entry<ST>(a, pl, few, many, p / a.Hkv, p % a.Hkv, lane_id() % 4, a.entries[p]);
     }
-    // the next part of a share, with the first entries of its table row on their way
-    auto next = [&](auto many_tag, TileWork &w, long &at, long wb, long we, int line, int share) __attribute__((always_inline)) -> bool {
-        constexpr bool MANY = decltype(many_tag)::value;
-        while (at < we) {
-            long s0, s1;
-            find_tile<ST, MANY>(a, pl, at, line, w, s0, s1);
-            const long from = max(at, s0), to = min(we, s1);
-            at = s1;
-            if (from >= to) continue;  // only places before the units
-            w.key0 += (int)(from - s0) * kUnit<ST, MANY>;
-            w.units = (int)(to - from);
-            w.record = record_of(s0, s1, wb, we);
-            w.cut = cut_row<MANY>(a, share, w.record & 1);
-            w.direct = w.record == 2 && !w.shared && scalar(pl.seq[w.b].c) == 0;
-            w.entries = page_list<ST, MANY>(a, w).fetch(0);
-            return true;
-        }
-        return false;
-    };
     // Workgroups are dealt to the eight XCDs in turn, and there in turn to the CUs.  On every XCD the two kinds are spread evenly, and
     // those of one XCD take neighbouring shares of a line, tiles of one KV head as a rule, whose rows they find in their L2; less
     // work than workgroups goes to all XCDs.
     const int xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8, groups = many_groups(scalar(pl.start[0][a.B]), scalar(pl.start[1][a.B]));
     const int each = groups / 8, before = in_xcd * each / (kPagedGroups / 8);  // many-row workgroups of an XCD, those before this one
+    // the next part of a share, with the first entries of its table row on their way
+    auto next = [&](const Kind &kind, const Shares &sh, int me, TileWork &w, long &at, long wb, long we) __attribute__((always_inline)) -> bool {
+        while (at < we) {
+            long s0, s1;
+            find_tile<ST>(a, pl, kind, at, sh.line, w, s0, s1);
+            const long from = max(at, s0), to = min(we, s1);
+            at = s1;
+            if (from >= to) continue;  // only places before the units
+            w.key0 += (int)(from - s0) << kind.unit;
+            w.units = (int)(to - from);
+            w.record = record_of(s0, s1, wb, we);
+            w.cut = cut_row(a, kind.many, me, w.record & 1);
+            w.direct = w.record == 2 && !w.shared && scalar(pl.seq[w.b].c) == 0;
+            w.entries = page_list<ST>(a, kind, w).fetch(0);
+            return true;
+        }
+        return false;
+    };
     if ((in_xcd + 1) * each / (kPagedGroups / 8) > before) {
         if constexpr (sizeof(ST) == 2) {
-            const Shares<true> &sh = many;
-            const int me = sh.n < groups ? before * 8 + xcd : xcd * each + before;
-            if (me < sh.n) {
-                const long wb = sh.begin(me), we = sh.begin(me + 1);
-                long at = wb;
-                TileWork w, then;
-                bool more = next(std::true_type{}, w, at, wb, we, sh.line, me);
+            const Kind kind = kind_of<ST>(true);
+            const int me = many.n < groups ? before * 8 + xcd : xcd * each + before;
+            if (me >= many.n) return;
+            const long wb = many.begin(me), we = many.begin(me + 1);
+            long at = wb;
+            TileWork w, then;
+            bool more = next(kind, many, me, w, at, wb, we);
 #pragma unroll 1
-                while (more) {
-                    more = next(std::true_type{}, then, at, wb, we, sh.line, me);
-                    attend_many<D>(a, pl, w, ring);
-                    w = then;
-                }
+            while (more) {
+                more = next(kind, many, me, then, at, wb, we);
+                attend_many<D>(a, pl, w, ring);
+                w = then;
             }
         }
     } else {
+        const Kind kind = kind_of<ST>(false);
         char *const even = wave == 0 ? k0 : wave == 1 ? k2 : wave == 2 ? v0 : v2, *const odd = wave == 0 ? k1 : wave == 1 ? k3 : wave == 2 ? v1 : v3;
-        const Shares<false> &sh = few;
         const int mine = in_xcd - before, of = kPagedGroups / 8 - each;  // few-row workgroups of the XCD
-        const int me = sh.n < of * 8 * kPagedWaves ? (wave * of + mine) * 8 + xcd : (xcd * of + mine) * kPagedWaves + wave;
-        if (me < sh.n) {
-            const long wb = sh.begin(me), we = sh.begin(me + 1);
-            long at = wb;
-            TileWork w, then;
-            bool more = next(std::false_type{}, w, at, wb, we, sh.line, me);
+        const int me = few.n < of * 8 * kPagedWaves ? (wave * of + mine) * 8 + xcd : (xcd * of + mine) * kPagedWaves + wave;
+        if (me >= few.n) return;
+        const long wb = few.begin(me), we = few.begin(me + 1);
+        long at = wb;
+        TileWork w, then;
+        bool more = next(kind, few, me, w, at, wb, we);
 #pragma unroll 1
-            while (more) {
-                more = next(std::false_type{}, then, at, wb, we, sh.line, me);
-                if (w.rows - w.rt * kFew <= 16) attend_few<ST, D, 1>(a, pl, w, even, odd);
-                else attend_few<ST, D, 2>(a, pl, w, even, odd);
-                w = then;
-            }
+        while (more) {
+            more = next(kind, few, me, then, at, wb, we);
+            if (w.rows - w.rt * kFew <= 16) attend_few<ST, D, 1>(a, pl, w, even, odd);
+            else attend_few<ST, D, 2>(a, pl, w, even, odd);
+            w = then;
         }
     }
 }
@@ -1141,7 +1164,7 @@ struct Join {
                 ml[i] = make_float2(-INFINITY, 0.f);
                 v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
                 if (x <= s.w1) {
-                    const long at = one ? whole : cut_row<MANY>(a, x, x == s.w0 ? s.begun : 0) + r;
+                    const long at = one ? whole : cut_row(a, MANY, x, x == s.w0 ? s.begun : 0) + r;
                     ml[i] = *reinterpret_cast<const float2 *>((one ? a.row_ml : a.cut_ml) + at * 2);
                     v[i] = *reinterpret_cast<const f32x4 *>((one ? a.row_o : a.cut_o) + at * D + 4 * c4);
                 }
@@ -1210,15 +1233,15 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_cuts_kernel(const Pa
             j.put(a, (long)(b * a.Hq + e / none) * a.T + e % none, c4);
         }
     }
-    const Shares<MANY> sh = *reinterpret_cast<const Shares<MANY> *>(a.plan + (MANY ? kPlanShares / 2 : 0));
+    const Shares sh = *reinterpret_cast<const Shares *>(a.plan + (MANY ? kPlanShares / 2 : 0));
     if ((int)blockIdx.x + 1 >= sh.n) return;
     const long cut = sh.begin(blockIdx.x + 1);
     TileWork w;
     long s0, s1;
-    find_tile<ST, MANY>(a, pl, cut, sh.line, w, s0, s1);
+    find_tile<ST>(a, pl, kind_of<ST>(MANY), cut, sh.line, w, s0, s1);
     if (cut <= s0 || sh.begin(blockIdx.x) > s0) return;  // not through its units; not its first
     const int rows = min(w.rows - w.rt * ROWS, ROWS);
-    const Span span = span_of<MANY>(sh, s0, (int)(s1 - s0));
+    const Span span = span_of(sh, s0, (int)(s1 - s0));
     for (int r = blockIdx.y * NG + grp; r < rows; r += gridDim.y * NG) {
         int bq, t, g;
         if (!query_of(a, pl, w, w.rt * ROWS + r, bq, t, g)) continue;

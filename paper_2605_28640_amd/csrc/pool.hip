@@ -22,17 +22,6 @@ struct PoolView {
 
 __device__ __forceinline__ int pages_of(int tokens, int shift) { return (int)(((uint32_t)tokens + (1u << shift) - 1) >> shift); }
 
-// inclusive prefix sum over a wave
-__device__ __forceinline__ int wave_scan_i(int v)
-{
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int o = __shfl_up(v, d, kWave);
-        if (lane_id() >= d) v += o;
-    }
-    return v;
-}
-
 // what precedes this thread's value among the workgroup's, and (total) their sum; tot: LDS of one word a wave
 __device__ __forceinline__ int block_scan_i(int v, int *tot, int &total)
 {

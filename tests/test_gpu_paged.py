@@ -135,6 +135,13 @@ def test_many_sequences(rs, dtype):
     b.check(*b.run(), heads=[0, 3])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompts_of_many_tiles(rs, dtype):
+    """More row tiles to a sequence than a wave has lanes; one of them, and none, for the others."""
+    b = Batch(rs, 4, 1, 64, 16, [2600, 2100, 0, 30], (), 0, 2600, [2600, 900, 0, 1], dtype, seed=13)
+    b.check(*b.run(), heads=[0, 3])
+
+
 def test_listed_in_another_order_and_twice(rs):
     b = Batch(rs, 4, 2, 64, 16, [40, 35, 70, 90], (), 0, 1)
     out, lse = b.run()
@@ -212,6 +219,16 @@ def test_sequences_and_shares_that_are_out_of_range(rs):
                   [[0, 2, -3]] * 3, [[0, 2 ** 31 - 1, 1]] * 3):  # none of these describes a run: each by itself
         b.share = share
         b.check(*b.run())  # (joined in another order than without the argument)
+
+
+def test_shares_whose_runs_overlap(rs):
+    """No page_pool_share gives these: an entry belongs to the run that it names, and to none if that does not reach it."""
+    b = Batch(rs, 4, 2, 64, 16, [64, 70, 90], (3,), 48, 1, None, "f32")
+    for share in ([[0, 3, 3], [1, 2, 2], [1, 2, 2]], [[0, 3, 3], [1, 2, 3], [0, 3, 1]], [[0, 2, 3], [0, 2, 3], [0, 2, 3]]):
+        b.share = share
+        first = b.run()
+        b.check(*first)
+        assert all(torch.equal(x, y) for x, y in zip(first, b.run()))
 
 
 def test_a_longer_workspace_and_what_it_held_before(rs):
