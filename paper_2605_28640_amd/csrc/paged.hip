@@ -12,7 +12,10 @@
 //     own, the next step's K and the V of two steps on their way.  No barrier anywhere; what a wave waits for at
 //     a tile's beginning and end, the others of its CU fill.
 //   many rows (tiles of 128; bfloat16): bound by the matrix units.  A workgroup: every wave takes 32 rows, all four go through the same
-//     keys, K and V tiles in a ring of four LDS slots filled three steps ahead, one barrier a step.
+//     keys, K and V tiles in a ring of LDS slots, one barrier a step.  Where a sequence's own rows fill more than a small tile, all tiles of
+//     the call are of this kind, and a kernel with nothing else in it takes three workgroups to a CU (168 registers, three
+//     slots of 16 KB filled two steps ahead) instead of two (four slots, three steps): eight prompts' questions of 150 to 384 tokens after 16384, 32
+//     heads over 8, 670 us against 731; one prompt of 32768 tokens 9.5 ms against 10.6 (929 TFLOP/s).
 // In both S^T = K Q^T and O^T = V^T P^T, so that a lane holds the keys of one query and P^T goes from the accumulators into the
 // second product as it is.
 //
@@ -36,6 +39,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 constexpr int kPagedGroups = 512;      // two workgroups a CU
+constexpr int kManyGroups = 768;       // where all tiles are of many rows: three
+constexpr int kCus = 256;
 constexpr int kMaxList = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;          // the softmax's reference point moves when the maximum has grown by more (base-2 exponent)
@@ -56,7 +61,8 @@ struct PagedParams {
     struct JoinEntry *entries;  // [B][Hkv], for the join where a sequence's rows are one tile, else nullptr
     long few_base;              // the first row of the few-row tiles' boundary records
     int few_rows;               // rows that a few-row tile of this call can have
-    int own_many;               // whether a sequence's own tiles are of many rows
+    int own_many;               // whether a sequence's own tiles are of many rows (then all are)
+    int groups;                 // workgroups of the first launch
     int B, Hq, Hkv, G, S, M, N, shift, T;
     float scale;
 };
@@ -220,9 +226,9 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
 
 // How many of the workgroups take many-row tiles: by the bytes of both kinds' keys, a multiple of the eight XCDs, at least eight for
 // each kind that there is.
-__device__ __forceinline__ int many_groups(int few_line, int many_line)
+__device__ __forceinline__ int many_groups(int few_line, int many_line, int groups)
 {
-    if (many_line == 0 || few_line == 0) return many_line > 0 ? kPagedGroups : 0;
+    if (many_line == 0 || few_line == 0) return many_line > 0 ? groups : 0;
     const float many = (float)many_line * 5.f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
     return 8 * max(1, min(kPagedGroups / 8 - 1, (int)(part * (kPagedGroups / 8) + 0.5f)));
 }
@@ -231,9 +237,10 @@ __device__ __forceinline__ int many_groups(int few_line, int many_line)
 // first by its memory path (four sequences of 65536 tokens, 8 heads, with equal shares: every one of the first 256 workgroups done after
 // 131-145 us, every other after 157-171).
 struct Shares {
-    static constexpr int kOlder = 11, kNewer = 9;
+    static constexpr int kOlder = 11, kOldest = 12, kNewer = 9;
     int line, n;             // places of a KV head, shares
-    int of_xcd, older, sum;  // shares of an XCD, those of its first workgroups, their places' weights together (0: equal shares)
+    int of_xcd, older, weight;  // shares of an XCD, those of its first workgroups, the weight of one of these
+    int sum;                 // the weights of an XCD's shares together (0: equal shares)
     int each, more;          // equal shares: the first `more` have each + 1
     long all;
     double unit;             // places for each unit of weight
@@ -241,20 +248,21 @@ struct Shares {
     float per_unit;          // of unit; equal shares: of a share's places
     float per_xcd, per_sum;  // of of_xcd, of sum
     Shares() = default;
-    __device__ __forceinline__ Shares(const Plan &pl, int B, int Hkv, bool MANY)
+    __device__ __forceinline__ Shares(const Plan &pl, int B, int Hkv, int all_groups, bool MANY)
     {
         static_assert(sizeof(Shares) <= kPlanShares / 2, "room in the workspace");
-        const int f = scalar(pl.start[0][B]), m = scalar(pl.start[1][B]), groups = many_groups(f, m);
+        const int f = scalar(pl.start[0][B]), m = scalar(pl.start[1][B]), groups = many_groups(f, m, all_groups);
         line = MANY ? m : f;
         all = (long)line * Hkv;
-        const int half = groups / 16;  // many-row workgroups among an XCD's first 32
-        of_xcd = MANY ? groups / 8 : (kPagedGroups - groups) / 8 * kPagedWaves;
-        older = MANY ? half : (kPagedGroups / 16 - half) * kPagedWaves;
+        const int first = groups == kManyGroups ? kCus / 8 : groups / 16;  // many-row workgroups among an XCD's first 32
+        of_xcd = MANY ? groups / 8 : (all_groups - groups) / 8 * kPagedWaves;
+        older = MANY ? first : (kCus / 8 - first) * kPagedWaves;
+        weight = groups == kManyGroups ? kOldest : kOlder;
         n = 8 * of_xcd;
         sum = 0;
         each = 1, more = 0, unit = 0., per_unit = per_xcd = per_sum = 0.f;
         if (n > 0 && all >= 4l * n) {
-            sum = older * kOlder + (of_xcd - older) * kNewer;
+            sum = older * weight + (of_xcd - older) * kNewer;
             per_sum = __builtin_amdgcn_rcpf((float)sum);
             per_xcd = __builtin_amdgcn_rcpf((float)of_xcd);
             unit = (double)all * (double)(0.125f * per_sum);  // (off by 2^-22 of it: begin() rounds a whole number back up)
@@ -275,7 +283,7 @@ struct Shares {
         if (sum == 0) return w * each + min(w, more);
         if (w >= n) return all;
         const int x = quotient(w, per_xcd), i = w - x * of_xcd;
-        return (long)((double)(x * sum + min(i, older) * kOlder + max(i - older, 0) * kNewer) * unit + 0.0625);
+        return (long)((double)(x * sum + min(i, older) * weight + max(i - older, 0) * kNewer) * unit + 0.0625);
     }
     __device__ __forceinline__ int owner(long place) const
     {
@@ -284,7 +292,7 @@ struct Shares {
             w = (int)((float)place * per_unit);
         } else {
             const int at = (int)((float)place * per_unit), x = quotient(at, per_sum), r = at - x * sum;
-            w = x * of_xcd + (r < older * kOlder ? r / kOlder : older + (r - older * kOlder) / kNewer);
+            w = x * of_xcd + (r < older * weight ? (weight == kOldest ? r / kOldest : r / kOlder) : older + (r - older * weight) / kNewer);
         }
         w = max(0, min(w, n - 1));
         while (w > 0 && begin(w) > place) --w;  // (at most a step or two: the quotients are rounded)
@@ -773,8 +781,11 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------
-// 32-wide matrix instructions: lane (lq, h) = (lane % 32, lane / 32) holds query lq and keys 8 i + 4 h .. + 3 of a step's 32.
-template <int D>
+// 32-wide matrix instructions: lane (lq, h) = (lane % 32, lane / 32) holds query lq and keys 8 i + 4 h .. + 3 of a step's 32.  With three slots
+// (three waves to a SIMD) registers are what is short: no step is passed over (one that no row of the wave sees comes out as nothing,
+// its weights are 0 and its values finite, or the tile is taken key by key), since a way round the arithmetic keeps a second set of accumulators,
+// and what a lane's addresses differ in is worked out anew every step.
+template <int D, int SLOTS>
 __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl, const TileWork &w, const Ring &lds)
 {
     constexpr int NC = D / 16, NDT = D / 32, CR = D / 8, RW = 64 / CR, RPI = kPagedWaves * RW, CPT = 32 / RPI, ROW = 2 * D;
@@ -811,9 +822,12 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     int valid1 = look_up(1);
 #pragma unroll
     for (int i = 0; i < CPT; ++i) stage_k(i, lds.k1), stage_v(i, lds.v1);
-    int valid2 = look_up(2);
+    int valid2 = 0;
+    if constexpr (SLOTS == 4) {
+        valid2 = look_up(2);
 #pragma unroll
-    for (int i = 0; i < CPT; ++i) stage_k(i, lds.k2), stage_v(i, lds.v2);
+        for (int i = 0; i < CPT; ++i) stage_k(i, lds.k2), stage_v(i, lds.v2);
+    }
 
     // ---- this lane's query ----
     int bq = 0, t = 0, g = 0;
@@ -843,9 +857,9 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     // operand addresses inside a tile: K row lq, chunk 2 c + h; V through the transpose read, lane = 32 h + 16 dg + L supplying 8 bytes of row
     // 16 c + 4 h + L / 4 (+ 8 for the second read) at channel 32 dt + 16 dg + 4 (L % 4)
     const int L16 = lane & 15, dg = (lane >> 4) & 1;
-    const uint32_t koff = (uint32_t)(lq * ROW + ((h ^ chunk_swizzle<D>(lq)) * 16));
+    uint32_t koff = (uint32_t)(lq * ROW + ((h ^ chunk_swizzle<D>(lq)) * 16));
     const int rowa = 4 * h + (L16 >> 2);
-    const uint32_t voff = (uint32_t)(rowa * ROW + (((2 * dg + ((L16 & 3) >> 1)) ^ chunk_swizzle<D>(rowa)) * 16) + 8 * (L16 & 1));
+    uint32_t voff = (uint32_t)(rowa * ROW + (((2 * dg + ((L16 & 3) >> 1)) ^ chunk_swizzle<D>(rowa)) * 16) + 8 * (L16 & 1));
 
     f32x16 oacc[NDT];
 #pragma unroll
@@ -854,18 +868,21 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
         for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
     const float cs = __int_as_float(scalar(__float_as_int(a.scale * kLog2e)));
     float m = -INFINITY, l = 0.f;
-    wait_loads<4 * CPT>();  // the first tile has landed
+    wait_loads<2 * (SLOTS - 2) * CPT>();  // the first tile has landed
     asm volatile("s_barrier" ::: "memory");
 
     auto step = [&](auto buf_tag, int it) __attribute__((always_inline)) {
         constexpr int BUF = decltype(buf_tag)::value;
         const char *cK = BUF == 0 ? lds.k0 : BUF == 1 ? lds.k1 : BUF == 2 ? lds.k2 : lds.k3, *cV = BUF == 0 ? lds.v0 : BUF == 1 ? lds.v1 : BUF == 2 ? lds.v2 : lds.v3;
-        char *nK = BUF == 0 ? lds.k3 : BUF == 1 ? lds.k0 : BUF == 2 ? lds.k1 : lds.k2, *nV = BUF == 0 ? lds.v3 : BUF == 1 ? lds.v0 : BUF == 2 ? lds.v1 : lds.v2;
+        asm volatile("" : "+v"(koff), "+v"(voff));  // (else the 12 addresses made of them are kept in registers)
+        constexpr int TO = (BUF + SLOTS - 1) % SLOTS;  // what the step before this one has read
+        char *nK = TO == 0 ? lds.k0 : TO == 1 ? lds.k1 : TO == 2 ? lds.k2 : lds.k3, *nV = TO == 0 ? lds.v0 : TO == 1 ? lds.v1 : TO == 2 ? lds.v2 : lds.v3;
         const int key = w.key0 + it * 32, here = valid0;
+        const int then = look_up(it + SLOTS - 1);  // (past the last step: descriptors of no rows)
         valid0 = valid1;
-        valid1 = valid2;
-        valid2 = look_up(it + 3);  // (past the last step: descriptors of no rows)
-        const bool live = key <= wave_last && it < n_steps;
+        valid1 = SLOTS == 4 ? valid2 : then;
+        valid2 = then;
+        const bool live = SLOTS == 3 || (key <= wave_last && it < n_steps);
         if (key + 31 > tile_first) odd |= not_finite<bf16>(cV, threadIdx.x, kPagedThreads, 32 * ROW / 16);
         if (!live) {
 #pragma unroll
@@ -895,6 +912,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
             const bool edge = key + 31 > first_last;
 #pragma unroll
             for (int v = 0; v < 16; ++v) s[v] *= cs;
+            asm volatile("" : "+v"(s));  // (nothing of what follows is begun before this: it would not fit beside the scores)
             if (edge || here != (16 | 16 << 8)) {
                 const int sees0 = min(here & 255, edge ? last + 1 - key : 16) - 4 * h, sees1 = min(here >> 8, edge ? last - 15 - key : 16) - 4 * h;
 #pragma unroll
@@ -955,18 +973,18 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
             __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
             __builtin_amdgcn_s_setprio(0);
         }
-        // the next step's tile has landed (the two after it may be on their way), and this wave has read what it needs
-        __builtin_amdgcn_s_waitcnt(0x0070 | (4 * CPT));
+        // the next step's tile has landed (those after it may be on their way), and this wave has read what it needs
+        __builtin_amdgcn_s_waitcnt(0x0070 | (2 * (SLOTS - 2) * CPT));
         asm volatile("s_barrier" ::: "memory");
     };
     // (whole turns of the ring: steps past the last one only pass the barrier.  With ways out between the steps the compiler keeps two
     // sets of accumulators and copies one to the other every step.)
 #pragma unroll 1
-    for (int it = 0; it < n_steps; it += 4) {
+    for (int it = 0; it < n_steps; it += SLOTS) {
         step(std::integral_constant<int, 0>{}, it);
         step(std::integral_constant<int, 1>{}, it + 1);
         step(std::integral_constant<int, 2>{}, it + 2);
-        step(std::integral_constant<int, 3>{}, it + 3);
+        if constexpr (SLOTS == 4) step(std::integral_constant<int, 3>{}, it + 3);
     }
     wait_loads<0>();  // (nothing lands in the ring any more)
     if (__syncthreads_or(odd)) return attend_by_key<bf16, D>(a, pl, kind_of<bf16>(true), w);
@@ -1037,8 +1055,9 @@ __device__ __forceinline__ void fill_join_entry(const PagedParams &a, const Plan
     }
 }
 
-template <typename ST, int D>
-__global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const PagedParams a)
+// ALL_MANY: for calls all of whose tiles are of many rows
+template <typename ST, int D, bool ALL_MANY>
+__global__ __launch_bounds__(kPagedThreads) __attribute__((amdgpu_waves_per_eu(ALL_MANY ? 3 : 2, ALL_MANY ? 3 : 2))) void paged_attend_kernel(const PagedParams a)
 {
     constexpr int TILE = kKeys<ST> * D * (int)sizeof(ST);
     __shared__ __attribute__((aligned(1024))) char k0[TILE];
@@ -1047,13 +1066,13 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
     __shared__ __attribute__((aligned(1024))) char v0[TILE];
     __shared__ __attribute__((aligned(1024))) char v1[TILE];
     __shared__ __attribute__((aligned(1024))) char v2[TILE];
-    __shared__ __attribute__((aligned(1024))) char k3[TILE];
-    __shared__ __attribute__((aligned(1024))) char v3[TILE];
+    __shared__ __attribute__((aligned(ALL_MANY ? 16 : 1024))) char k3[ALL_MANY ? 16 : TILE];
+    __shared__ __attribute__((aligned(ALL_MANY ? 16 : 1024))) char v3[ALL_MANY ? 16 : TILE];
     extern __shared__ __attribute__((aligned(16))) char lds_plan[];
     const Ring ring{k0, k1, k2, k3, v0, v1, v2, v3};
     const Plan pl(lds_plan, a.B);
     make_plan<ST>(a, pl);
-    const Shares few(pl, a.B, a.Hkv, false), many(pl, a.B, a.Hkv, true);
+    const Shares few(pl, a.B, a.Hkv, a.groups, false), many(pl, a.B, a.Hkv, a.groups, true);
     if (blockIdx.x == 0) {  // for the join
         const Plan to(a.plan + kPlanShares, a.B);
         if (threadIdx.x == 0) {
@@ -1071,14 +1090,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
     }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (a.entries && wave == kPagedWaves - 1) {  // (here, and not when all is done: what it needs would have to be kept in registers until then)
-        for (int p = blockIdx.x + kPagedGroups * (lane_id() / 4); p < a.B * a.Hkv; p += kPagedGroups * 16)
+        for (int p = blockIdx.x + a.groups * (lane_id() / 4); p < a.B * a.Hkv; p += a.groups * 16)
             if (lane_id() % 4 < 3) fill_join_entry<ST>(a, pl, few, many, p / a.Hkv, p % a.Hkv, lane_id() % 4, a.entries[p]);
     }
     // Workgroups are dealt to the eight XCDs in turn, and there in turn to the CUs.  On every XCD the two kinds are spread evenly, and
     // those of one XCD take neighbouring shares of a line, tiles of one KV head as a rule, whose rows they find in their L2; less
     // work than workgroups goes to all XCDs.
-    const int xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8, groups = many_groups(scalar(pl.start[0][a.B]), scalar(pl.start[1][a.B]));
-    const int each = groups / 8, before = in_xcd * each / (kPagedGroups / 8);  // many-row workgroups of an XCD, those before this one
+    const int xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8, groups = many_groups(scalar(pl.start[0][a.B]), scalar(pl.start[1][a.B]), a.groups), of_xcd = a.groups / 8;
+    const int each = groups / 8, before = in_xcd * each / of_xcd;  // many-row workgroups of an XCD, those before this one
     // the next part of a share, with the first entries of its table row on their way
     auto next = [&](const Kind &kind, const Shares &sh, int me, TileWork &w, long &at, long wb, long we) __attribute__((always_inline)) -> bool {
         while (at < we) {
@@ -1097,7 +1116,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
         }
         return false;
     };
-    if ((in_xcd + 1) * each / (kPagedGroups / 8) > before) {
+    if (ALL_MANY || (in_xcd + 1) * each / of_xcd > before) {
         if constexpr (sizeof(ST) == 2) {
             const Kind kind = kind_of<ST>(true);
             const int me = many.n < groups ? before * 8 + xcd : xcd * each + before;
@@ -1109,14 +1128,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend_kernel(const Pa
 #pragma unroll 1
             while (more) {
                 more = next(kind, many, me, then, at, wb, we);
-                attend_many<D>(a, pl, w, ring);
+                attend_many<D, ALL_MANY ? 3 : 4>(a, pl, w, ring);
                 w = then;
             }
         }
-    } else {
+    } else if constexpr (!ALL_MANY) {
         const Kind kind = kind_of<ST>(false);
         char *const even = wave == 0 ? k0 : wave == 1 ? k2 : wave == 2 ? v0 : v2, *const odd = wave == 0 ? k1 : wave == 1 ? k3 : wave == 2 ? v1 : v3;
-        const int mine = in_xcd - before, of = kPagedGroups / 8 - each;  // few-row workgroups of the XCD
+        const int mine = in_xcd - before, of = of_xcd - each;  // few-row workgroups of the XCD
         const int me = few.n < of * 8 * kPagedWaves ? (wave * of + mine) * 8 + xcd : (xcd * of + mine) * kPagedWaves + wave;
         if (me >= few.n) return;
         const long wb = few.begin(me), we = few.begin(me + 1);
@@ -1258,6 +1277,7 @@ static int tile_rows(const rs_shape *s) { return s->dtype == RS_BF16 ? kMany : k
 struct PagedLayout {
     bool own_many, shares;   // a sequence's own tiles are of many rows; rows of several sequences may be put together
     int few_rows;            // rows of a few-row tile, at most
+    int groups;              // of the first launch
     size_t many, cut, rows;  // boundary records' rows of many-row tiles, of both kinds; row records
     size_t off_ml, off_plan, total;
 };
@@ -1271,8 +1291,10 @@ static PagedLayout paged_layout(const rs_shape *s, int T_new)
     const long most = x.shares ? own * s->B : own;
     x.own_many = s->dtype == RS_BF16 && own > kFew;
     x.few_rows = (int)(most < kFew ? most : kFew);
-    x.many = (s->dtype == RS_BF16 && most > kFew) ? (size_t)2 * kPagedGroups * kMany : 0;
-    x.cut = x.many + (size_t)2 * kPagedGroups * kPagedWaves * x.few_rows;
+    // (three of 49.4 KB and 36 bytes an entry in the 160 KB of a CU; of longer lists, two)
+    x.groups = x.own_many && s->B <= 112 ? kManyGroups : kPagedGroups;
+    x.many = (s->dtype == RS_BF16 && most > kFew) ? (size_t)2 * x.groups * kMany : 0;
+    x.cut = x.many + (x.own_many ? 0 : (size_t)2 * kPagedGroups * kPagedWaves * x.few_rows);
     x.rows = x.shares ? (size_t)s->B * s->Hq * T_new * 2 : 0;
     x.off_ml = RS_WS_CTRL_BYTES + align256((x.cut + x.rows) * s->D * 4);
     x.off_plan = x.off_ml + align256((x.cut + x.rows) * 8);
@@ -1298,10 +1320,11 @@ static int check_paged(const rs_shape *s, const rs_pool *p, int T_new)
 template <typename ST, int D>
 static void paged_launch(const PagedParams &a, hipStream_t stream)
 {
-    paged_attend_kernel<ST, D><<<kPagedGroups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
+    if (sizeof(ST) == 2 && a.own_many) paged_attend_kernel<ST, D, sizeof(ST) == 2><<<a.groups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
+    else paged_attend_kernel<ST, D, false><<<a.groups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
     const long rows = (long)a.B * a.Hq * a.T;
     if (a.entries) paged_join_rows_kernel<ST, D><<<(unsigned)(rows < 8192 ? rows : 8192), 64, 0, stream>>>(a);
-    else if (sizeof(ST) == 2) paged_join_cuts_kernel<ST, D, true><<<dim3(kPagedGroups, 4), kPagedThreads, 0, stream>>>(a);
+    else if (sizeof(ST) == 2) paged_join_cuts_kernel<ST, D, true><<<dim3((unsigned)a.groups, 4), kPagedThreads, 0, stream>>>(a);
     else paged_join_cuts_kernel<ST, D, false><<<kPagedGroups * kPagedWaves, kPagedThreads, 0, stream>>>(a);
 }
 
@@ -1337,7 +1360,7 @@ int32_t attn_paged(const rs_shape *s, const rs_pool *p, const void *q, const voi
     a.cut_ml = (float *)((char *)ws + x.off_ml), a.row_ml = a.cut_ml + x.cut * 2;
     a.plan = (char *)ws + x.off_plan;
     a.entries = x.shares ? (JoinEntry *)(a.plan + kPlanShares + plan_room(s->B)) : nullptr;
-    a.few_base = (long)x.many, a.few_rows = x.few_rows, a.own_many = x.own_many;
+    a.few_base = (long)x.many, a.few_rows = x.few_rows, a.own_many = x.own_many, a.groups = x.groups;
     a.B = s->B, a.Hq = s->Hq, a.Hkv = s->Hkv, a.G = s->Hq / s->Hkv;
     a.S = p->S, a.M = p->M, a.N = p->N, a.shift = __builtin_ctz((unsigned)p->P), a.T = T_new;
     a.scale = scale;

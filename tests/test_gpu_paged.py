@@ -142,6 +142,27 @@ def test_prompts_of_many_tiles(rs, dtype):
     b.check(*b.run(), heads=[0, 3])
 
 
+MANY = [
+    # Hq, Hkv, D, P, lens, runs, shared, T, counts: every sequence has more rows than a small tile
+    (8, 2, 128, 16, [100, 97, 130, 60], (3,), 64, 12, [12, 5, 12, 0]),          # with room for others' in a large one
+    (6, 2, 64, 32, [200, 230, 225, 700, 300], (2, 2), 192, 11, None),           # two runs
+    (40, 1, 128, 16, [40, 41, 600], (2,), 32, 3, [3, 1, 2]),
+    (4, 2, 64, 16, [20 + b % 45 for b in range(150)], (100,), 16, 17, None),    # a long list
+    (2, 2, 128, 16, [33, 129, 4000], (), 0, 33, [33, 33, 20]),                  # one row past a small tile; one step past a turn of the ring
+]
+
+
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_many_rows_a_sequence(rs, case):
+    Hq, Hkv, D, P, lens, runs, shared, T, counts = MANY[case]
+    say("many", case)
+    b = Batch(rs, Hq, Hkv, D, P, lens, runs, shared, T, counts, "bf16", seed=40 + case)
+    got = b.run()
+    b.check(*got, heads=[0, Hq - 1])
+    b.check(*b.run(share=False), heads=[0, Hq - 1])
+    assert all(torch.equal(x, y) for x, y in zip(got, b.run()))
+
+
 def test_listed_in_another_order_and_twice(rs):
     b = Batch(rs, 4, 2, 64, 16, [40, 35, 70, 90], (), 0, 1)
     out, lse = b.run()
