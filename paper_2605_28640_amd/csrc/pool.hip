@@ -3,8 +3,12 @@
 //
 // A page is free exactly when its reference count is 0, and the lowest numbered free page is always taken first, so there is
 // no free list to keep in step: the counts are the only state.  Finding pages is one workgroup's pass over the counts (4 bytes
-// a page), in order, with a prefix sum over its threads; a fork's and a release's table rows are a launch of their own over all
-// CUs.  Every call is decided as a whole by that one workgroup before anything is written: refused calls change nothing.
+// a page), in order, with a prefix sum over its threads.  Every call is decided as a whole by that one workgroup before anything is
+// written: refused calls change nothing.  What bounds these calls is the trips to memory that follow from one another (list,
+// lengths, table, counts: 0.5 us and more each) and the launches themselves, not bytes; so rows of the table are
+// written by the deciding workgroup where they are few, and by a second launch over all CUs where they are not.
+// Kernel time, us: room for 64 tokens of 64 sequences 6, for 8 questions of up to 384 tokens 7; a release of 4 sequences of 2000 tokens 3, a
+// fork 7, their shares 2.4; of 64 with 32700 tokens (two launches each) 7, 10.5, 6.5; compaction of 1000 pages 4.4 + 3.0, of 32768 18 + 5.
 #include "check.h"
 #include "common.h"
 
@@ -166,13 +170,18 @@ __device__ __forceinline__ void free_row(const PoolView &p, int seq, int n, int 
         if (page >= 0 && page < p.N) atomicSub(&p.refs[page], 1);
     }
 }
-// Rows of so few entries in all are done by the workgroup that decides (a wave a row), others by a launch of their own.
-constexpr long kRowsHere = 8192;
+// The rows of n sequences are done by the workgroup that decides, a wave a row at a time, 64 entries a trip, where a wave has at
+// most 8 trips to make; else by a launch of their own.  A release, a fork and its copies of n sequences of M pages, us, here / apart:
+// 16 of 126 25.8 / 32.5, 32 of 250 26.0 / 30.1, 16 of 501 26.5 / 30.1, 64 of 126 29.9 / 30.1; 16 of 1001 40.6 / 30.2, 64 of 501 51.3 / 38.0.
+static bool rows_here(long n, long M) { return (n + 15) / 16 * ((M + 63) / 64) <= 8; }
+// Likewise the comparison of neighbours, 256 entries a trip after the two for list and lengths: 16 of 126 28.2 / 32.5, 64 of 126 29.5 / 30.1,
+// 4 of 1876 27.3 / 29.8; 64 of 501 41.7 / 38.0.
+static bool shares_here(long n, long M) { return (n + 15) / 16 * (2 + (M + 255) / 256) <= 12; }
 
 // full: n words, the pages that entry i takes over from its source (none where the call is refused)
 __global__ __launch_bounds__(kPoolThreads) void pool_fork_kernel(PoolView p, const int32_t *__restrict__ src,
                                                                  const int32_t *__restrict__ dst, int n, int2 *pairs, int2 *carry,
-                                                                 int32_t *full, int32_t *list, uint32_t *err, bool rows_here)
+                                                                 int32_t *full, int32_t *list, uint32_t *err, bool here)
 {
     __shared__ uint32_t seen[kMaxSeqs / 32];
     __shared__ int tot[kPoolThreads / kWave];
@@ -221,7 +230,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_fork_kernel(PoolView p, con
         if (carry) carry[i] = cr;
     }
     if (bad && tid == 0) *err = kErrPages;
-    if (!rows_here || bad) return;
+    if (!here || bad) return;
     __syncthreads();
     for (int i = tid >> 6; i < n; i += kPoolThreads / kWave) fork_row(p, src[i], dst[i], full[i], lane_id(), kWave);
 }
@@ -235,7 +244,7 @@ __global__ __launch_bounds__(256) void pool_fork_rows_kernel(PoolView p, const i
 
 // held: n words, the pages that entry i gives up (none where the call is refused)
 __global__ __launch_bounds__(kPoolThreads) void pool_free_kernel(PoolView p, const int32_t *__restrict__ seq, int n, int32_t *held,
-                                                                 uint32_t *err, bool rows_here)
+                                                                 uint32_t *err, bool here)
 {
     __shared__ uint32_t seen[kMaxSeqs / 32];
     const int tid = threadIdx.x;
@@ -252,7 +261,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_free_kernel(PoolView p, con
         if (!bad) p.len[seq[i]] = 0;
     }
     if (bad && tid == 0) *err = kErrPages;
-    if (!rows_here || bad) return;
+    if (!here || bad) return;
     __syncthreads();
     for (int i = tid >> 6; i < n; i += kPoolThreads / kWave) free_row(p, seq[i], held[i], lane_id(), kWave);
 }
@@ -461,7 +470,8 @@ struct CopyView {
 };
 
 // Listed pages of every KV head from one pool to another (or the same).  Nothing but bytes: a page of one head is one run of
-// P rows, 2 KB and more.  A workgroup takes (pair, head) after (pair, head).
+// P rows, 2 KB and more.  A workgroup takes (pair, head) after (pair, head).  1.1 GB (16384 pages of 16 tokens, 8 heads of
+// 128): 236 us, 4.7 TB/s, what a plain copy reaches; 64 pages of 64 tokens 20 us.
 __global__ __launch_bounds__(256) void page_copy_kernel(CopyView s, CopyView d, const int2 *__restrict__ pairs, int n,
                                                         const int32_t *__restrict__ n_pairs, int Hkv, int page_bytes, int meta_bytes)
 {
@@ -588,7 +598,8 @@ __device__ __forceinline__ void put_bounds(ST *bounds, int slice, float (&lo)[8]
 
 // One token a sequence: s = g s + (1 - g) x in float32, the rounded state to the token's row, its page's bounds from the page's rows so
 // far, which need not have been current before.  Nothing but trips to memory: the list, then length and table, then the rows of the
-// page, everything else beside them; a wave for 64 channels, its eight slices reading the page's rows side by side.
+// page, everything else beside them; a wave for 64 channels, its eight slices reading the page's rows side by side.  64
+// sequences, 8 heads of 128: 5.3 us (a wave for 128 channels, rows one after the other: 8).
 template <typename ST, int D>
 __global__ __launch_bounds__(64) void append_token_kernel(const AppendParams a)
 {
@@ -630,7 +641,8 @@ __global__ __launch_bounds__(64) void append_token_kernel(const AppendParams a)
 // Several tokens a sequence.  The recurrence is linear, so a run of tokens is (A, S): s -> A s + S, and runs compose: a workgroup takes 32 W tokens at a
 // time, 4 a slice; every slice forms its run's (A, S), a scan over the slices (shuffles in a wave, LDS between waves) gives each
 // its first state, from which it goes through its 4 tokens as written.  The next tokens' inputs are on their way meanwhile.  Then the bounds
-// of the pages touched, from their rows.
+// of the pages touched, from their rows.  8 questions of 150 to 384 tokens, 8 heads of 128: 22 us (token after token 165; with slices of one wave
+// only, 32).
 template <typename ST, int D, int W>
 __global__ __launch_bounds__(64 * W) void append_run_kernel(const AppendParams a)
 {
@@ -754,7 +766,9 @@ __global__ __launch_bounds__(64 * W) void append_run_kernel(const AppendParams a
     __syncthreads();  // all rows are written
     const int j0 = (x.L - n) >> a.shift, j1 = (x.L - 1) >> a.shift;
     float lo[8], hi[8];
-    if (a.shift <= 6) {  // small pages, many of them: one a slice
+    // Small pages, many of them: one a slice; larger ones one a wave.  8 runs of 200 tokens, us: pages of 16 22.4 / 27.3, 32 22.9 / 24.1,
+    // 64 25.2 / 23.2, 512 53.5 / 28.2.
+    if (a.shift <= 5) {
         for (int j = j0 + wave * 8 + slice; j <= j1; j += 8 * W) {
             const int page = x.row[j], rows = min(1 << a.shift, x.L - (j << a.shift));
             if (page < 0 || page >= a.N) continue;
@@ -776,12 +790,17 @@ __global__ __launch_bounds__(64 * W) void append_run_kernel(const AppendParams a
     }
 }
 
+// Runs: one wave where the run is at most its 32 tokens at a time or the waves fill the chip without more of them; else four.  One / four, us, with
+// the call that makes room: 128 workgroups 32 tokens 14.5 / 14.8, 64 17.8 / 15 to 17, 384 65.7 / 29.8; 512 workgroups 64 22.2 / 25.6, 128
+// 34.0 / 29.1; 1024 workgroups 32 19.6 / 40.0, 128 43.4 / 48.8, 384 103 / 112.
 template <typename ST, int D>
 static void append_launch(const AppendParams &a, int B, hipStream_t stream)
 {
     const dim3 grid((unsigned)B, (unsigned)(a.Hkv * (D / 64)));
+    const long groups = (long)B * a.Hkv * (D / 64);
+    const bool one_wave = a.T_new <= 32 || groups >= 1024 || (groups >= 512 && a.T_new <= 64);
     if (a.T_new == 1) append_token_kernel<ST, D><<<grid, 64, 0, stream>>>(a);
-    else if (a.T_new <= 32) append_run_kernel<ST, D, 1><<<grid, 64, 0, stream>>>(a);
+    else if (one_wave) append_run_kernel<ST, D, 1><<<grid, 64, 0, stream>>>(a);
     else append_run_kernel<ST, D, 4><<<grid, 256, 0, stream>>>(a);
 }
 
@@ -864,10 +883,10 @@ int32_t page_pool_fork(const rs_pool *p, int32_t *table, int32_t *len, int32_t *
         return RS_INVALID_ARG;
     const PoolScratch x = scratch(p, ws);
     const PoolView v = view(p, table, len, refs);
-    const bool rows_here = (long)n * p->M <= kRowsHere;
+    const bool here = rows_here(n, p->M);
     pool_fork_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, src, dst, n, (int2 *)pairs_out, (int2 *)carry_out, x.seqs, x.pages,
-                                                                  x.err, rows_here);
-    if (!rows_here) pool_fork_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, src, dst, x.seqs);
+                                                                  x.err, here);
+    if (!here) pool_fork_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, src, dst, x.seqs);
     return launch_status();
 }
 
@@ -879,9 +898,9 @@ int32_t page_pool_free(const rs_pool *p, int32_t *table, int32_t *len, int32_t *
     if (!seq || !aligned16(seq)) return RS_INVALID_ARG;
     const PoolScratch x = scratch(p, ws);
     const PoolView v = view(p, table, len, refs);
-    const bool rows_here = (long)n * p->M <= kRowsHere;
-    pool_free_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, seq, n, x.seqs, x.err, rows_here);
-    if (!rows_here) pool_free_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, seq, x.seqs);
+    const bool here = rows_here(n, p->M);
+    pool_free_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, seq, n, x.seqs, x.err, here);
+    if (!here) pool_free_rows_kernel<<<dim3((unsigned)n, row_groups(p)), 256, 0, (hipStream_t)stream>>>(v, seq, x.seqs);
     return launch_status();
 }
 
@@ -910,7 +929,7 @@ int32_t page_pool_share(const rs_pool *p, const int32_t *table, const int32_t *l
     if (n < 1 || min_pages < 1) return RS_INVALID_ARG;
     if (n > kMaxShared) return RS_UNSUPPORTED;
     const PoolView v = view(p, const_cast<int32_t *>(table), const_cast<int32_t *>(len), nullptr);
-    if ((long)n * p->M <= 4 * kRowsHere) {
+    if (shares_here(n, p->M)) {
         pool_share_kernel<<<1, kMaxShared, 0, (hipStream_t)stream>>>(v, seq, share_out, n, min_pages);
         return launch_status();
     }

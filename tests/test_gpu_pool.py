@@ -120,6 +120,20 @@ def test_refused_as_a_whole(rs):
     assert d.reserve([0, 1], [0, 0])
 
 
+@pytest.mark.parametrize("n,M", [(3, 700), (200, 5), (128, 64), (60, 300), (17, 257)])
+def test_long_lists_and_wide_tables(rs, n, M):
+    d, r = Device(rs, n * 3 + M + 9, 2 * n + 1, M, 16), random.Random(n)
+    assert d.reserve([0], [16 * M - 20])
+    assert d.fork([0] * n, list(range(1, n + 1)))
+    assert d.reserve(list(range(1, n + 1)), [r.randint(0, 20) for _ in range(n)])
+    d.share(list(range(n + 1)), 1)
+    some = r.sample(range(n + 1), n)
+    assert d.fork(some, list(range(n + 1, 2 * n + 1)))
+    d.share([s for i in range(n) for s in (some[i], n + 1 + i)], 2)
+    assert d.free(r.sample(range(2 * n + 1), n))
+    d.compact()
+
+
 def test_share(rs):
     d = Device(rs, 300, 12, 250, 16)
     assert d.reserve([0, 1, 2], [3213, 16 * 5, 7])
@@ -185,6 +199,8 @@ APPEND = [
     (2, 2, 128, 16, 100, [3, 160], [100, 99]),
     (2, 1, 64, 512, 700, [100, 0], None),
     (5, 2, 128, 64, 33, [64, 63, 1, 130, 0], [33, 2, 33, 9, 40]),  # (counts above T_new are cut)
+    (8, 32, 128, 32, 40, list(range(10, 18)), None),               # many heads
+    (16, 32, 128, 64, 70, list(range(50, 66)), [70 - i for i in range(16)]),
 ]
 
 
