@@ -26,8 +26,8 @@
  *     point leaves them zero again when its kernels have finished.  One workspace
  *     must not be used by two calls that can run at the same time.
  *   - Return value: RS_OK or an error code below.  Nothing is printed or thrown.
- *     A kernel-side failure of a bounded wait is recorded in the workspace and
- *     reported by ratsparse_async_status().
+ *     A kernel-side failure of a bounded wait, and a pool's call that cannot be taken, is
+ *     recorded in the workspace and reported by ratsparse_async_status().
  *   - Outputs must not alias inputs, with one exception: rat_scan may run in place
  *     (k_cache == k and v_cache == v) when the two layouts coincide, i.e. t0 == 0 and
  *     T_new == Tcap; every row is read before it is overwritten.
@@ -45,7 +45,9 @@
  *     HIP graph and replayed.  rat_scan, quest_select_decode and sparse_attn_decode (and
  *     their _group forms) hand a fresh call tag to their kernels on every call (it tells this call's
  *     words in the workspace from stale ones) and must be called, not replayed.
- *     rat_decode_step keeps its tag and the sequence length on the device and may be replayed.
+ *     rat_decode_step keeps its tag and the sequence length on the device and may be replayed, and
+ *     so may all calls over a pool of pages (page_pool_*, page_copy, rat_state_copy,
+ *     rat_append_paged, attn_paged): lengths, tables and counts live on the device.
  */
 #ifndef RATSPARSE_H
 #define RATSPARSE_H

@@ -25,6 +25,15 @@
 // lengths alone: each workgroup works it out for itself, by a prefix sum over the list, so lengths live on the device and nothing has to
 // be planned by the host.  What a share holds of a tile goes to one of its two boundary records if the tile goes on in another
 // share, to the row's record if the row has a second part (shared and own), else straight to the output; a second launch joins the records.
+//
+// Measured, us back to back (bfloat16, 32 heads over 8, D 128, pages of 16 unless said; the bytes of K and V that a call cannot do without):
+//   24 sequences of 40 to 9000 tokens: 86, of which the first launch 81 for 444 MB (5.5 TB/s)
+//   32 sequences that share 32768 tokens and have 30 to 1500 of their own: 66.5; first launch 54 (237 MB, of which the shared
+//     134 MB are met by 128 rows a head), join 8.5; 64 that share 4096, 32 heads over 32, pages of 64: 82 (397 MB); 48 in three runs that share
+//     12000, pages of 32: 90 (403 MB)
+//   8 sequences' 150 to 384 new tokens after 16384: 670 to 695 (585 GFLOP, 860 TFLOP/s), join 33 for 100 MB of cut tiles' records
+//   one prompt of 4096 tokens 218 to 238 (576 to 630 TFLOP/s), 32768 9500 (925)
+//   float32, 2 sequences of 600 tokens, 4 heads over 2: 13.5, all of it launches and trips to memory
 #include <type_traits>
 
 #include "check.h"
@@ -43,7 +52,8 @@ constexpr int kManyGroups = 768;       // where all tiles are of many rows: thre
 constexpr int kCus = 256;
 constexpr int kMaxList = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kSlack = 8.f;          // the softmax's reference point moves when the maximum has grown by more (base-2 exponent)
+constexpr float kSlack = 8.f;          // the softmax's reference point moves when the maximum has grown by more (base-2 exponent): weights
+                                       // up to 2^8, as exact in float32 and bfloat16 as those up to 1, and the accumulators are rescaled seldom
 constexpr int kFew = 32, kMany = 128;  // rows of a tile
 
 // keys a wave of a few-row tile takes at a time
@@ -101,7 +111,9 @@ __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 struct Kind {
     bool many;
     int rows, unit;  // log2 of a tile's rows, of a unit's keys
-    int before;      // what beginning and ending a tile costs, in units
+    // what beginning and ending a tile costs, in units; 32768 shared by 32, 4096 by 64, in us: many-row tiles 1 / 2 / 3 units 67.1, 67.4, 68.2 and
+    // 83.9, 83.6, 83.7; few-row 2 / 3 / 4 68.4, 67.4, 70.3 and 83.2, 83.6, 84.2
+    int before;
     // a tile of n units takes n places of its line and those before them; a tile without units none
     __device__ __forceinline__ int places(int n) const { return n > 0 ? n + before : 0; }
     __device__ __forceinline__ int tiles(int r) const { return (int)(((unsigned)r + (1u << rows) - 1) >> rows); }
@@ -225,7 +237,8 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
 }
 
 // How many of the workgroups take many-row tiles: by the bytes of both kinds' keys, a multiple of the eight XCDs, at least eight for
-// each kind that there is.
+// each kind that there is.  A unit of many-row tiles is 128 keys, one of few-row tiles 32; a byte of it is weighted 1.25 for the arithmetic (weights
+// 4 / 5 / 6: 32768 tokens shared by 32 sequences 68.7 / 67.4 / 67.6 us, 4096 by 64 97.1 / 83.6 / 85.1, 12000 in three runs 94.6 / 91.6 / 97.3).
 __device__ __forceinline__ int many_groups(int few_line, int many_line, int groups)
 {
     if (many_line == 0 || few_line == 0) return many_line > 0 ? groups : 0;
@@ -235,7 +248,8 @@ __device__ __forceinline__ int many_groups(int few_line, int many_line, int grou
 // A line's division into shares.  With few places, equal ones, no more than there are places.  Else shares by the eight XCDs, in each those of
 // its first 32 workgroups 11 places for every 9 of the others': two workgroups are on a CU, and the one that came first is served
 // first by its memory path (four sequences of 65536 tokens, 8 heads, with equal shares: every one of the first 256 workgroups done after
-// 131-145 us, every other after 157-171).
+// 131-145 us, every other after 157-171).  10:10 / 11:9 / 12:8, us: 32768 shared by 32 70.3 / 67.4 / 68.0, 4096 by 64 85.9 / 83.6 / 86.3,
+// questions after 16384 766 / 738 / 774.  Where there are three to a CU, 12 for 9 (10:10 / 11:9 / 12:9 / 13:9: 689 / 679 / 672 / 681).
 struct Shares {
     static constexpr int kOlder = 11, kOldest = 12, kNewer = 9;
     int line, n;             // places of a KV head, shares
@@ -549,7 +563,7 @@ __device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &
 // ---- few rows --------------------------------------------------------------------------------------------------
 // 16-wide matrix instructions: lane (l16, lg) = (lane % 16, lane / 16) holds query l16 and, of every 16 keys, 4 lg .. 4 lg + 3.
 // K operand: row l16, 16 bytes at chunk 4 kk + lg, straight from memory (a load touches 64 bytes of each of 16 rows; the lines
-// are used up by the loads beside it).  V operand, bfloat16: transpose reads of the row-major tile, chunks of a row
+// are used up by the loads beside it: streaming 444 MB so, 5.5 TB/s).  V operand, bfloat16: transpose reads of the row-major tile, chunks of a row
 // permuted so that 32 lanes reading two chunks of each of 8 rows touch every bank once; float32: four chunks of each of 4 rows.
 template <typename ST, int D>
 struct FewRows {
