@@ -245,7 +245,10 @@ __device__ __forceinline__ int many_groups(int few_line, int many_line, int grou
     const float many = (float)many_line * 5.f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
     return 8 * max(1, min(kPagedGroups / 8 - 1, (int)(part * (kPagedGroups / 8) + 0.5f)));
 }
-// A line's division into shares.  With few places, equal ones, no more than there are places.  Else shares by the eight XCDs, in each those of
+// A line's division into shares.  With few places, equal ones, of at least a 24th of what an entry of the list has (1 to 8 places): a share more
+// is a record more for the join (at least 1 / 2 / 4 / 8 places, us, 32 heads over 8: one sequence of 8000 tokens 47.2 / 32.6 / 28.0 / 30.9, of 32000
+// 67.4 / 67.0 / 62.9 / 49.0, four of 2000 27.4 / 23.1 / 23.5 / 29.1, two of 600, 4 heads over 2, 13.9 / 14.7 / 16.4 / 20.1; 64 new tokens after
+// 16000 109 / 109 / 84 / 77, 24 each after 600 to 900, 16 heads over 8, float32, 59.7 / 45.5 / 46.6 / 46.7).  Else shares by the eight XCDs, in each those of
 // its first 32 workgroups 11 places for every 9 of the others': two workgroups are on a CU, and the one that came first is served
 // first by its memory path (four sequences of 65536 tokens, 8 heads, with equal shares: every one of the first 256 workgroups done after
 // 131-145 us, every other after 157-171).  10:10 / 11:9 / 12:8, us: 32768 shared by 32 70.3 / 67.4 / 68.0, 4096 by 64 85.9 / 83.6 / 86.3,
@@ -259,8 +262,8 @@ struct Shares {
     long all;
     double unit;             // places for each unit of weight
     // reciprocals: a division of integers, or one in 64 bits, costs the beginning of every launch as much as 30 other instructions
-    float per_unit;          // of unit; equal shares: of a share's places
-    float per_xcd, per_sum;  // of of_xcd, of sum
+    float per_unit;          // of unit
+    float per_xcd, per_sum;  // of of_xcd, of sum; equal shares: of each, of each + 1
     Shares() = default;
     __device__ __forceinline__ Shares(const Plan &pl, int B, int Hkv, int all_groups, bool MANY)
     {
@@ -282,11 +285,13 @@ struct Shares {
             unit = (double)all * (double)(0.125f * per_sum);  // (off by 2^-22 of it: begin() rounds a whole number back up)
             per_unit = (float)(8 * sum) * __builtin_amdgcn_rcpf((float)all);
         } else {
-            n = (int)min((long)n, all);
+            const int least = max(1, min(8, (int)((float)line * __builtin_amdgcn_rcpf(24.f * (float)B))));
+            n = min(n, quotient((int)all + least - 1, __builtin_amdgcn_rcpf((float)least)));
             if (n > 0) {
                 each = (int)all / n;
                 more = (int)all - each * n;
-                per_unit = (float)n * __builtin_amdgcn_rcpf((float)all);
+                per_xcd = __builtin_amdgcn_rcpf((float)each);
+                per_sum = __builtin_amdgcn_rcpf((float)(each + 1));
             }
         }
     }
@@ -303,7 +308,8 @@ struct Shares {
     {
         int w;
         if (sum == 0) {
-            w = (int)((float)place * per_unit);
+            const int longer = more * (each + 1), p = (int)place;
+            w = p < longer ? quotient(p, per_sum) : more + quotient(p - longer, per_xcd);
         } else {
             const int at = (int)((float)place * per_unit), x = quotient(at, per_sum), r = at - x * sum;
             w = x * of_xcd + (r < older * weight ? (weight == kOldest ? r / kOldest : r / kOlder) : older + (r - older * weight) / kNewer);
@@ -1337,9 +1343,10 @@ static void paged_launch(const PagedParams &a, hipStream_t stream)
     if (sizeof(ST) == 2 && a.own_many) paged_attend_kernel<ST, D, sizeof(ST) == 2><<<a.groups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
     else paged_attend_kernel<ST, D, false><<<a.groups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
     const long rows = (long)a.B * a.Hq * a.T;
+    // (workgroups a cut few-row tile 1 / 2 / 4, us: 24 tokens each after 600 to 900 52.1 / 45.2 / 42.8, 100 each after 2000 to 3000 315 / 319 / 328)
     if (a.entries) paged_join_rows_kernel<ST, D><<<(unsigned)(rows < 8192 ? rows : 8192), 64, 0, stream>>>(a);
     else if (sizeof(ST) == 2) paged_join_cuts_kernel<ST, D, true><<<dim3((unsigned)a.groups, 4), kPagedThreads, 0, stream>>>(a);
-    else paged_join_cuts_kernel<ST, D, false><<<kPagedGroups * kPagedWaves, kPagedThreads, 0, stream>>>(a);
+    else paged_join_cuts_kernel<ST, D, false><<<dim3(kPagedGroups * kPagedWaves, 2), kPagedThreads, 0, stream>>>(a);
 }
 
 }  // namespace rs
