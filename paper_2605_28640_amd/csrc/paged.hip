@@ -245,8 +245,10 @@ __device__ __forceinline__ int many_groups(int few_line, int many_line, int grou
     const float many = (float)many_line * 5.f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
     return 8 * max(1, min(kPagedGroups / 8 - 1, (int)(part * (kPagedGroups / 8) + 0.5f)));
 }
-// A line's division into shares.  With few places, equal ones, of at least a 24th of what an entry of the list has (1 to 8 places): a share more
-// is a record more for the join (at least 1 / 2 / 4 / 8 places, us, 32 heads over 8: one sequence of 8000 tokens 47.2 / 32.6 / 28.0 / 30.9, of 32000
+// A line's division into shares.  With few places, equal ones, of at least a 24th of what an entry of the list has (1 to 8 places; a sixth of many rows', whose
+// records are four times as large: a 24th / 12th / sixth / third, 32 heads over 8, 64 tokens each after 600 to 900 45.4 / 46.0 / 41.0 / 46.6, 19 each
+// after 1376 shared ones 36.1 / 36.2 / 33.5 / 37.9): a share more
+// is a record more for the join (at least 1 / 2 / 4 / 8 places, us: one sequence of 8000 tokens 47.2 / 32.6 / 28.0 / 30.9, of 32000
 // 67.4 / 67.0 / 62.9 / 49.0, four of 2000 27.4 / 23.1 / 23.5 / 29.1, two of 600, 4 heads over 2, 13.9 / 14.7 / 16.4 / 20.1; 64 new tokens after
 // 16000 109 / 109 / 84 / 77, 24 each after 600 to 900, 16 heads over 8, float32, 59.7 / 45.5 / 46.6 / 46.7).  Else shares by the eight XCDs, in each those of
 // its first 32 workgroups 11 places for every 9 of the others': two workgroups are on a CU, and the one that came first is served
@@ -285,7 +287,7 @@ struct Shares {
             unit = (double)all * (double)(0.125f * per_sum);  // (off by 2^-22 of it: begin() rounds a whole number back up)
             per_unit = (float)(8 * sum) * __builtin_amdgcn_rcpf((float)all);
         } else {
-            const int least = max(1, min(8, (int)((float)line * __builtin_amdgcn_rcpf(24.f * (float)B))));
+            const int least = max(1, min(8, (int)((float)line * __builtin_amdgcn_rcpf((MANY ? 6.f : 24.f) * (float)B))));
             n = min(n, quotient((int)all + least - 1, __builtin_amdgcn_rcpf((float)least)));
             if (n > 0) {
                 each = (int)all / n;
