@@ -44,6 +44,25 @@ __device__ __forceinline__ int block_scan_i(int v, int *tot, int &total)
     return before + inc - v;
 }
 
+// The same of values whose sum may pass 32 bits (a call may ask for 2^27 pages 1024 times): 16 bits and the rest of each side by side.  What
+// precedes a value is right wherever it fits 32 bits itself.
+__device__ __forceinline__ int block_scan_wide(int v, int2 *tot, long &total)
+{
+    const int wave = threadIdx.x >> 6, low = v & 0xffff, high = v >> 16, l = wave_scan_i(low), h = wave_scan_i(high);
+    if (lane_id() == kWave - 1) tot[wave] = make_int2(l, h);
+    __syncthreads();
+    int2 before = make_int2(l - low, h - high), sum = make_int2(0, 0);
+#pragma unroll
+    for (int w = 0; w < kPoolThreads / kWave; ++w) {
+        const int2 x = tot[w];
+        if (w < wave) before.x += x.x, before.y += x.y;
+        sum.x += x.x, sum.y += x.y;
+    }
+    __syncthreads();
+    total = sum.x + ((long)sum.y << 16);
+    return (int)((uint32_t)before.x + ((uint32_t)before.y << 16));
+}
+
 // The free pages, ascending, to list, `most` of them; returns how many were found (more perhaps, fewer if there are no more).  Called by
 // the whole workgroup.
 __device__ __forceinline__ int free_pages(const int32_t *refs, int N, int most, int *tot, int32_t *list)
@@ -102,6 +121,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_reserve_kernel(PoolView p, 
 {
     __shared__ uint32_t seen[kMaxSeqs / 32];
     __shared__ int tot[kPoolThreads / kWave];
+    __shared__ int2 wide[kPoolThreads / kWave];
     const int tid = threadIdx.x;
     seen[tid] = 0u;
     __syncthreads();
@@ -120,11 +140,19 @@ __global__ __launch_bounds__(kPoolThreads) void pool_reserve_kernel(PoolView p, 
                 else need = pages_of(L + t, p.shift) - pages_of(L, p.shift);
             }
         }
-        int total;
-        const int at = block_scan_i(need, tot, total);
-        if (i < n) offs[i] = (int)needed + at;
+        // (more than N, or all of it: the same refusal; the wide sum costs every call 0.2 us)
+        long total;
+        int at;
+        if (p.N < (1 << 21) - 1) {
+            int sum;
+            at = block_scan_i(min(need, p.N + 1), tot, sum);
+            total = sum;
+        } else {
+            at = block_scan_wide(need, wide, total);
+        }
+        if (i < n) offs[i] = (int)needed + at;  // (no more than N, or nobody looks at it)
         needed += total;
-        if (needed > p.N) bad = true;  // (and the sum stays far from the end of its range)
+        if (needed > p.N) bad = true;
         if (__syncthreads_or(bad)) break;
     }
     bad = __syncthreads_or(bad);

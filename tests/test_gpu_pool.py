@@ -358,3 +358,60 @@ def test_plain_and_other_arguments_make_the_same_call(rs):
                     lambda: rs.attn_paged(s, d.p, x.to(torch.bfloat16), k, v, d.table, d.len, ints([1]), None, 1, None, 0.0, out, lse, d.ws)):
             with pytest.raises(rs.RatsparseError):
                 bad()
+
+
+@pytest.mark.parametrize("N", [(1 << 21) - 2, (1 << 21) - 1, 1 << 22])
+@pytest.mark.parametrize("S,M,n,want", [(128, 1 << 24, 128, 16 << 24),                # 2^31 pages together: negative as 32 bits
+                                        (256, 1 << 24, 256, 16 << 24),                # 2^32: nothing
+                                        (1024, (1 << 22) + 1, 1024, 16 * ((1 << 22) + 1)),  # 2^32 + 1024: few
+                                        (1024, 1 << 21, 1024, 16 << 21),              # each no more than there may be pages
+                                        (1100, 1 << 22, 1100, (16 << 22) - 15)])      # over two turns of a workgroup's threads
+def test_more_pages_asked_for_than_32_bits_count(rs, N, S, M, n, want):
+    """Refused as a whole, like any call that asks for more than there is.  (The table is not looked at: it may hold anything.)"""
+    p = rs.make_pool(N, S, M, 16)
+    table = torch.empty(S, M, dtype=torch.int32, device="cuda")
+    length, refs = ints([0] * S), torch.zeros(N, dtype=torch.int32, device="cuda")
+    ws = rs.Workspace(rs.page_pool_workspace_bytes(p))
+    granted, seq = ints([7] * n), torch.arange(n, dtype=torch.int32, device="cuda")
+    for each in (None, torch.full((n,), want, dtype=torch.int32, device="cuda")):
+        rs.page_pool_reserve(p, table, length, refs, seq, each, want, granted, ws)
+        with pytest.raises(rs.RatsparseError, match="status 7"):
+            ws.async_status()
+        assert not length.any() and not refs.any() and not granted.any()
+        granted.fill_(7)
+    del table  # (up to 18 GB)
+    torch.cuda.empty_cache()
+
+
+def test_all_pages_at_once(rs):
+    """The most that can be given, over more than one turn of the threads."""
+    N, S = 5000, 1030
+    d = Device(rs, N, S, 5, 16)
+    want = [80] * 900 + [0] * 30 + [60, 64] * 50
+    assert sum(-(-w // 16) for w in want) == 4900
+    assert d.reserve(list(range(S)), want)
+    assert not d.reserve(list(range(900, 921)), [80] * 20 + [1])
+    assert d.reserve(list(range(900, 920)), [80] * 20) and d.m.free_pages() == []
+
+
+def test_room_in_a_pool_of_many_pages(rs):
+    """Sums formed in two halves, of needs on both sides of 2^16: every sequence gets the next pages in order."""
+    N, S, M = (1 << 21) + 77, 40, 70000
+    p = rs.make_pool(N, S, M, 16)
+    table, length, refs = torch.full((S, M), -1, dtype=torch.int32, device="cuda"), ints([0] * S), torch.zeros(N, dtype=torch.int32, device="cuda")
+    ws = rs.Workspace(rs.page_pool_workspace_bytes(p))
+    need = [65535, 65536, 65537, 1, 0, 69999] + [50001 + 17 * i for i in range(34)]
+    want = [max(0, 16 * n - 3) for n in need]
+    granted, seq = ints([0] * S), list(reversed(range(S)))
+    rs.page_pool_reserve(p, table, length, refs, ints(seq), ints(want), 1, granted, ws)
+    ws.async_status()
+    at = 0
+    for s, n, w in zip(seq, need, want):
+        assert torch.equal(table[s, :n], torch.arange(at, at + n, dtype=torch.int32, device="cuda")) and table[s, n:].eq(-1).all()
+        at += n
+    assert refs[:at].eq(1).all() and not refs[at:].any() and granted.tolist() == want and length.tolist() == want[::-1]
+    assert at + 69998 <= N < at + 2 * 69998
+    rs.page_pool_reserve(p, table, length, refs, ints([35, 36]), ints([16 * 69998] * 2), 1, None, ws)  # (one of them could be taken)
+    with pytest.raises(rs.RatsparseError, match="status 7"):
+        ws.async_status()
+    assert not refs[at:].any()
