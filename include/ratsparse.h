@@ -97,7 +97,7 @@ int32_t ratsparse_workspace_init(void *ws, size_t ws_bytes, void *stream);
 
 /* Waits for `stream`, then returns RS_OK, or RS_ASYNC_TIMEOUT if a kernel that used
  * `ws` gave up a bounded wait (its outputs are then undefined), or RS_POOL_REFUSED if a page_pool call
- * that used it changed nothing; clears the record. */
+ * that used it changed nothing (RS_ASYNC_TIMEOUT where both happened); clears the record. */
 int32_t ratsparse_async_status(void *ws, void *stream);
 
 /* Measurement aid (no part of the method): enqueue a plain streaming read of `bytes` bytes at

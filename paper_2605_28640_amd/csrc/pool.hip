@@ -19,6 +19,12 @@ constexpr int kMaxSeqs = 32768;      // a bit of LDS each
 constexpr int kMaxShared = 1024;     // sequences of one page_pool_share call: a thread each
 constexpr uint32_t kErrPages = 2u;   // the asynchronous error word of a refused call
 
+// by one thread of a refused call; an expired wait that is on record already says more: outputs of an earlier call are undefined
+__device__ __forceinline__ void put_refusal(uint32_t *err)
+{
+    if (*err == 0u) *err = kErrPages;
+}
+
 struct PoolView {
     int32_t *table, *len, *refs;
     int N, S, M, shift;  // shift: log2 of the page size
@@ -163,7 +169,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_reserve_kernel(PoolView p, 
     if (bad) {
         if (granted)
             for (int i = tid; i < n; i += kPoolThreads) granted[i] = 0;
-        if (tid == 0) *err = kErrPages;
+        if (tid == 0) put_refusal(err);
         return;
     }
     for (int r = tid; r < total; r += kPoolThreads) {
@@ -257,7 +263,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_fork_kernel(PoolView p, con
         pairs[i] = pr;
         if (carry) carry[i] = cr;
     }
-    if (bad && tid == 0) *err = kErrPages;
+    if (bad && tid == 0) put_refusal(err);
     if (!here || bad) return;
     __syncthreads();
     for (int i = tid >> 6; i < n; i += kPoolThreads / kWave) fork_row(p, src[i], dst[i], full[i], lane_id(), kWave);
@@ -288,7 +294,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_free_kernel(PoolView p, con
         held[i] = bad ? 0 : pages_of(p.len[seq[i]], p.shift);
         if (!bad) p.len[seq[i]] = 0;
     }
-    if (bad && tid == 0) *err = kErrPages;
+    if (bad && tid == 0) put_refusal(err);
     if (!here || bad) return;
     __syncthreads();
     for (int i = tid >> 6; i < n; i += kPoolThreads / kWave) free_row(p, seq[i], held[i], lane_id(), kWave);

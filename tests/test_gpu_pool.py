@@ -415,3 +415,22 @@ def test_room_in_a_pool_of_many_pages(rs):
     with pytest.raises(rs.RatsparseError, match="status 7"):
         ws.async_status()
     assert not refs[at:].any()
+
+
+def test_a_refusal_leaves_an_expired_wait_on_record(rs):
+    """One workspace for a scan, whose wait expired (1 in the first word), and a call on the pool that is refused after it."""
+    d = Device(rs, 10, 4, 6, 16)
+    word = d.ws.buf[:4].view(torch.int32)
+    calls = (lambda: rs.page_pool_reserve(*d.state(), ints([9]), None, 1, None, d.ws),
+             lambda: rs.page_pool_fork(*d.state(), ints([9]), ints([1]), ints([[5, 5]]), None, d.ws),
+             lambda: rs.page_pool_free(*d.state(), ints([9]), d.ws))
+    for call in calls:
+        word.fill_(1)
+        call()
+        with pytest.raises(rs.RatsparseError, match="status 5"):
+            d.ws.async_status()
+        d.ws.async_status()
+        call(), call()
+        with pytest.raises(rs.RatsparseError, match="status 7"):
+            d.ws.async_status()
+        d.ws.async_status()
