@@ -645,7 +645,7 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
     bool real[RT];
     long row[RT];
     int last[RT];                 // the last position the row sees (-1: there is no such row)
-    int first_last = 0x7fffffff;  // the smallest of the tile's rows
+    int first_last = 0x7fffffff;  // the smallest of the tile's rows (what comes of rows that do not exist is dropped)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         int bq, t, g;
@@ -661,12 +661,12 @@ __device__ __forceinline__ void attend_few(const PagedParams &a, const Plan &pl,
             const f32x4 x = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const char *>((const ST *)a.q + row[rt] * D) + 64 * kk + 16 * lg);
             qf[rt][kk] = real[rt] ? x : f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        first_last = min(first_last, last[rt]);
+        if (real[rt]) first_last = min(first_last, last[rt]);
     }
 #pragma unroll
     for (int m = 1; m < 16; m <<= 1) first_last = min(first_last, __shfl_xor(first_last, m, kWave));
     first_last = __builtin_amdgcn_readfirstlane(first_last);
-    if (w.shared) first_last = 0x7fffffff;  // every row sees all of it (what comes of rows that do not exist is dropped)
+    if (w.shared || first_last >= w.limit - 1) first_last = 0x7fffffff;  // every row sees all keys there are
 
     f32x4 oacc[RT][NDT];
     float m[RT], l[RT];
@@ -863,7 +863,7 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
         const f32x4 x = *reinterpret_cast<const f32x4 *>((const bf16 *)a.q + row * D + 16 * c + 8 * h);
         qf[c] = __builtin_bit_cast(bf16x8, real ? x : f32x4{0.f, 0.f, 0.f, 0.f});
     }
-    int first_last = last, wave_last = last;  // the smallest and the largest of the wave's rows
+    int first_last = real ? last : 0x7fffffff, wave_last = last;  // the smallest and the largest of the wave's rows
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
         first_last = min(first_last, __shfl_xor(first_last, x, kWave));
@@ -872,8 +872,9 @@ __device__ __forceinline__ void attend_many(const PagedParams &a, const Plan &pl
     first_last = __builtin_amdgcn_readfirstlane(first_last);
     wave_last = __builtin_amdgcn_readfirstlane(wave_last);
     if (w.shared) first_last = 0x7fffffff, wave_last = wave_last >= 0 ? 0x7fffffff : -1;
-    // the smallest of the tile's rows (later positions are later rows of it)
-    const int tile_first = w.shared ? 0x7fffffff : pl.seq[w.b].L - pl.seq[w.b].n + w.rt * kMany / a.G;
+    // the smallest of the tile's rows (later positions are later rows of it); as far as there are keys that it does not see
+    int tile_first = pl.seq[w.b].L - pl.seq[w.b].n + w.rt * kMany / a.G;
+    if (w.shared || tile_first >= w.limit - 1) tile_first = 0x7fffffff;
     bool odd = false;  // values that are not finite where some row may not look
 
     // operand addresses inside a tile: K row lq, chunk 2 c + h; V through the transpose read, lane = 32 h + 16 dg + L supplying 8 bytes of row

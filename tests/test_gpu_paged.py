@@ -473,3 +473,26 @@ def test_a_workspace_used_for_other_calls_in_between(rs, case):
         torch.cuda.synchronize()
         for (o, l), (wo, wl) in zip(outs, want):
             assert torch.equal(o, wo) and torch.equal(l, wl), rep
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,T", [(4, 1, 1), (8, 1, 1), (2, 2, 1), (20, 1, 1), (40, 1, 1), (4, 1, 3)])
+def test_values_that_every_row_sees(rs, Hq, Hkv, T, dtype):
+    """Rows of V without a number that all of a tile's rows see: their channels are not numbers, and nothing else changes by a bit (no
+    row is taken key by key for them).  Rows of a tile that do not exist are not rows that see less."""
+    say("visible", Hq, Hkv, T, dtype)
+    for bad in (float("nan"), float("inf")):
+        b = Batch(rs, Hq, Hkv, 128, 16, [45, 200, 64, 1500], (), 0, T, None, dtype, seed=17)
+        clean, lse = b.run()
+        for i, at in ((0, [3, 45 - T]), (1, [0, 100, 200 - T]), (2, [64 - T]), (3, [640, 1500 - T])):
+            if T > 1:  # far from the new tokens, whose steps some rows do not see to their end
+                at = [x for x in at if x < b.m.len[i] - 64]
+            b.v[:, b.m.rows(i)[at], 5::32] = bad
+        out, l2 = b.run()
+        assert torch.equal(l2, lse)
+        odd = torch.zeros(128, dtype=torch.bool, device="cuda")
+        odd[5::32] = True
+        assert torch.equal(out[..., ~odd], clean[..., ~odd])
+        for i in range(4):
+            if T == 1 or i in (1, 3):
+                assert torch.isnan(out[i][..., odd]).all() if math.isnan(bad) else torch.isposinf(out[i][..., odd]).all()
