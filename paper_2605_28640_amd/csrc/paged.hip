@@ -237,13 +237,16 @@ __device__ __forceinline__ void make_plan(const PagedParams &a, const Plan &pl)
 }
 
 // How many of the workgroups take many-row tiles: by the bytes of both kinds' keys, a multiple of the eight XCDs, at least eight for
-// each kind that there is.  A unit of many-row tiles is 128 keys, one of few-row tiles 32; a byte of it is weighted 1.25 for the arithmetic (weights
-// 4 / 5 / 6: 32768 tokens shared by 32 sequences 68.7 / 67.4 / 67.6 us, 4096 by 64 97.1 / 83.6 / 85.1, 12000 in three runs 94.6 / 91.6 / 97.3).
+// each kind that there is.  A unit of many-row tiles is 128 keys, one of few-row tiles 32; a byte of it is weighted 1.3 for the arithmetic (units
+// weighted 5 / 5.25 / 5.5: 32768 tokens shared by 32 sequences 61 us each, 4096 by 64, 32 heads of 64, 60.8 / 54.0 / 54.0, 12000 in three runs
+// 80.7 / 80.5 / 83.5).  An even number to an XCD, whose two halves then lie alike, the first on CUs by themselves, the second beside the first:
+// odd numbers leave CUs with one of each kind.  38 / 39 / 40 / 41 of 64, 32768 tokens by 32: 61.3 / 65.3 / 61.5 / 63.7; 30 / 31 / 32 / 33, 16384 by 16
+// 42.0 / 47.1 / 42.7 / 47.8; 17 / 18 / 19 / 20, 8192 by 9 with 2000 to 4000 of their own 45.4 / 42.3 / 45.2 / 43.0; 11 / 12, 4096 by 64, 32 heads, 83.3 / 78.0.
 __device__ __forceinline__ int many_groups(int few_line, int many_line, int groups)
 {
     if (many_line == 0 || few_line == 0) return many_line > 0 ? groups : 0;
-    const float many = (float)many_line * 5.f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
-    return 8 * max(1, min(kPagedGroups / 8 - 1, (int)(part * (kPagedGroups / 8) + 0.5f)));
+    const float many = (float)many_line * 5.25f, part = many / (many + (float)few_line);  // (in bfloat16's units: both kinds exist only there)
+    return 8 * max(1, min(kPagedGroups / 8 - 1, 2 * (int)(part * (kPagedGroups / 16) + 0.5f)));
 }
 // A line's division into shares.  With few places, equal ones, of at least a 24th of what an entry of the list has (1 to 8 places; a sixth of many rows', whose
 // records are four times as large: a 24th / 12th / sixth / third, 32 heads over 8, 64 tokens each after 600 to 900 45.4 / 46.0 / 41.0 / 46.6, 19 each
