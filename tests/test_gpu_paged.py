@@ -496,3 +496,99 @@ def test_values_that_every_row_sees(rs, Hq, Hkv, T, dtype):
         for i in range(4):
             if T == 1 or i in (1, 3):
                 assert torch.isnan(out[i][..., odd]).all() if math.isnan(bad) else torch.isposinf(out[i][..., odd]).all()
+
+
+def places(dtype, G, Hkv, P, lens, T, counts, run, shared):
+    """How a call's work is divided, counted on the host: for each kind of tile (few rows, many rows) the places of its line over all KV
+    heads, and the shares it is cut into where it is long.  One run of `run` sequences from the first on, `shared` tokens."""
+    bf = dtype == "bf16"
+    counts = [T] * len(lens) if counts is None else counts
+    rows, unit, before = {False: 32, True: 128}, {False: 32 if bf else 16, True: 128}, {False: 3, True: 2}
+    line = {False: 0, True: 0}
+    own_many, together = bf and T * G > 32, T * G < (128 if bf else 32)
+    shared = shared // P * P if together and run > 1 else 0
+    for b, (L, n) in enumerate(zip(lens, counts)):
+        k0 = shared if b < run else 0
+        for t0 in range(0, n * G, rows[own_many]):
+            keys = L - n + min(n - 1, (t0 + rows[own_many] - 1) // G) + 1 - k0
+            line[own_many] += -(-keys // unit[own_many]) + before[own_many] if keys > 0 else 0
+    if shared:
+        many = bf and run * T * G > 32
+        line[many] += -(-run * T * G // rows[many]) * (-(-shared // unit[many]) + before[many])
+    groups = 768 if own_many and len(lens) <= 112 else 512
+    if line[False] and line[True]:
+        part = 5.25 * line[True] / (5.25 * line[True] + line[False])
+        taken = 8 * max(1, min(63, 2 * int(part * 32 + 0.5)))
+    else:
+        taken = groups if line[True] else 0
+    return (line[False] * Hkv, (groups - taken) * 4), (line[True] * Hkv, taken)
+
+
+LONG = [
+    # Hq, Hkv, D, P, lens, run, shared, T, counts, keys of a share at least (few rows, many rows; 0: no such line)
+    (16, 8, 64, 16, [9000, 17000, 7001, 300, 9500], 2, 7000, 1, None, (64, 0)),         # one token each, a run whose rows are few
+    (16, 8, 64, 16, [24016 + 40 * b for b in range(24)], 24, 24000, 1, None, (64, 512)),  # a long prompt's rows are many, the rest few
+    (4, 4, 64, 512, [600000], 0, 0, 1, None, (1100, 0)),                                # more entries of the table to a share than a wave lists at once
+    (32, 32, 64, 16, [20000, 3000], 0, 0, 300, [300, 120], (0, 1100)),                  # several tiles of 128 rows; three workgroups a CU
+    (16, 16, 64, 16, [24010 + 190 * b for b in range(8)], 8, 24000, 40, None, (0, 512)),  # more new tokens than a small tile's rows, over a shared prompt
+    (4, 4, 64, 16, [420 + b for b in range(120)], 0, 0, 33, None, (0, 512)),            # a list for which two workgroups fit a CU
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_lines_cut_into_long_shares(rs, case, dtype):
+    """Four places of a line and more to a share: shares are weighted by which workgroup came first.  Rows at the ends of tiles, of the first and
+    the last KV head, of every sequence."""
+    Hq, Hkv, D, P, lens, run, shared, T, counts, least = LONG[case]
+    say("long", case, dtype)
+    dt, G, B = tdtype(dtype), Hq // Hkv, len(lens)
+    lines = places(dtype, G, Hkv, P, lens, T, counts, run, shared)
+    summed = 0  # terms that a sum takes one after the other: the keys of a share (twice the mean is more than the weights give), then the shares
+    for (all_places, shares), keys, unit in zip(lines, least, (32 if dtype == "bf16" else 16, 128)):
+        if dtype == "bf16":
+            assert (all_places > 0) == (keys > 0)
+        if all_places:
+            assert all_places >= 4 * shares and all_places * unit >= (keys if dtype == "bf16" else 0) * shares
+            summed += 2 * all_places * unit // shares + -(-shares // Hkv)
+    M = -(-max(lens) // P)
+    m = Pool(sum(-(-x // P) for x in lens) - max(0, run - 1) * (shared // P) + 5, B, M, P)
+    r, gen = np.random.default_rng(case), torch.Generator(device="cuda").manual_seed(case)
+    pages = r.permutation(m.N).tolist()
+    first = [pages.pop() for _ in range(shared // P)]
+    for b in range(B):
+        m.len[b] = lens[b]
+        row = first[:] if b < run else []
+        row += [pages.pop() for _ in range(-(-lens[b] // P) - len(row))]
+        m.table[b][:len(row)] = row
+    k, v = (torch.randn(Hkv, m.N * P, D, device="cuda", generator=gen).to(dt) for _ in range(2))
+    q = torch.randn(B, Hq, T, D, device="cuda", generator=gen).to(dt)
+    share = [[0, run, shared // P] if b < run else [b, 1, 0] for b in range(B)]
+    s, p = rs.make_shape(B, Hq, Hkv, D, m.N * P, P, dt), rs.make_pool(m.N, B, M, P)
+    ws = rs.Workspace(rs.attn_paged_workspace_bytes(s, p, T))
+    args = (s, p, q, k, v, ints(m.table), ints(m.len), ints(list(range(B))), ints(counts) if counts else None, T, ints(share), 1 / math.sqrt(D))
+    got = []
+    for _ in range(2):
+        out, lse = torch.full((B, Hq, T, D), 7.0, device="cuda", dtype=dt), torch.full((B, Hq, T), 7.0, device="cuda")
+        rs.attn_paged(*args, out, lse, ws)
+        torch.cuda.synchronize()
+        got.append((out, lse))
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+    bf, e, worst = dtype == "bf16", 2.0 ** -24, 0.0
+    for b in range(B):
+        rows, L, n = m.rows(b), lens[b], counts[b] if counts else T
+        terms = min(L, summed) + 16
+        some = sorted({t for x in (0, 31, 32, 127, 128, 255, 256, n * G - 1) for t in (x // G,) if t < n})
+        assert out[b, :, n:].eq(7.0).all() and lse[b, :, n:].eq(7.0).all()
+        for h in sorted({0, G - 1, Hq - 1}):
+            kk, vv = (x[h // G, torch.from_numpy(rows).cuda()].float().cpu().numpy() for x in (k, v))
+            o, z = (x[b, h, some].float().cpu().numpy() for x in (out, lse))
+            want, lw, mag, big = attention(q[b, h, some].float().cpu().numpy(), kk, vv, [L - n + t for t in some], args[-1])
+            # as in Batch.check, but for the sums
+            delta = 2 * ((D + 4) * e * big + 4 * e * (1 + np.abs(lw)))
+            tol = mag * (2 * delta[:, None] + terms * e + (2.0 ** -8 if bf else 0)) * 1.01
+            tol = tol + (2.0 ** -8 * (np.abs(want) + tol) if bf else 0) + 1e-30
+            assert np.all(np.abs(o - want) <= tol), (b, h, float((np.abs(o - want) / tol).max()))
+            assert np.all(np.abs(z - lw) <= delta + terms * e + 2 * e * np.abs(lw)), (b, h)
+            worst = max(worst, float((np.abs(o - want) / tol).max()))
+    say("  of the tolerance: %.3f" % worst)
