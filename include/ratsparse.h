@@ -367,7 +367,8 @@ int32_t snapkv_compress_lse(const rs_shape *s, const void *q_win, const void *k_
  * page_pool_reserve, _fork and _free are decided as a whole on the device: if one entry cannot be taken (a
  * sequence out of range or listed twice, more tokens than M pages hold, too few free pages) nothing at all
  * changes, and ratsparse_async_status() answers RS_POOL_REFUSED.  None keeps state on the host: all calls of this
- * section may be captured into a graph and replayed. */
+ * section may be captured into a graph and replayed.  Heads: Hq <= 8160, whatever the length of the list (elsewhere
+ * B Hq <= 8160). */
 typedef struct rs_pool {
     int32_t N; /* pages of the pool; N P < 2^31 */
     int32_t S; /* sequences (rows of the table), at most 32768 */
@@ -435,7 +436,7 @@ int32_t rat_state_copy(const rs_shape *s, float *state_k, float *state_v, int32_
  *   meta: every page that gets a row has its bounds formed anew from its rows so far (they need not have been current
  *         before), or NULL
  *   n_new [B] int32 or NULL: T_new for each; counts above T_new are taken as T_new, below 0 as 0
- * Nothing is done for a sequence out of range, listed before, or with fewer than n_new tokens; rows whose table entry names
+ * B <= 32768.  Nothing is done for a sequence out of range, listed before, or with fewer than n_new tokens; rows whose table entry names
  * no page are not written.  Long prompts are better scanned as contiguous rows (rat_scan) and copied into their pages. */
 int32_t rat_append_paged(const rs_shape *s, const rs_pool *p, const void *k, const void *v, const float *g, float *state_k,
                          float *state_v, void *k_pool, void *v_pool, void *meta, const int32_t *table, const int32_t *len,

@@ -1330,7 +1330,7 @@ static PagedLayout paged_layout(const rs_shape *s, int T_new)
 
 static int check_paged(const rs_shape *s, const rs_pool *p, int T_new)
 {
-    int st = check_shape(s, true);
+    int st = check_rows(s, true);
     if (st == RS_OK) st = check_pool(p);
     if (st != RS_OK) return st;
     if (p->P != s->P || (long)p->N * p->P != s->Tcap || T_new < 1) return RS_INVALID_ARG;

@@ -975,8 +975,8 @@ int32_t page_pool_share(const rs_pool *p, const int32_t *table, const int32_t *l
 int32_t page_copy(const rs_shape *s_src, const void *k_src, const void *v_src, const void *meta_src, const rs_shape *s_dst, void *k_dst,
                   void *v_dst, void *meta_dst, const int32_t *pairs, int32_t n, const int32_t *n_pairs, void *stream)
 {
-    int st = check_shape(s_src, true);
-    if (st == RS_OK) st = check_shape(s_dst, true);
+    int st = check_rows(s_src, true);
+    if (st == RS_OK) st = check_rows(s_dst, true);
     if (st != RS_OK) return st;
     if (s_src->Hkv != s_dst->Hkv || s_src->D != s_dst->D || s_src->P != s_dst->P || s_src->dtype != s_dst->dtype) return RS_INVALID_ARG;
     if (!k_src || !v_src || !k_dst || !v_dst || !pairs || (meta_src == nullptr) != (meta_dst == nullptr)) return RS_INVALID_ARG;
@@ -996,7 +996,7 @@ int32_t page_copy(const rs_shape *s_src, const void *k_src, const void *v_src, c
 
 int32_t rat_state_copy(const rs_shape *s, float *state_k, float *state_v, int32_t S, const int32_t *pairs, int32_t n, void *stream)
 {
-    const int st = check_shape(s, false);
+    const int st = check_rows(s, false);
     if (st != RS_OK) return st;
     if (!state_k || !state_v || !pairs || !aligned16(state_k) || !aligned16(state_v) || !aligned16(pairs) || n < 1 || S < 1) return RS_INVALID_ARG;
     const int row4 = s->Hkv * s->D / 4;
@@ -1009,10 +1009,11 @@ int32_t rat_append_paged(const rs_shape *s, const rs_pool *p, const void *k, con
                          void *k_pool, void *v_pool, void *meta, const int32_t *table, const int32_t *len, const int32_t *seq,
                          const int32_t *n_new, int32_t T_new, void *stream)
 {
-    int st = check_shape(s, true);
+    int st = check_rows(s, true);
     if (st == RS_OK) st = check_pool(p);
     if (st != RS_OK) return st;
     if (p->P != s->P || (long)p->N * p->P != s->Tcap || T_new < 1) return RS_INVALID_ARG;
+    if (s->B > kMaxSeqs) return RS_UNSUPPORTED;
     if (!k || !v || !g || !state_k || !state_v || !k_pool || !v_pool || !table || !len || !seq) return RS_INVALID_ARG;
     for (const void *x : {k, v, (const void *)g, (const void *)state_k, (const void *)state_v, (const void *)k_pool, (const void *)v_pool,
                           (const void *)meta, (const void *)table, (const void *)len, (const void *)seq, (const void *)n_new})

@@ -592,3 +592,11 @@ def test_lines_cut_into_long_shares(rs, case, dtype):
             assert np.all(np.abs(z - lw) <= delta + terms * e + 2 * e * np.abs(lw)), (b, h)
             worst = max(worst, float((np.abs(o - want) / tol).max()))
     say("  of the tolerance: %.3f" % worst)
+
+
+def test_more_listed_heads_than_the_contiguous_calls_take(rs):
+    """B Hq past 8160, which limits calls whose heads have control words of a workspace."""
+    r = np.random.default_rng(4)
+    lens = [33 + int(x) for x in r.integers(0, 40, 300)]
+    b = Batch(rs, 32, 8, 64, 16, lens, (5, 200), 32, 1, None, "bf16", seed=21)
+    b.check(*b.run(), heads=[0, 31])

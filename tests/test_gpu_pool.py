@@ -434,3 +434,20 @@ def test_a_refusal_leaves_an_expired_wait_on_record(rs):
         with pytest.raises(rs.RatsparseError, match="status 7"):
             d.ws.async_status()
         d.ws.async_status()
+
+
+def test_more_listed_heads_than_the_contiguous_calls_take(rs):
+    """B Hq is limited where a head has control words of a workspace; these calls have none.  rat_append_paged, page_copy, rat_state_copy."""
+    B, Hq, Hkv, D, P, dt = 700, 16, 2, 64, 16, torch.float32
+    d = Device(rs, B, B, 2, P)
+    assert d.reserve(list(range(B)), [1] * B)
+    s = rs.make_shape(B, Hq, Hkv, D, B * P, P, dt)
+    k, v = torch.randn(B, Hkv, 1, D, device="cuda"), torch.randn(B, Hkv, 1, D, device="cuda")
+    sk, sv = torch.zeros(B, Hkv, D, device="cuda"), torch.zeros(B, Hkv, D, device="cuda")
+    kp, vp = torch.zeros(Hkv, B * P, D, device="cuda"), torch.zeros(Hkv, B * P, D, device="cuda")
+    rs.rat_append_paged(s, d.p, k, v, torch.zeros_like(k), sk, sv, kp, vp, None, d.table, d.len, ints(list(range(B))), None, 1)
+    assert torch.equal(sk, k[:, :, 0]) and torch.equal(kp[:, ::P], k[:, :, 0].transpose(0, 1)) and torch.equal(vp[:, ::P], v[:, :, 0].transpose(0, 1))
+    rs.page_copy(s, kp, vp, None, s, kp, vp, None, ints([[3, 699]]), None)
+    assert torch.equal(kp[:, 699 * P:], kp[:, 3 * P:4 * P])
+    rs.rat_state_copy(s, sk, sv, ints([[3, 699]]))
+    assert torch.equal(sk[699], sk[3])

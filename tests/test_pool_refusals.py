@@ -158,3 +158,21 @@ def test_signatures(name, names):
     for wrong in (n - 1, n + 1):
         with pytest.raises(TypeError):
             fast(*[None] * wrong)
+
+
+def test_listed_heads_are_not_limited_by_control_words():
+    """A list of 1024 sequences is taken whatever the heads; a contiguous call's B Hq is limited."""
+    lib, p = rs.load(), _pool()
+    s = ctypes.byref(rs.make_shape(1024, 64, 8, 64, 256, 16, BF))
+    assert lib.attn_paged_workspace_bytes(s, p, 1) > 0 and lib.sparse_attn_decode_workspace_bytes(s, 256, 4) == 0
+    need = lib.attn_paged_workspace_bytes(s, p, 1)
+    assert lib.attn_paged(s, p, A, A, A, A, A, A, None, 1, None, 0.1, A, None, A, need - 1, None) == 3
+    assert lib.page_copy(s, A, A, None, s, A, A, None, A, 0, None, None) == 1 and lib.rat_state_copy(s, A, A, 4, A, 0, None) == 1
+    assert lib.rat_append_paged(s, p, A, A, A, A, A, A, A, None, A, A, A, None, 0, None) == 1
+    # more heads than a sequence may have
+    wide = ctypes.byref(rs.make_shape(1, 8161, 8161, 128, 256, 16, BF))
+    assert lib.rat_append_paged(wide, p, A, A, A, A, A, A, A, None, A, A, A, None, 1, None) == 2
+    assert lib.attn_paged_workspace_bytes(wide, p, 1) == 0 and lib.page_copy(wide, A, A, None, wide, A, A, None, A, 1, None, None) == 2
+    assert lib.rat_state_copy(wide, A, A, 4, A, 1, None) == 2
+    longer = ctypes.byref(rs.make_shape(32769, 2, 2, 64, 256, 16, BF))
+    assert lib.rat_append_paged(longer, p, A, A, A, A, A, A, A, None, A, A, A, None, 1, None) == 2
