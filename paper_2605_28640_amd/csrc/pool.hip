@@ -949,7 +949,7 @@ int32_t page_pool_compact(const rs_pool *p, int32_t *table, int32_t *len, int32_
     pool_compact_kernel<<<1, kPoolThreads, 0, (hipStream_t)stream>>>(v, x.pages, x.pages2, x.pages3, x.word, (int2 *)pairs_out, n_pairs_out);
     const long cells = (long)p->S * p->M;
     const unsigned groups = (unsigned)(cells >= 2048l * 256 ? 2048 : (cells + 255) / 256);
-    pool_renumber_kernel<<<groups, 256, 0, (hipStream_t)stream>>>(v, x.pages, x.word, (int2 *)pairs_out, n_pairs_out, p->N / 2);
+    pool_renumber_kernel<<<groups, 256, 0, (hipStream_t)stream>>>(v, x.pages, x.word, (int2 *)pairs_out, n_pairs_out, p->N > 1 ? p->N / 2 : 1);
     return launch_status();
 }
 

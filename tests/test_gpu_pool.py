@@ -451,3 +451,14 @@ def test_more_listed_heads_than_the_contiguous_calls_take(rs):
     assert torch.equal(kp[:, 699 * P:], kp[:, 3 * P:4 * P])
     rs.rat_state_copy(s, sk, sv, ints([[3, 699]]))
     assert torch.equal(sk[699], sk[3])
+
+
+def test_compaction_of_a_pool_of_one_page(rs):
+    """Nothing can move: the list's one entry says so, for a copy that goes without the number of pairs."""
+    d = Device(rs, 1, 1, 1, 16)
+    for room in (0, 3):
+        assert d.reserve([0], [room])
+        pairs, n = ints([[0, 0]]), ints([9])
+        rs.page_pool_compact(*d.state(), pairs, n, d.ws)
+        assert d.m.compact() == [] and n.item() == 0 and pairs.tolist() == [[-1, -1]]
+        d.check("compact")
