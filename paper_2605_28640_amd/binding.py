@@ -330,6 +330,16 @@ def _need(t, dtype, *shape):
     return p
 
 
+def _scratch(ws):
+    """Address and size of a workspace; one that shows its buffer has to have it on the current device."""
+    buf = getattr(ws, "buf", None)
+    if buf is not None:
+        _ptr(buf)
+        if buf.get_device() != torch.cuda.current_device():
+            raise RatsparseError("the workspace has to be on the current device")
+    return ws.ptr, ws.nbytes
+
+
 def _sequences(p, table, len, refs):
     return (_need(table, torch.int32, p.S, p.M), _need(len, torch.int32, p.S), _need(refs, torch.int32, p.N))
 
@@ -349,7 +359,7 @@ def page_pool_reserve(p, table, len, refs, seq, want, T_new, granted, ws):
         return
     n = seq.numel()
     _check(load().page_pool_reserve(ctypes.byref(p), *_sequences(p, table, len, refs), _need(seq, torch.int32, n), n,
-                                    _need(want, torch.int32, n), T_new, _need(granted, torch.int32, n), ws.ptr, ws.nbytes,
+                                    _need(want, torch.int32, n), T_new, _need(granted, torch.int32, n), *_scratch(ws),
                                     _stream()))
 
 
@@ -359,15 +369,14 @@ def page_pool_fork(p, table, len, refs, src, dst, pairs_out, carry_out, ws):
     n = src.numel()
     _check(load().page_pool_fork(ctypes.byref(p), *_sequences(p, table, len, refs), _need(src, torch.int32, n),
                                  _need(dst, torch.int32, n), n, _need(pairs_out, torch.int32, n, 2),
-                                 _need(carry_out, torch.int32, n, 2), ws.ptr, ws.nbytes, _stream()))
+                                 _need(carry_out, torch.int32, n, 2), *_scratch(ws), _stream()))
 
 
 def page_pool_free(p, table, len, refs, seq, ws):
     if _calls().page_pool_free(p, table, len, refs, seq, ws):
         return
     n = seq.numel()
-    _check(load().page_pool_free(ctypes.byref(p), *_sequences(p, table, len, refs), _need(seq, torch.int32, n), n, ws.ptr,
-                                 ws.nbytes, _stream()))
+    _check(load().page_pool_free(ctypes.byref(p), *_sequences(p, table, len, refs), _need(seq, torch.int32, n), n, *_scratch(ws), _stream()))
 
 
 def page_pool_compact(p, table, len, refs, pairs_out, n_pairs_out, ws):
@@ -375,7 +384,7 @@ def page_pool_compact(p, table, len, refs, pairs_out, n_pairs_out, ws):
         return
     _check(load().page_pool_compact(ctypes.byref(p), *_sequences(p, table, len, refs),
                                     _need(pairs_out, torch.int32, max(p.N // 2, 1), 2), _need(n_pairs_out, torch.int32, 1),
-                                    ws.ptr, ws.nbytes, _stream()))
+                                    *_scratch(ws), _stream()))
 
 
 def page_pool_share(p, table, len, seq, min_pages, share_out):
@@ -432,4 +441,4 @@ def attn_paged(s, p, q, k_pool, v_pool, table, len, seq, n_new, T_new, share, sc
     _check(load().attn_paged(ctypes.byref(s), ctypes.byref(p), _need(q, dt, *rows, s.D), kp, vp, _need(table, torch.int32, p.S, p.M),
                              _need(len, torch.int32, p.S), _need(seq, torch.int32, s.B), _need(n_new, torch.int32, s.B), T_new,
                              _need(share, torch.int32, s.B, 3), scale, _need(out, dt, *rows, s.D),
-                             _need(lse_out, torch.float32, *rows), ws.ptr, ws.nbytes, _stream()))
+                             _need(lse_out, torch.float32, *rows), *_scratch(ws), _stream()))

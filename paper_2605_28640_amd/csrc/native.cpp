@@ -116,7 +116,7 @@ struct Args {
     }
     rs_shape shape(int i) { return structure<rs_shape>(i, g_shape); }
     rs_pool pool(int i) { return structure<rs_pool>(i, g_pool); }
-    // a workspace's buffer
+    // a workspace's buffer, on the device of the typed tensors before it
     void *workspace(int i, size_t &bytes)
     {
         bytes = 0;
@@ -126,8 +126,13 @@ struct Args {
         if (buf && THPVariable_CheckExact(buf)) {
             try {
                 const at::Tensor &t = THPVariable_Unpack(buf);
-                p = t.data_ptr();
-                bytes = (size_t)t.numel();
+                const int d = (int)t.get_device();
+                if (!t.is_cuda() || (device >= 0 && d != device)) {
+                    refuse();
+                } else {
+                    p = t.data_ptr();
+                    bytes = (size_t)t.numel();
+                }
             } catch (const std::exception &) {
                 refuse();
             }

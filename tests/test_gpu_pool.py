@@ -462,3 +462,19 @@ def test_compaction_of_a_pool_of_one_page(rs):
         rs.page_pool_compact(*d.state(), pairs, n, d.ws)
         assert d.m.compact() == [] and n.item() == 0 and pairs.tolist() == [[-1, -1]]
         d.check("compact")
+
+
+def test_a_workspace_that_is_not_on_the_device(rs):
+    """Refused before anything is enqueued, by every call over a pool that takes one."""
+    d, one, pairs = Device(rs, 10, 4, 6, 16), ints([0]), ints([[0, 0]] * 5)
+    d.ws.buf = d.ws.buf.cpu()
+    s = rs.make_shape(1, 1, 1, 64, 160, 16, torch.float32)
+    x, rows = torch.zeros(1, 1, 1, 64, device="cuda"), torch.zeros(1, 160, 64, device="cuda")
+    for call in (lambda: rs.page_pool_reserve(*d.state(), one, None, 1, None, d.ws),
+                 lambda: rs.page_pool_fork(*d.state(), one, one, pairs[:1], None, d.ws),
+                 lambda: rs.page_pool_free(*d.state(), one, d.ws),
+                 lambda: rs.page_pool_compact(*d.state(), pairs, one.clone(), d.ws),
+                 lambda: rs.attn_paged(s, d.p, x, rows, rows, d.table, d.len, one, None, 1, None, 0.1, x.clone(), None, d.ws)):
+        with pytest.raises(AssertionError):
+            call()
+    assert not d.len.any() and not d.refs.any()

@@ -176,3 +176,10 @@ def test_listed_heads_are_not_limited_by_control_words():
     assert lib.rat_state_copy(wide, A, A, 4, A, 1, None) == 2
     longer = ctypes.byref(rs.make_shape(32769, 2, 2, 64, 256, 16, BF))
     assert lib.rat_append_paged(longer, p, A, A, A, A, A, A, A, None, A, A, A, None, 1, None) == 2
+
+
+def test_a_workspace_that_is_not_on_the_device():
+    ws = rs.Workspace.__new__(rs.Workspace)
+    ws.buf = torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(AssertionError):
+        rs._scratch(ws)
