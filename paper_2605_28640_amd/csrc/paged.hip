@@ -561,7 +561,8 @@ __device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &
 #pragma unroll
             for (int j = 0; j < 4; ++j) z = fmaf(q[j], to_f32(((const ST *)a.k)[at + j]), z);
             z = group_sum<C4>(z) * cs;
-            const float top = fmaxf(m, z), f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), p = z == top ? 1.f : __builtin_amdgcn_exp2f(z - top);
+            const float top = fmaxf(m, z), bias = top == -INFINITY ? 0.f : top;  // (infinities as the products' way has them)
+            const float f = __builtin_amdgcn_exp2f(m - bias), p = __builtin_amdgcn_exp2f(z - bias);
             m = top;
             l = l * f + p;
 #pragma unroll

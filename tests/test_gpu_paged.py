@@ -600,3 +600,24 @@ def test_more_listed_heads_than_the_contiguous_calls_take(rs):
     lens = [33 + int(x) for x in r.integers(0, 40, 300)]
     b = Batch(rs, 32, 8, 64, 16, lens, (5, 200), 32, 1, None, "bf16", seed=21)
     b.check(*b.run(), heads=[0, 31])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_without_a_number_where_a_tile_goes_key_by_key(rs, dtype):
+    """Keys of infinities that rows see, in a tile whose last value no other row may look at: rows get what they get without that value."""
+    b = Batch(rs, 4, 2, 64, 16, [45, 60, 50], (), 0, 20, None, dtype, seed=23)
+    b.q[..., 0] = b.q[..., 0].abs() + 0.5
+    b.k[:, b.m.rows(0)[30], 0] = float("inf")   # seen by the rows from position 30 on, of 25 to 44: no numbers
+    b.k[:, b.m.rows(1)[50], 0] = float("-inf")  # counts for nothing
+    b.k[:, b.m.rows(2)[:45], 0] = float("-inf")  # rows of positions 30 to 44 see nothing else
+    plain, lse = b.run()
+    for i in range(3):
+        b.v[:, int(b.m.rows(i)[-1]), 3] = float("nan")
+    out, l2 = b.run()
+    for o, z in ((plain, lse), (out, l2)):
+        assert torch.isfinite(o[0, :, :5]).all() and torch.isnan(o[0, :, 5:-1]).all() and torch.isnan(z[0, :, 5:-1]).all()
+        assert torch.isfinite(o[1, :, :-1]).all() and torch.isfinite(z[1, :, :-1]).all()
+        assert o[2, :, :15].eq(0).all() and torch.isneginf(z[2, :, :15]).all() and torch.isfinite(o[2, :, 15:-1]).all()
+    # as in test_values_that_a_row_does_not_see
+    for i, rows in ((0, slice(0, 5)), (1, slice(0, 19)), (2, slice(15, 19))):
+        assert (out[i, :, rows].float() - plain[i, :, rows].float()).abs().max() <= 4 * 2.0 ** -8 * b.v[:, b.m.rows(i)[:-1]].float().abs().max()
