@@ -14,8 +14,8 @@
 //   many rows (tiles of 128; bfloat16): bound by the matrix units.  A workgroup: every wave takes 32 rows, all four go through the same
 //     keys, K and V tiles in a ring of LDS slots, one barrier a step.  Where a sequence's own rows fill more than a small tile, all tiles of
 //     the call are of this kind, and a kernel with nothing else in it takes three workgroups to a CU (168 registers, three
-//     slots of 16 KB filled two steps ahead) instead of two (four slots, three steps): eight prompts' questions of 150 to 384 tokens after 16384, 32
-//     heads over 8, 670 us against 731; one prompt of 32768 tokens 9.5 ms against 10.6 (929 TFLOP/s).
+//     slots of 16 KB filled two steps ahead) instead of two (four slots, three steps): when it was chosen, eight prompts' questions of 150 to 384 tokens
+//     after 16384, 32 heads over 8, 670 us against 731; one prompt of 32768 tokens 9.5 ms against 10.6.
 // In both S^T = K Q^T and O^T = V^T P^T, so that a lane holds the keys of one query and P^T goes from the accumulators into the
 // second product as it is.
 //
@@ -26,14 +26,17 @@
 // be planned by the host.  What a share holds of a tile goes to one of its two boundary records if the tile goes on in another
 // share, to the row's record if the row has a second part (shared and own), else straight to the output; a second launch joins the records.
 //
-// Measured, us back to back (bfloat16, 32 heads over 8, D 128, pages of 16 unless said; the bytes of K and V that a call cannot do without):
-//   24 sequences of 40 to 9000 tokens: 86, of which the first launch 81 for 444 MB (5.5 TB/s)
-//   32 sequences that share 32768 tokens and have 30 to 1500 of their own: 66.5; first launch 54 (237 MB, of which the shared
-//     134 MB are met by 128 rows a head), join 8.5; 64 that share 4096, 32 heads over 32, pages of 64: 82 (397 MB); 48 in three runs that share
-//     12000, pages of 32: 90 (403 MB)
-//   8 sequences' 150 to 384 new tokens after 16384: 670 to 695 (585 GFLOP, 860 TFLOP/s), join 33 for 100 MB of cut tiles' records
-//   one prompt of 4096 tokens 218 to 238 (576 to 630 TFLOP/s), 32768 9500 (925)
-//   float32, 2 sequences of 600 tokens, 4 heads over 2: 13.5, all of it launches and trips to memory
+// Measured, us back to back on a card at work (bfloat16, 32 heads over 8, D 128, pages of 16 unless said; the bytes of K and V that a call cannot
+// do without; by counters, what came from beyond the L2 caches):
+//   24 sequences of 40 to 9000 tokens: 82, of which the first launch 76 for 446 MB (449 fetched, 5.9 TB/s)
+//   32 sequences that share 32768 tokens and have 30 to 1500 of their own: 65; first launch 56 (237 MB, of which the shared
+//     134 MB are met by 128 rows a head; 239 fetched), join 9; 64 that share 4096, 32 heads over 32, pages of 64: 79 (397 MB); 48 in three runs
+//     that share 12000, pages of 32: 86.5 (403 MB)
+//   8 sequences' 150 to 384 new tokens after 16384: 655 (585 GFLOP, 890 TFLOP/s), join 31 for 100 MB of cut tiles' records; matrix units busy
+//     47 % of the cycles at 1.95 to 1.97 GHz, half of the L2's requests miss (2.6 GB fetched for 80 MB of K and V).  From an idle card the first dozen calls take up
+//     to 890, the clock not being what it is later
+//   one prompt of 4096 tokens 189 to 195 (705 to 727 TFLOP/s), 32768 9300 (946)
+//   one sequence of 8000 tokens 21, four of 2000 19.5; float32, 2 sequences of 600 tokens, 4 heads over 2: 13.5, all of it launches and trips to memory
 #include <type_traits>
 
 #include "check.h"
@@ -111,8 +114,8 @@ __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
 struct Kind {
     bool many;
     int rows, unit;  // log2 of a tile's rows, of a unit's keys
-    // what beginning and ending a tile costs, in units; 32768 shared by 32, 4096 by 64, in us: many-row tiles 1 / 2 / 3 units 67.1, 67.4, 68.2 and
-    // 83.9, 83.6, 83.7; few-row 2 / 3 / 4 68.4, 67.4, 70.3 and 83.2, 83.6, 84.2
+    // what beginning and ending a tile costs, in units; 32768 shared by 32, 4096 by 64, in us: many-row tiles 1 / 2 / 3 units 61.4, 61.6, 61.7 and
+    // 77.5, 78.2, 78.4; few-row 2 / 3 / 4 62.3, 61.6, 61.7 and 78.2 each
     int before;
     // a tile of n units takes n places of its line and those before them; a tile without units none
     __device__ __forceinline__ int places(int n) const { return n > 0 ? n + before : 0; }
@@ -249,15 +252,16 @@ __device__ __forceinline__ int many_groups(int few_line, int many_line, int grou
     return 8 * max(1, min(kPagedGroups / 8 - 1, 2 * (int)(part * (kPagedGroups / 16) + 0.5f)));
 }
 // A line's division into shares.  With few places, equal ones, of at least a 24th of what an entry of the list has (1 to 8 places; a sixth of many rows', whose
-// records are four times as large: a 24th / 12th / sixth / third, 32 heads over 8, 64 tokens each after 600 to 900 45.4 / 46.0 / 41.0 / 46.6, 19 each
-// after 1376 shared ones 36.1 / 36.2 / 33.5 / 37.9): a share more
-// is a record more for the join (at least 1 / 2 / 4 / 8 places, us: one sequence of 8000 tokens 47.2 / 32.6 / 28.0 / 30.9, of 32000
-// 67.4 / 67.0 / 62.9 / 49.0, four of 2000 27.4 / 23.1 / 23.5 / 29.1, two of 600, 4 heads over 2, 13.9 / 14.7 / 16.4 / 20.1; 64 new tokens after
-// 16000 109 / 109 / 84 / 77, 24 each after 600 to 900, 16 heads over 8, float32, 59.7 / 45.5 / 46.6 / 46.7).  Else shares by the eight XCDs, in each those of
-// its first 32 workgroups 11 places for every 9 of the others': two workgroups are on a CU, and the one that came first is served
+// records are four times as large: a 24th / 12th / sixth / third, 32 heads over 8, 64 tokens each after 600 to 900 52.3 / 52.2 / 45.8 / 47.7, 19 each
+// after 1376 shared ones 35.1 / 35.1 / 35.3 / 32.3): a share more
+// is a record more for the join (at least 1 / 2 / 4 / 8 places, us: one sequence of 8000 tokens 44.5 / 28.5 / 22.0 / 21.1, of 32000
+// 62.8 / 62.8 / 58.8 / 43.8, four of 2000 24.4 / 19.8 / 18.2 / 19.3, eight of 2000 to 3000 with 4 new tokens each 32.5 / 32.5 / 29.2 / 27.0, two of 600, 4 heads
+// over 2, 13.4 / 13.3 / 13.9 / 17.5; 24 new tokens each after 600 to 900, 16 heads over 8, float32, 62.3 / 62.1 / 50.9 / 58.1).  Else shares by the eight
+// XCDs, in each those of its first 32 workgroups 11 places for every 9 of the others': two workgroups are on a CU, and the one that came first is served
 // first by its memory path (four sequences of 65536 tokens, 8 heads, with equal shares: every one of the first 256 workgroups done after
-// 131-145 us, every other after 157-171).  10:10 / 11:9 / 12:8, us: 32768 shared by 32 70.3 / 67.4 / 68.0, 4096 by 64 85.9 / 83.6 / 86.3,
-// questions after 16384 766 / 738 / 774.  Where there are three to a CU, 12 for 9 (10:10 / 11:9 / 12:9 / 13:9: 689 / 679 / 672 / 681).
+// 131-145 us, every other after 157-171).  10:10 / 11:9 / 12:8, us: 32768 shared by 32 60.3 / 61.6 / 63.6, 4096 by 64 78.4 / 78.2 / 78.5,
+// 12000 in three runs 80.0 / 78.5 / 78.3, 24 of 40 to 3000, 32 heads, 107.0 / 105.2 / 105.2.  Where there are three to a CU, 12 for 9 (questions after
+// 16384, 9:9 / 11:9 / 12:9 / 13:9: 663 / 662 / 647 / 662).
 struct Shares {
     static constexpr int kOlder = 11, kOldest = 12, kNewer = 9;
     int line, n;             // places of a KV head, shares
@@ -575,7 +579,7 @@ __device__ __forceinline__ void attend_by_key(const PagedParams &a, const Plan &
 // ---- few rows --------------------------------------------------------------------------------------------------
 // 16-wide matrix instructions: lane (l16, lg) = (lane % 16, lane / 16) holds query l16 and, of every 16 keys, 4 lg .. 4 lg + 3.
 // K operand: row l16, 16 bytes at chunk 4 kk + lg, straight from memory (a load touches 64 bytes of each of 16 rows; the lines
-// are used up by the loads beside it: streaming 444 MB so, 5.5 TB/s).  V operand, bfloat16: transpose reads of the row-major tile, chunks of a row
+// are used up by the loads beside it: streaming 446 MB so, 5.9 TB/s).  V operand, bfloat16: transpose reads of the row-major tile, chunks of a row
 // permuted so that 32 lanes reading two chunks of each of 8 rows touch every bank once; float32: four chunks of each of 4 rows.
 template <typename ST, int D>
 struct FewRows {
@@ -1350,7 +1354,8 @@ static void paged_launch(const PagedParams &a, hipStream_t stream)
     if (sizeof(ST) == 2 && a.own_many) paged_attend_kernel<ST, D, sizeof(ST) == 2><<<a.groups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
     else paged_attend_kernel<ST, D, false><<<a.groups, kPagedThreads, plan_bytes(a.B), stream>>>(a);
     const long rows = (long)a.B * a.Hq * a.T;
-    // (workgroups a cut few-row tile 1 / 2 / 4, us: 24 tokens each after 600 to 900 52.1 / 45.2 / 42.8, 100 each after 2000 to 3000 315 / 319 / 328)
+    // (workgroups a cut few-row tile 1 / 2 / 4, float32, 16 heads over 8, us: 24 tokens each of 4 after 600 to 900 51.9 / 45.4 / 43.7, of 8 59.2 / 53.3 / 53.7,
+    // 100 each of 8 after 2000 to 3000 195 / 195 / 204)
     if (a.entries) paged_join_rows_kernel<ST, D><<<(unsigned)(rows < 8192 ? rows : 8192), 64, 0, stream>>>(a);
     else if (sizeof(ST) == 2) paged_join_cuts_kernel<ST, D, true><<<dim3((unsigned)a.groups, 4), kPagedThreads, 0, stream>>>(a);
     else paged_join_cuts_kernel<ST, D, false><<<dim3(kPagedGroups * kPagedWaves, 2), kPagedThreads, 0, stream>>>(a);
