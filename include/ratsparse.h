@@ -451,7 +451,8 @@ int32_t rat_append_paged(const rs_shape *s, const rs_pool *p, const void *k, con
  *   share [B, 3] int32 or NULL: as page_pool_share writes it for the same list: a run's common pages are read once for all its
  *       sequences.  Its values are taken on trust in one respect: the first sequence's pages are used for the
  *       whole run.  A table entry that names no page hides its tokens.
- * B <= 1024.  Workspace: attn_paged_workspace_bytes().  Results do not depend on the order in which workgroups finish. */
+ * B <= 1024, B Hq T_new <= 2e9, and the work that list, T_new and M P could mean is counted in 32 bits (one token each: B M P
+ * below about 5e9 tokens; RS_UNSUPPORTED above).  Workspace: attn_paged_workspace_bytes().  Results do not depend on the order in which workgroups finish. */
 size_t attn_paged_workspace_bytes(const rs_shape *s, const rs_pool *p, int32_t T_new);
 int32_t attn_paged(const rs_shape *s, const rs_pool *p, const void *q, const void *k_pool, const void *v_pool, const int32_t *table,
                    const int32_t *len, const int32_t *seq, const int32_t *n_new, int32_t T_new, const int32_t *share, float scale,

@@ -532,6 +532,8 @@ LONG = [
     (32, 32, 64, 16, [20000, 3000], 0, 0, 300, [300, 120], (0, 1100)),                  # several tiles of 128 rows; three workgroups a CU
     (16, 16, 64, 16, [24010 + 190 * b for b in range(8)], 8, 24000, 40, None, (0, 512)),  # more new tokens than a small tile's rows, over a shared prompt
     (4, 4, 64, 16, [420 + b for b in range(120)], 0, 0, 33, None, (0, 512)),            # a list for which two workgroups fit a CU
+    (16, 8, 64, 16, [60001 + b % 7 for b in range(24)], 24, 60000, 1, None, (300, 512)),  # nearly all CUs for the rows that are many
+    (16, 8, 64, 16, [5000 + 200 * b for b in range(24)], 24, 256, 1, None, (512, 512)),   # nearly none
 ]
 
 
