@@ -458,6 +458,80 @@ int32_t attn_paged(const rs_shape *s, const rs_pool *p, const void *q, const voi
                    const int32_t *len, const int32_t *seq, const int32_t *n_new, int32_t T_new, const int32_t *share, float scale,
                    void *out, float *lse_out, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- A cache in 4 bits -----------------------------------------------------------------
+ * Not in the paper; offered for caches that are to be a quarter as large as in bfloat16.  32 neighbouring channels of a row share a power of
+ * two; a channel is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign:
+ *   k4, v4             [B, Hkv, Tcap, D/2]  uint8   two channels a byte, the lower one in the low half; 0 .. 7 in the order above, 8 more with the sign
+ *   k4_scale, v4_scale [B, Hkv, Tcap, D/32] uint8   the exponent + 127 (2 .. 252); 255: the group's values are NaN
+ * 68 bytes a row of 128 channels, 34 of 64.  The values are bfloat16 numbers exactly.  A shape's dtype is that of queries, results, page bounds
+ * and of rows that go in or come out.
+ * Every sequence has a length of its own, in device memory (the library only reads it, but for cache_evict and kv4_evict):
+ *   len [B] int32   tokens of the sequence, rows 0 .. len - 1; values above Tcap are taken as Tcap, below 0 as 0
+ * All calls of this section and the next may be captured into a graph and replayed.  They take B Hkv <= 65535 and Tcap <= 2^30
+ * (RS_UNSUPPORTED above), the attention B <= 1024; Hq <= 8160. */
+
+/* The last n_new[b] tokens of sequence b (positions len - n_new .. len - 1) go into the cache.
+ *   k, v  [B, Hkv, T_src, D] dtype   the i-th of them is row t_src + i (a staging buffer or a whole cache, as rat_scan leaves it);
+ *                                    rows past n_new[b] are not read.  0 <= t_src, t_src + T_new <= T_src, T_new <= Tcap
+ *   n_new [B] int32 or NULL: T_new for each; counts above T_new are taken as T_new, below 0 as 0; more than len: none
+ *   meta  [B, Hkv, Tcap/P, 2, D] dtype or NULL: every page that gets a row has its Quest bounds formed anew from the stored values of its rows
+ *         so far, as quest_page_meta does for a cache of dtype; a NaN is passed over
+ * A group takes the smallest power of two with at most 7 of it in its largest magnitude; values are rounded to nearest, ties to the even
+ * number of the list, and above 6 to 6.  A group that holds an infinity or NaN is stored as NaN.  Where a row is stored twice the same, its bytes are the same. */
+int32_t kv4_append(const rs_shape *s, const void *k, const void *v, int64_t T_src, int64_t t_src, const int32_t *len, const int32_t *n_new,
+                   int32_t T_new, uint8_t *k4, uint8_t *k4_scale, uint8_t *v4, uint8_t *v4_scale, void *meta, void *stream);
+
+/* The bounds alone, of every page that holds one of the last n_new[b] tokens (T_new = Tcap, n_new = len: of all; after a kv4_evict). */
+int32_t kv4_page_meta(const rs_shape *s, const uint8_t *k4, const uint8_t *k4_scale, const int32_t *len, const int32_t *n_new, int32_t T_new, void *meta,
+                      void *stream);
+
+/* Rows as the values that they stand for: k_out, v_out [B, Hkv, T, D] dtype, row i: token t0 + i, or, with t0 < 0, token len + t0 + i (t0 = -T: the
+ * last T tokens).  Rows of tokens that a sequence does not have are left as they were.  -Tcap <= t0 < Tcap. */
+int32_t kv4_fetch(const rs_shape *s, const uint8_t *k4, const uint8_t *k4_scale, const uint8_t *v4, const uint8_t *v4_scale, const int32_t *len,
+                  int64_t t0, int32_t T, void *k_out, void *v_out, void *stream);
+
+/* Attention of one token over the cache (Eq. 4): q [B, Hq, D] dtype over the tokens t < len[b], all of them or those of listed pages.
+ *   idx     [B, H_idx, K] int32 or NULL (all tokens): pages, as quest_select_decode (H_idx = Hq) or quest_select_decode_group (H_idx = Hkv) list
+ *           them; entries that name no page are skipped, each page at most once.  H_idx and K count for nothing without it
+ *   tally   [B, Hkv, Tcap] float32 or NULL (and with idx NULL): see attn_decode_tally
+ *   out     [B, Hq, D] dtype, lse_out [B, Hq] float32 or NULL.  A row that sees nothing, or only scores of -inf, gets zeros and a
+ *           log-sum-exp of -inf
+ * The weights are rounded to bfloat16 for the product with bfloat16 results (half a step of 2^-8 each), and kept in float32 for float32 ones.
+ * The order of every sum follows from the lengths: the same call gives the same bits. */
+size_t kv4_attn_decode_workspace_bytes(const rs_shape *s, int32_t H_idx, int32_t K, int32_t with_tally);
+int32_t kv4_attn_decode(const rs_shape *s, const void *q, const uint8_t *k4, const uint8_t *k4_scale, const uint8_t *v4, const uint8_t *v4_scale,
+                        const int32_t *len, float scale, const int32_t *idx, int32_t H_idx, int32_t K, float *tally, int32_t n_fresh, void *out,
+                        float *lse_out, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- Caches that give up rows while they are decoded ---------------------------------------
+ * Not in the paper, whose cache compression (SnapKV) happens once, after the prompt.  Here every row's weight is counted step by step, and a
+ * sequence that outgrows its budget keeps the rows that have had most of it.
+ *
+ * Attention of one token over all rows, as sparse_attn_decode without a list, for sequences of len[b] tokens (see above), with the tally:
+ *   tally [B, Hkv, Tcap] float32, in/out:  tally[b, h, t] += sum over the query heads of KV head h of their attention weight of row t, t < len[b].
+ *         Rows len - n_fresh .. len - 1 are new since the last call: theirs is set, not added to (n_fresh = 1 in a decode loop).  Rows
+ *         from len on are left as they were.  A prompt's tally may start from zeros or from votes_out of snapkv_compress.
+ * float32 caches are attended in float32 throughout, of bfloat16 ones as kv4_attn_decode says. */
+size_t attn_decode_tally_workspace_bytes(const rs_shape *s);
+int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache, const void *v_cache, const int32_t *len, float scale, float *tally,
+                          int32_t n_fresh, void *out, float *lse_out, void *ws, size_t ws_bytes, void *stream);
+
+/* Every sequence with more than n_keep + n_slack tokens keeps n_keep rows of each KV head: the tokens at positions below n_first and the last
+ * n_recent ones, and of the others those with the largest tally (the lower row first among equal ones; NaN counts as the smallest).
+ * Rows that stay and lie before n_keep stay where they are; those behind it move, in order, to the places of the dropped ones before it, with
+ * their tally and position; len becomes n_keep.  Rows from n_keep on, and sequences within their budget, are left as they were.  From then on
+ * rows are not in the order of their positions, which attention does not ask for.
+ *   pos  [B, Hkv, Tcap] int32, in/out: position of the token in each row;  mark [B, 2] int32, in/out: the rows whose position is on record, the tokens
+ *        that the sequence has had.  Zero mark (only it) when a sequence begins: rows that come after those on record get the positions
+ *        that follow, and pos is written only here.
+ *   1 <= n_keep <= Tcap; n_first + n_recent <= n_keep
+ * Quest bounds of a cache that has given up rows are formed anew (quest_page_meta, kv4_page_meta). */
+size_t cache_evict_workspace_bytes(const rs_shape *s, int32_t n_keep);
+int32_t cache_evict(const rs_shape *s, void *k_cache, void *v_cache, float *tally, int32_t *pos, int32_t *mark, int32_t *len, int32_t n_keep, int32_t n_first,
+                    int32_t n_recent, int32_t n_slack, void *ws, size_t ws_bytes, void *stream);
+int32_t kv4_evict(const rs_shape *s, uint8_t *k4, uint8_t *k4_scale, uint8_t *v4, uint8_t *v4_scale, float *tally, int32_t *pos, int32_t *mark, int32_t *len,
+                  int32_t n_keep, int32_t n_first, int32_t n_recent, int32_t n_slack, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

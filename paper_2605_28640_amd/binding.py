@@ -86,6 +86,16 @@ SIGNATURES = {
     "rat_append_paged": (_i32, [_shp, _pool, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp]),
     "attn_paged_workspace_bytes": (_sz, [_shp, _pool, _i32]),
     "attn_paged": (_i32, [_shp, _pool, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _f32, _vp, _vp, _vp, _sz, _vp]),
+    "kv4_append": (_i32, [_shp, _vp, _vp, _i64, _i64, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "kv4_page_meta": (_i32, [_shp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "kv4_fetch": (_i32, [_shp, _vp, _vp, _vp, _vp, _vp, _i64, _i32, _vp, _vp, _vp]),
+    "kv4_attn_decode_workspace_bytes": (_sz, [_shp, _i32, _i32, _i32]),
+    "kv4_attn_decode": (_i32, [_shp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "attn_decode_tally_workspace_bytes": (_sz, [_shp]),
+    "attn_decode_tally": (_i32, [_shp, _vp, _vp, _vp, _vp, _f32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "cache_evict_workspace_bytes": (_sz, [_shp, _i32]),
+    "cache_evict": (_i32, [_shp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _sz, _vp]),
+    "kv4_evict": (_i32, [_shp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _sz, _vp]),
 }
 
 
@@ -442,3 +452,84 @@ def attn_paged(s, p, q, k_pool, v_pool, table, len, seq, n_new, T_new, share, sc
                              _need(len, torch.int32, p.S), _need(seq, torch.int32, s.B), _need(n_new, torch.int32, s.B), T_new,
                              _need(share, torch.int32, s.B, 3), scale, _need(out, dt, *rows, s.D),
                              _need(lse_out, torch.float32, *rows), *_scratch(ws), _stream()))
+
+
+# ---- a cache in 4 bits, and caches that give up rows: sequences of lengths of their own, in device memory ----
+
+
+def _four(s, k4, k4_scale, v4, v4_scale):
+    rows = (s.B, s.Hkv, s.Tcap)
+    return (_need(k4, torch.uint8, *rows, s.D // 2), _need(k4_scale, torch.uint8, *rows, s.D // 32), _need(v4, torch.uint8, *rows, s.D // 2),
+            _need(v4_scale, torch.uint8, *rows, s.D // 32))
+
+
+def _type(s):
+    return torch.bfloat16 if s.dtype == RS_BF16 else torch.float32
+
+
+def _bounds(s, meta):
+    return _need(meta, _type(s), s.B, s.Hkv, s.Tcap // s.P if s.P > 0 else 0, 2, s.D)
+
+
+def kv4_append(s, k, v, t_src, len, n_new, T_new, k4, k4_scale, v4, v4_scale, meta):
+    """k, v [B, Hkv, T_src, D]: the new tokens are rows t_src .. t_src + T_new - 1."""
+    T_src = k.shape[2] if k.dim() == 4 else 0
+    src = (_type(s), s.B, s.Hkv, T_src, s.D)
+    _check(load().kv4_append(ctypes.byref(s), _need(k, *src), _need(v, *src), T_src, t_src, _need(len, torch.int32, s.B), _need(n_new, torch.int32, s.B),
+                             T_new, *_four(s, k4, k4_scale, v4, v4_scale), _bounds(s, meta), _stream()))
+
+
+def kv4_page_meta(s, k4, k4_scale, len, n_new, T_new, meta):
+    kc, ks, _, _ = _four(s, k4, k4_scale, None, None)
+    _check(load().kv4_page_meta(ctypes.byref(s), kc, ks, _need(len, torch.int32, s.B), _need(n_new, torch.int32, s.B), T_new, _bounds(s, meta),
+                                _stream()))
+
+
+def kv4_fetch(s, k4, k4_scale, v4, v4_scale, len, t0, T, k_out, v_out):
+    to = (_type(s), s.B, s.Hkv, T, s.D)
+    _check(load().kv4_fetch(ctypes.byref(s), *_four(s, k4, k4_scale, v4, v4_scale), _need(len, torch.int32, s.B), t0, T, _need(k_out, *to),
+                            _need(v_out, *to), _stream()))
+
+
+def kv4_attn_decode_workspace_bytes(s, H_idx, K, with_tally):
+    return load().kv4_attn_decode_workspace_bytes(ctypes.byref(s), H_idx, K, bool(with_tally))
+
+
+def kv4_attn_decode(s, q, k4, k4_scale, v4, v4_scale, len, scale, idx, tally, n_fresh, out, lse_out, ws):
+    """idx: [B, Hq or Hkv, K] pages or None."""
+    H, K = (idx.shape[1], idx.shape[2]) if idx is not None and idx.dim() == 3 else (0, 0)
+    rows = (s.B, s.Hq)
+    _check(load().kv4_attn_decode(ctypes.byref(s), _need(q, _type(s), *rows, s.D), *_four(s, k4, k4_scale, v4, v4_scale), _need(len, torch.int32, s.B),
+                                  scale, _need(idx, torch.int32, s.B, H, K), H, K, _need(tally, torch.float32, s.B, s.Hkv, s.Tcap), n_fresh,
+                                  _need(out, _type(s), *rows, s.D), _need(lse_out, torch.float32, *rows), *_scratch(ws), _stream()))
+
+
+def attn_decode_tally_workspace_bytes(s):
+    return load().attn_decode_tally_workspace_bytes(ctypes.byref(s))
+
+
+def attn_decode_tally(s, q, k_cache, v_cache, len, scale, tally, n_fresh, out, lse_out, ws):
+    dt, rows, cache = _type(s), (s.B, s.Hq), (s.B, s.Hkv, s.Tcap)
+    _check(load().attn_decode_tally(ctypes.byref(s), _need(q, dt, *rows, s.D), _need(k_cache, dt, *cache, s.D), _need(v_cache, dt, *cache, s.D),
+                                    _need(len, torch.int32, s.B), scale, _need(tally, torch.float32, *cache), n_fresh, _need(out, dt, *rows, s.D),
+                                    _need(lse_out, torch.float32, *rows), *_scratch(ws), _stream()))
+
+
+def cache_evict_workspace_bytes(s, n_keep):
+    return load().cache_evict_workspace_bytes(ctypes.byref(s), n_keep)
+
+
+def _kept(s, tally, pos, mark, len):
+    cache = (s.B, s.Hkv, s.Tcap)
+    return (_need(tally, torch.float32, *cache), _need(pos, torch.int32, *cache), _need(mark, torch.int32, s.B, 2), _need(len, torch.int32, s.B))
+
+
+def cache_evict(s, k_cache, v_cache, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws):
+    rows = (_type(s), s.B, s.Hkv, s.Tcap, s.D)
+    _check(load().cache_evict(ctypes.byref(s), _need(k_cache, *rows), _need(v_cache, *rows), *_kept(s, tally, pos, mark, len), n_keep, n_first, n_recent,
+                              n_slack, *_scratch(ws), _stream()))
+
+
+def kv4_evict(s, k4, k4_scale, v4, v4_scale, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws):
+    _check(load().kv4_evict(ctypes.byref(s), *_four(s, k4, k4_scale, v4, v4_scale), *_kept(s, tally, pos, mark, len), n_keep, n_first, n_recent, n_slack,
+                            *_scratch(ws), _stream()))

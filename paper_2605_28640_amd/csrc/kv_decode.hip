@@ -1,0 +1,721 @@
+// One token's dense attention over caches of sequences of different lengths, with a tally of the weight that every row has had, and the
+// same over whole or listed pages of a 4-bit cache.
+//   z_t = scale q . k_t,  m = max z,  l = sum e^(z_t - m),  out = sum e^(z_t - m) v_t / l,  tally_t += sum over a KV head's queries of e^(z_t - m) / l
+// Work: a tile is a KV head's (listed pages of a query head: the query head's) up to 16 queries of one sequence; its tokens, in units of 64, lie on a
+// line, tile after tile, sequence after sequence.  The line is divided evenly among the workgroups, whatever the lengths, which every
+// workgroup reads for itself.  A workgroup takes the units of its share four at a time, one a wave; the four waves' results are put
+// together in LDS, and are the tile's result or, where the line is cut inside the tile, a record that a second launch joins with the others.
+// The order of every sum follows from the lengths alone.  The tally needs the weights' sum over all tokens, so the scores (float32) go to
+// the workspace and the second launch turns them into weights.
+#include "check.h"
+#include "common.h"
+#include "kv4.h"
+
+namespace rs {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kQ = 16;         // queries of a tile, at most
+constexpr int kUnit = 64;      // tokens of a unit
+constexpr int kWaves = 4, kThreads = kWaves * kWave;
+constexpr int kGroups = 768;   // workgroups of the first launch, at most
+constexpr int kMaxB = 1024;
+constexpr float kSlack = 8.f;  // the reference point of a softmax moves when the maximum has grown by more (base-2 exponent): weights stay below 2^8
+
+struct DecodeParams {
+    const void *q, *k, *v;        // k, v: rows, or codes
+    const uint8_t *ks, *vs;       // scale bytes
+    const int32_t *len, *idx;
+    void *out;
+    float *lse, *tally;
+    float *rec_o, *rec_ml, *lse2, *z;  // records [2 kGroups, kQ, D], [.., 2]; base-2 log-sum-exps [B, Hq]; scores [B, Hq, z_row]
+    int *start;                   // [B + 1] units of the sequences before
+    int B, Hq, Hkv, H, G, RT, D;  // H: heads with tiles of their own, G queries each, in RT tiles
+    int Tcap, K, shift, list_units, z_row, groups, fresh;
+    float scale;
+};
+
+__device__ __forceinline__ float quad_max(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return half_pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return half_pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ __forceinline__ int length_of(const DecodeParams &a, int b)
+{
+    const int n = a.len[b];
+    return n < 0 ? 0 : n > a.Tcap ? a.Tcap : n;
+}
+__device__ __forceinline__ int units_of(const DecodeParams &a, int b)
+{
+    const int n = length_of(a, b);
+    return a.idx ? (n > 0 ? a.list_units : 0) : (n + kUnit - 1) / kUnit;
+}
+
+// the line's shares
+struct LineShares {
+    int total, n;
+    __device__ __forceinline__ LineShares(int sum, int heads, int groups)
+    {
+        total = sum * heads;
+        n = (total + kWaves - 1) / kWaves;
+        if (n > groups) n = groups;
+    }
+    __device__ __forceinline__ int begin(int i) const { return (int)((long)i * total / n); }
+    __device__ __forceinline__ int of(int unit) const { return (int)((((long)unit + 1) * n - 1) / total); }  // whose a unit is
+};
+
+// units of the sequences before each, in LDS
+__device__ __forceinline__ void make_start(const DecodeParams &a, int *start, int *wave_tot)
+{
+    constexpr int EACH = kMaxB / kThreads;
+    const int t = threadIdx.x, lane = lane_id(), wave = t / kWave;
+    int x[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int b = t * EACH + i;
+        x[i] = b < a.B ? units_of(a, b) : 0;
+        sum += x[i];
+    }
+    const int incl = wave_scan_i(sum);
+    if (lane == kWave - 1) wave_tot[wave] = incl;
+    __syncthreads();
+    int at = incl - sum;
+    for (int w = 0; w < wave; ++w) at += wave_tot[w];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int b = t * EACH + i;
+        if (b <= a.B) start[b] = at;
+        at += x[i];
+    }
+    if (t == kThreads - 1 && a.B == kMaxB) start[kMaxB] = at;
+    __syncthreads();
+}
+
+struct LineTile {
+    int b, h, rt, s0, s1;  // sequence, head, 16 queries of it, its units on the line
+};
+__device__ __forceinline__ LineTile find_tile(const DecodeParams &a, const int *start, int unit)
+{
+    const int HR = a.H * a.RT;
+    int lo = 0, hi = a.B;  // the last b with start[b] HR <= unit
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (scalar(start[mid]) * HR <= unit) lo = mid;
+        else hi = mid;
+    }
+    LineTile w;
+    const int first = scalar(start[lo]), n = scalar(start[lo + 1]) - first, hr = (unit - first * HR) / n;
+    w.b = lo;
+    w.h = hr / a.RT;
+    w.rt = hr - w.h * a.RT;
+    w.s0 = first * HR + hr * n;
+    w.s1 = w.s0 + n;
+    return w;
+}
+
+// the token row that a query's first 16 tokens of a unit begin at, and how many of them there are
+template <int NH>
+struct StepWhere {
+    int at[NH], valid[NH];
+};
+
+// ---- the rows of a step: 16 NH tokens ------------------------------------------------------------------------------------
+// Lane (l16, lg) = (lane % 16, lane / 16) takes token l16 of every 16 as the K operand, and query l16.  V goes through a tile in LDS: 32 bfloat16
+// rows (float32: 16), 16-byte chunks permuted so that the transpose reads of the product touch every bank once.
+template <bool FOUR, typename ST, int D>
+struct StepRows;
+
+// 4 bits: a lane's part of a row is D / 8 neighbouring bytes, D / 4 channels of one group: one load, one scale.  The queries' channels follow.
+template <typename ST, int D>
+struct StepRows<true, ST, D> {
+    static constexpr int NH = 4, NK = D / 32, TERMS = sizeof(ST) == 2 ? 1 : 3, ROW = 2 * D, CODES = D / 2, SCALES = D / 32;
+    uint32_t kc[NH][NK], vc[NH][NK], kf[NH], vf[NH];
+    bf16x8 qf[TERMS][NK];
+    int lane, l16, lg;
+
+    __device__ __forceinline__ static int swizzle(int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
+    __device__ __forceinline__ void load_q(const ST *q, bool real)
+    {
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            float x[8];
+            Row8<ST>::load(q + lg * (D / 4) + kk * 8, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float rest = real ? x[j] : 0.f;
+#pragma unroll
+                for (int n = 0; n < TERMS; ++n) {  // float32 as the sum of three bfloat16 numbers: all of its 24 bits
+                    const __bf16 part = (__bf16)rest;
+                    qf[n][kk][j] = part;
+                    rest -= (float)part;
+                }
+            }
+        }
+    }
+    template <int N>
+    __device__ __forceinline__ static void load_codes(LdsSource src, uint32_t at, uint32_t (&c)[N])
+    {
+        if constexpr (N == 4) {
+            const auto x = __builtin_amdgcn_raw_buffer_load_b128(src, at, 0, 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] = (uint32_t)x[i];
+        } else {
+            const auto x = __builtin_amdgcn_raw_buffer_load_b64(src, at, 0, 2);
+            c[0] = (uint32_t)x[0], c[1] = (uint32_t)x[1];
+        }
+    }
+    __device__ __forceinline__ void load_k(const DecodeParams &a, long base, const StepWhere<NH> &x)
+    {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const long row = base + x.at[h];
+            load_codes(lds_source_sized((const uint8_t *)a.k + row * CODES, x.valid[h] * CODES), (uint32_t)(l16 * CODES + lg * (CODES / 4)), kc[h]);
+            kf[h] = __builtin_amdgcn_raw_buffer_load_b8(lds_source_sized(a.ks + row * SCALES, x.valid[h] * SCALES),
+                                                        (uint32_t)(l16 * SCALES + (D == 128 ? lg : lg >> 1)), 0, 0);
+        }
+    }
+    __device__ __forceinline__ void load_v(const DecodeParams &a, long base, const StepWhere<NH> &x)
+    {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const long row = base + x.at[h];
+            load_codes(lds_source_sized((const uint8_t *)a.v + row * CODES, x.valid[h] * CODES), (uint32_t)(lane * (CODES / 4)), vc[h]);
+            vf[h] = __builtin_amdgcn_raw_buffer_load_b8(lds_source_sized(a.vs + row * SCALES, x.valid[h] * SCALES),
+                                                        (uint32_t)((lane >> 2) * SCALES + (D == 128 ? lane & 3 : (lane & 3) >> 1)), 0, 0);
+        }
+    }
+    // S^T = K Q^T of 16 tokens: tokens 4 lg .. 4 lg + 3 of query l16
+    __device__ __forceinline__ f32x4 scores(int h) const
+    {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        const float f = kv4_scale(kf[h] & 255u);
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            uint32_t p[4];
+            kv4_values(kc[h][kk], f, p);
+            const bf16x8 k = __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
+#pragma unroll
+            for (int n = 0; n < TERMS; ++n) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[n][kk], s, 0, 0, 0);
+        }
+        return s;
+    }
+    // O^T += V^T P^T; p: the weights of all 16 NH tokens
+    __device__ __forceinline__ void values(char *tile, const f32x4 (&p)[NH], f32x4 (&o)[D / 16])
+    {
+#pragma unroll
+        for (int half = 0; half < NH / 2; ++half) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = 16 * h + (lane >> 2);
+                const float f = kv4_scale(vf[2 * half + h] & 255u);
+#pragma unroll
+                for (int c = 0; c < NK; ++c) {
+                    uint32_t w[4];
+                    kv4_values(vc[2 * half + h][c], f, w);
+                    *reinterpret_cast<uint4 *>(tile + row * ROW + (((lane & 3) * NK + c) ^ swizzle(row)) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            product32<ST, D, TERMS>(tile, p[2 * half], p[2 * half + 1], o, l16, lg);
+        }
+    }
+    template <typename PT, int DD, int N>
+    __device__ __forceinline__ static void product32(const char *tile, const f32x4 &p0, const f32x4 &p1, f32x4 (&o)[DD / 16], int l16, int lg)
+    {
+        bf16x8 pf[N];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float rest = i < 4 ? p0[i] : p1[i - 4];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const __bf16 part = (__bf16)rest;
+                pf[n][i] = part;
+                rest -= (float)part;
+            }
+        }
+        const int r = 4 * lg + (l16 >> 2);
+        const uint32_t at = (uint32_t)(r * 2 * DD + ((((l16 & 3) >> 1) ^ swizzle(r)) * 16) + 8 * (l16 & 1));
+#pragma unroll
+        for (int dt = 0; dt < DD / 16; ++dt) {
+            union {
+                s16x4 h[2];
+                bf16x8 f;
+            } x;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                x.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(tile + (at ^ (uint32_t)(32 * dt)) + h * 16 * 2 * DD));
+#pragma unroll
+            for (int n = 0; n < N; ++n) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.f, pf[n], o[dt], 0, 0, 0);
+        }
+    }
+};
+
+// bfloat16 and float32 rows: 16-byte operands at chunk 4 kk + lg of a row
+template <typename ST, int D>
+struct StepRows<false, ST, D> {
+    static constexpr bool BF = sizeof(ST) == 2;
+    static constexpr int NH = BF ? 2 : 1, ROW = D * (int)sizeof(ST), NK = ROW / 64, CR = ROW / 16, RW = 64 / CR, NL = 16 / RW;
+    f32x4 kx[NH][NK], vx[NH][NL], qf[NK];
+    int lane, l16, lg;
+
+    __device__ __forceinline__ static int swizzle(int row)
+    {
+        if (!BF) return 4 * ((row >> 2) & 3);
+        return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3);
+    }
+    __device__ __forceinline__ void load_q(const ST *q, bool real)
+    {
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const char *>(q) + 64 * kk + 16 * lg);
+            qf[kk] = real ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    __device__ __forceinline__ void load_k(const DecodeParams &a, long base, const StepWhere<NH> &x)
+    {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const LdsSource src = lds_source_sized((const char *)a.k + (base + x.at[h]) * ROW, x.valid[h] * ROW);
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk)
+                kx[h][kk] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (uint32_t)(l16 * ROW + lg * 16 + 64 * kk), 0, 2));
+        }
+    }
+    __device__ __forceinline__ void load_v(const DecodeParams &a, long base, const StepWhere<NH> &x)
+    {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const LdsSource src = lds_source_sized((const char *)a.v + (base + x.at[h]) * ROW, x.valid[h] * ROW);
+#pragma unroll
+            for (int i = 0; i < NL; ++i) vx[h][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (uint32_t)(lane * 16 + 1024 * i), 0, 2));
+        }
+    }
+    __device__ __forceinline__ f32x4 scores(int h) const
+    {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            if constexpr (BF) {
+                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[h][kk]), __builtin_bit_cast(bf16x8, qf[kk]), s, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[h][kk][j], qf[kk][j], s, 0, 0, 0);
+            }
+        }
+        return s;
+    }
+    __device__ __forceinline__ void values(char *tile, const f32x4 (&p)[NH], f32x4 (&o)[D / 16])
+    {
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int row = 16 * h + i * RW + lane / CR;
+                *reinterpret_cast<f32x4 *>(tile + row * ROW + ((lane % CR) ^ swizzle(row)) * 16) = vx[h][i];
+            }
+        if constexpr (BF) {
+            StepRows<true, ST, D>::template product32<ST, D, 1>(tile, p[0], p[1], o, l16, lg);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 4 * lg + j;
+                const uint32_t at = (uint32_t)(r * ROW + (((l16 >> 2) ^ swizzle(r)) * 16) + 4 * (l16 & 3));
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt)
+                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float *>(tile + (at ^ (uint32_t)(64 * dt))), p[0][j], o[dt], 0, 0, 0);
+            }
+        }
+    }
+};
+
+// a row's result: 4 channels from c on
+template <typename ST>
+__device__ __forceinline__ void put(const DecodeParams &a, long row, int c, const f32x4 &o, float m, float l)
+{
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    ST *const to = (ST *)a.out + row * a.D + c;
+    if constexpr (sizeof(ST) == 2) {
+        *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    } else {
+        *reinterpret_cast<float4 *>(to) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    }
+    if (c == 0) {
+        const float z = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);  // (base 2)
+        if (a.lse) a.lse[row] = z * kLn2;
+        a.lse2[row] = z;
+    }
+}
+
+template <bool FOUR, typename ST, int D, bool LISTED, bool TALLY>
+__global__ __launch_bounds__(kThreads) void decode_attend_kernel(const DecodeParams a)
+{
+    using R = StepRows<FOUR, ST, D>;
+    constexpr int NH = R::NH, STEP = 16 * NH, SPU = kUnit / STEP, C4 = D / 4;
+    __shared__ __attribute__((aligned(1024))) char tiles[kWaves][64 * D];
+    __shared__ float ml[kWaves][kQ][2];
+    __shared__ int start[kMaxB + 1];
+    __shared__ int wave_tot[kWaves];
+    make_start(a, start, wave_tot);
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b <= a.B; b += kThreads) a.start[b] = start[b];
+    const LineShares sh(scalar(start[a.B]), a.H * a.RT, a.groups);
+    if ((int)blockIdx.x >= sh.n) return;
+    const int wave = scalar(threadIdx.x / kWave);
+    R r;
+    r.lane = lane_id(), r.l16 = r.lane & 15, r.lg = r.lane >> 4;
+    char *const tile = tiles[wave];
+    const float cs = a.scale * kLog2e;
+    int at = sh.begin(blockIdx.x);
+    const int end = sh.begin(blockIdx.x + 1);
+#pragma unroll 1
+    while (at < end) {
+        const LineTile w = find_tile(a, start, at);
+        const int from = at - w.s0, to = min(end, w.s1) - w.s0;  // the tile's units that are this workgroup's
+        at = w.s0 + to;
+        const int L = scalar(length_of(a, w.b)), rows = min(a.G - w.rt * kQ, kQ);
+        const long base = (long)(w.b * a.Hkv + w.h / (a.H / a.Hkv)) * a.Tcap;
+        const long row0 = (long)w.b * a.Hq + w.h * a.G + w.rt * kQ;  // of the queries
+        const bool real = r.l16 < rows;
+        const int32_t *list = LISTED ? a.idx + (long)(w.b * a.H + w.h) * a.K : nullptr;
+        const int n_units = to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0, n_steps = n_units * SPU;
+        auto token_of = [&](int i) { return (from + wave + kWaves * (i / SPU)) * kUnit + i % SPU * STEP; };
+        auto look_up = [&](int i) -> StepWhere<NH> {  // (past the last step: no rows)
+            StepWhere<NH> x;
+            const int t = token_of(i);
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+                int row = t + 16 * h;
+                if constexpr (LISTED) {
+                    const int slot = row >> a.shift, page = i < n_steps && slot < a.K ? scalar(list[slot]) : -1;
+                    row = page < 0 || page >= (a.Tcap >> a.shift) ? a.Tcap : (page << a.shift) + (row & ((1 << a.shift) - 1));
+                }
+                const int left = L - row;
+                x.valid[h] = scalar(i >= n_steps || left < 0 ? 0 : left < 16 ? left : 16);
+                x.at[h] = scalar(x.valid[h] ? row : 0);
+            }
+            return x;
+        };
+        r.load_q((const ST *)a.q + (real ? row0 + r.l16 : row0) * D, real);
+        StepWhere<NH> x = look_up(0);
+        r.load_k(a, base, x);
+        r.load_v(a, base, x);
+        f32x4 o[D / 16];
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < n_steps; ++i) {
+            f32x4 s[NH];
+#pragma unroll
+            for (int h = 0; h < NH; ++h) s[h] = r.scores(h) * cs;
+            const StepWhere<NH> next = look_up(i + 1);
+            r.load_k(a, base, next);
+            float mx = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+                const int sees = x.valid[h] - 4 * r.lg;  // of the lane's four
+                if (x.valid[h] < 16) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[h][j] = j < sees ? s[h][j] : -INFINITY;
+                }
+                if constexpr (TALLY) {
+                    if (real) *reinterpret_cast<f32x4 *>(a.z + (row0 + r.l16) * a.z_row + token_of(i) + 16 * h + 4 * r.lg) = s[h];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[h][j]);
+            }
+            mx = quad_max(mx);
+            if (__any(mx - m > kSlack)) {  // (-inf from -inf compares false)
+                const float top = (mx - m > kSlack) ? mx : m, f = (m == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m - top);
+                l *= f;
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) o[dt] *= f;
+                m = top;
+            }
+            const float bias = (m == -INFINITY) ? 0.f : m;
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[h][j] = __builtin_amdgcn_exp2f(s[h][j] - bias);
+                    l += s[h][j];
+                }
+            r.values(tile, s, o);
+            x = next;
+            r.load_v(a, base, x);
+        }
+        // the four waves' parts
+        l = quad_sum(l);
+        if (r.lg == 0) ml[wave][r.l16][0] = m, ml[wave][r.l16][1] = l;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt)
+            *reinterpret_cast<f32x4 *>(tile + r.l16 * D * 4 + ((4 * dt + r.lg) ^ r.l16) * 16) = o[dt];
+        __syncthreads();
+        const bool whole = from == 0 && at == w.s1;
+        const long slot = 2l * blockIdx.x + (from == 0 ? 1 : 0);  // a tile that began in another share: the first of two records
+        for (int e = threadIdx.x; e < rows * C4; e += kThreads) {
+            const int row = e / C4, c4 = e % C4;
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i][row][0]);
+            f32x4 out = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                const float mi = ml[i][row][0], li = ml[i][row][1];
+                if (mi == -INFINITY && li == 0.f) continue;  // saw nothing
+                const float f = mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
+                sum += li * f;
+                out += *reinterpret_cast<const f32x4 *>(tiles[i] + row * D * 4 + (c4 ^ row) * 16) * f;
+            }
+            if (whole) {
+                put<ST>(a, row0 + row, 4 * c4, out, top, sum);
+            } else {
+                *reinterpret_cast<f32x4 *>(a.rec_o + (slot * kQ + row) * D + 4 * c4) = out;
+                if (c4 == 0) *reinterpret_cast<float2 *>(a.rec_ml + (slot * kQ + row) * 2) = make_float2(top, sum);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// the records of a tile: that of share first is its workgroup's second, those of the shares after it are their first
+__device__ __forceinline__ long record_of(int share, int first) { return 2l * share + (share == first ? 1 : 0); }
+
+__device__ __forceinline__ void join(float &m, float &l, f32x4 &o, float m1, float l1, const f32x4 &o1)
+{
+    if (m1 == -INFINITY && l1 == 0.f) return;
+    const float top = fmaxf(m, m1), f0 = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), f1 = m1 == top ? 1.f : __builtin_amdgcn_exp2f(m1 - top);
+    m = top;
+    l = l * f0 + l1 * f1;
+    o = o * f0 + o1 * f1;
+}
+
+// Workgroups 0 .. B Hq - 1 join the records of a query each; the others, 1024 tokens of a KV head each, add its queries' weights to the tally.
+template <typename ST, int D>
+__global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParams a)
+{
+    constexpr int C4 = D / 4, NG = kThreads / C4;
+    __shared__ float part[NG][D], part_ml[NG][2];
+    __shared__ float lse2[kThreads];
+    const int HR = a.H * a.RT;
+    const LineShares sh(a.start[a.B], HR, a.groups);
+    const int rows = a.B * a.Hq;
+    if ((int)blockIdx.x < rows) {
+        const int row = blockIdx.x, b = row / a.Hq, hq = row - b * a.Hq, h = hq / a.G, g = hq - h * a.G, rt = g / kQ, r = g % kQ;
+        const int n = a.start[b + 1] - a.start[b], s0 = a.start[b] * HR + (h * a.RT + rt) * n;
+        const int c4 = threadIdx.x % C4, grp = threadIdx.x / C4;
+        float m = -INFINITY, l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        if (n == 0) {
+            if (grp == 0) put<ST>(a, row, 4 * c4, o, m, l);
+            return;
+        }
+        const int first = sh.of(s0), last = sh.of(s0 + n - 1);
+        if (first == last) return;  // written as it is
+        constexpr int AHEAD = 4;
+        for (int i = first + grp; i <= last; i += AHEAD * NG) {
+            float2 x[AHEAD];
+            f32x4 v[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                x[j] = make_float2(-INFINITY, 0.f);
+                v[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (i + j * NG <= last) {
+                    const long at = record_of(i + j * NG, first) * kQ + r;
+                    x[j] = *reinterpret_cast<const float2 *>(a.rec_ml + at * 2);
+                    v[j] = *reinterpret_cast<const f32x4 *>(a.rec_o + at * D + 4 * c4);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) join(m, l, o, x[j].x, x[j].y, v[j]);
+        }
+        *reinterpret_cast<f32x4 *>(&part[grp][4 * c4]) = o;
+        if (c4 == 0) part_ml[grp][0] = m, part_ml[grp][1] = l;
+        __syncthreads();
+        if (grp == 0) {
+#pragma unroll
+            for (int i = 1; i < NG; ++i) join(m, l, o, part_ml[i][0], part_ml[i][1], *reinterpret_cast<const f32x4 *>(&part[i][4 * c4]));
+            put<ST>(a, row, 4 * c4, o, m, l);
+        }
+        return;
+    }
+    // ---- the tally ----
+    const int slices = (a.Tcap + 4 * kThreads - 1) / (4 * kThreads), e = blockIdx.x - rows, bh = e / slices, b = bh / a.Hkv, h = bh - b * a.Hkv;
+    const int t0 = (e - bh * slices) * 4 * kThreads, L = length_of(a, b);
+    if (t0 >= L) return;
+    const int n = a.start[b + 1] - a.start[b], lane = lane_id(), wave = threadIdx.x / kWave;
+    const int t = t0 + 4 * threadIdx.x;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g0 = 0; g0 < a.G; g0 += kThreads) {  // (more than 256 queries to a KV head: by turns)
+        const int n_g = min(a.G - g0, kThreads);
+        for (int i = wave; i < n_g; i += kWaves) {
+            const int g = g0 + i, rt = g / kQ, r = g % kQ;
+            const int s0 = a.start[b] * HR + (h * a.RT + rt) * n, first = sh.of(s0), last = sh.of(s0 + n - 1);
+            float z;
+            if (first == last) {
+                z = a.lse2[(long)b * a.Hq + h * a.G + g];
+            } else {
+                float m = -INFINITY, l = 0.f;
+                for (int x = first + lane; x <= last; x += kWave) {
+                    const float2 y = *reinterpret_cast<const float2 *>(a.rec_ml + (record_of(x, first) * kQ + r) * 2);
+                    f32x4 none = {0.f, 0.f, 0.f, 0.f};
+                    join(m, l, none, y.x, y.y, none);
+                }
+#pragma unroll
+                for (int k = kWave / 2; k >= 1; k >>= 1) {
+                    f32x4 none = {0.f, 0.f, 0.f, 0.f};
+                    const float m1 = shfl_xor_f(m, k), l1 = shfl_xor_f(l, k);
+                    join(m, l, none, m1, l1, none);
+                }
+                z = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+            }
+            if (lane == 0) lse2[i] = z;
+        }
+        __syncthreads();
+        if (t < L) {
+            const float *z = a.z + ((long)b * a.Hq + h * a.G + g0) * a.z_row + t;
+            for (int i = 0; i < n_g; ++i) {
+                const float4 x = *reinterpret_cast<const float4 *>(z + (long)i * a.z_row);
+                const float s = lse2[i] == -INFINITY ? 0.f : lse2[i];
+                w[0] += __builtin_amdgcn_exp2f(x.x - s), w[1] += __builtin_amdgcn_exp2f(x.y - s);
+                w[2] += __builtin_amdgcn_exp2f(x.z - s), w[3] += __builtin_amdgcn_exp2f(x.w - s);
+            }
+        }
+        __syncthreads();
+    }
+    float *to = a.tally + (long)bh * a.Tcap + t;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (t + j < L) to[j] = (t + j >= L - a.fresh ? 0.f : to[j]) + w[j];
+}
+
+struct DecodeLayout {
+    size_t ml, lse2, start, z, total;
+    int z_row;
+};
+static DecodeLayout decode_layout(const rs_shape *s, bool tally)
+{
+    DecodeLayout x;
+    x.z_row = tally ? (s->Tcap + kUnit - 1) / kUnit * kUnit : 0;
+    x.ml = RS_WS_CTRL_BYTES + (size_t)2 * kGroups * kQ * s->D * 4;
+    x.lse2 = x.ml + (size_t)2 * kGroups * kQ * 8;
+    x.start = x.lse2 + align256((size_t)s->B * s->Hq * 4);
+    x.z = x.start + align256((size_t)(s->B + 1) * 4);
+    x.total = x.z + (size_t)s->B * s->Hq * x.z_row * 4;
+    return x;
+}
+
+// H, K: heads and pages of the lists; 0, 0: none
+static int check_decode(const rs_shape *s, int H, int K)
+{
+    const bool listed = H != 0 || K != 0;
+    const int st = check_rows(s, listed);
+    if (st != RS_OK) return st;
+    if (listed && ((H != s->Hq && H != s->Hkv) || K < 1 || K > s->Tcap / s->P)) return RS_INVALID_ARG;
+    if (s->B > kMaxB || s->Tcap > (1 << 30)) return RS_UNSUPPORTED;
+    const double heads = listed ? H : s->Hkv, tiles = heads * ((s->Hq / heads + kQ - 1) / kQ), tokens = listed ? (double)K * s->P : s->Tcap;
+    // units of the line, and workgroups of the second launch
+    if (s->B * tiles * (tokens / kUnit + 1) > 2e9 || (double)s->B * s->Hq + (double)s->B * s->Hkv * (s->Tcap / 1024. + 1) > 2e9) return RS_UNSUPPORTED;
+    return RS_OK;
+}
+
+template <bool FOUR, typename ST, int D>
+static void decode_launch(const DecodeParams &a, hipStream_t stream)
+{
+    if constexpr (FOUR) {
+        if (a.idx) decode_attend_kernel<true, ST, D, true, false><<<a.groups, kThreads, 0, stream>>>(a);
+        else if (a.tally) decode_attend_kernel<true, ST, D, false, true><<<a.groups, kThreads, 0, stream>>>(a);
+        else decode_attend_kernel<true, ST, D, false, false><<<a.groups, kThreads, 0, stream>>>(a);
+    } else {
+        decode_attend_kernel<false, ST, D, false, true><<<a.groups, kThreads, 0, stream>>>(a);
+    }
+    const long slices = a.tally ? (long)a.B * a.Hkv * ((a.Tcap + 1023) / 1024) : 0;
+    decode_join_kernel<ST, D><<<(unsigned)((long)a.B * a.Hq + slices), kThreads, 0, stream>>>(a);
+}
+
+static int decode_run(const rs_shape *s, DecodeParams a, bool four, int H, int K, void *ws, hipStream_t stream)
+{
+    const DecodeLayout x = decode_layout(s, a.tally != nullptr);
+    char *const w = (char *)ws;
+    a.rec_o = (float *)(w + RS_WS_CTRL_BYTES), a.rec_ml = (float *)(w + x.ml), a.lse2 = (float *)(w + x.lse2);
+    a.start = (int *)(w + x.start), a.z = (float *)(w + x.z), a.z_row = x.z_row;
+    a.B = s->B, a.Hq = s->Hq, a.Hkv = s->Hkv, a.D = s->D, a.Tcap = s->Tcap;
+    a.H = a.idx ? H : s->Hkv, a.G = s->Hq / a.H, a.RT = (a.G + kQ - 1) / kQ, a.K = K;
+    a.shift = a.idx ? __builtin_ctz((unsigned)s->P) : 0;
+    a.list_units = a.idx ? (int)(((long)K * s->P + kUnit - 1) / kUnit) : 0;
+    const long most = (long)s->B * a.H * a.RT * (a.idx ? a.list_units : (s->Tcap + kUnit - 1) / kUnit);
+    a.groups = (int)((most + kWaves - 1) / kWaves < kGroups ? (most + kWaves - 1) / kWaves : kGroups);
+    const bool bf = s->dtype == RS_BF16;
+    if (four) {
+        if (bf && s->D == 128) decode_launch<true, bf16, 128>(a, stream);
+        else if (bf) decode_launch<true, bf16, 64>(a, stream);
+        else if (s->D == 128) decode_launch<true, float, 128>(a, stream);
+        else decode_launch<true, float, 64>(a, stream);
+    } else {
+        if (bf && s->D == 128) decode_launch<false, bf16, 128>(a, stream);
+        else if (bf) decode_launch<false, bf16, 64>(a, stream);
+        else if (s->D == 128) decode_launch<false, float, 128>(a, stream);
+        else decode_launch<false, float, 64>(a, stream);
+    }
+    return launch_status();
+}
+
+}  // namespace rs
+
+using namespace rs;
+
+extern "C" {
+
+size_t kv4_attn_decode_workspace_bytes(const rs_shape *s, int32_t H_idx, int32_t K, int32_t with_tally)
+{
+    return check_decode(s, H_idx, K) == RS_OK ? decode_layout(s, with_tally != 0).total : 0;
+}
+
+int32_t kv4_attn_decode(const rs_shape *s, const void *q, const uint8_t *k4, const uint8_t *k4_scale, const uint8_t *v4, const uint8_t *v4_scale,
+                        const int32_t *len, float scale, const int32_t *idx, int32_t H_idx, int32_t K, float *tally, int32_t n_fresh, void *out,
+                        float *lse_out, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!idx) H_idx = K = 0;
+    else if (H_idx < 1 || K < 1) return RS_INVALID_ARG;
+    const int st = check_decode(s, H_idx, K);
+    if (st != RS_OK) return st;
+    if (!q || !k4 || !k4_scale || !v4 || !v4_scale || !len || !out || (idx && tally) || (tally && n_fresh < 0)) return RS_INVALID_ARG;
+    for (const void *x : {q, (const void *)k4, (const void *)k4_scale, (const void *)v4, (const void *)v4_scale, (const void *)len, (const void *)idx,
+                          (const void *)tally, (const void *)out, (const void *)lse_out})
+        if (!aligned16(x)) return RS_INVALID_ARG;
+    if (!ws || !aligned16(ws) || ws_bytes < decode_layout(s, tally != nullptr).total) return RS_WORKSPACE_TOO_SMALL;
+    DecodeParams a = {};
+    a.q = q, a.k = k4, a.v = v4, a.ks = k4_scale, a.vs = v4_scale, a.len = len, a.idx = idx, a.out = out, a.lse = lse_out, a.tally = tally;
+    a.fresh = n_fresh, a.scale = scale;
+    return decode_run(s, a, true, H_idx, K, ws, (hipStream_t)stream);
+}
+
+size_t attn_decode_tally_workspace_bytes(const rs_shape *s) { return check_decode(s, 0, 0) == RS_OK ? decode_layout(s, true).total : 0; }
+
+int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache, const void *v_cache, const int32_t *len, float scale, float *tally,
+                          int32_t n_fresh, void *out, float *lse_out, void *ws, size_t ws_bytes, void *stream)
+{
+    const int st = check_decode(s, 0, 0);
+    if (st != RS_OK) return st;
+    if (!q || !k_cache || !v_cache || !len || !tally || !out || n_fresh < 0) return RS_INVALID_ARG;
+    for (const void *x : {q, k_cache, v_cache, (const void *)len, (const void *)tally, (const void *)out, (const void *)lse_out})
+        if (!aligned16(x)) return RS_INVALID_ARG;
+    if (!ws || !aligned16(ws) || ws_bytes < decode_layout(s, true).total) return RS_WORKSPACE_TOO_SMALL;
+    DecodeParams a = {};
+    a.q = q, a.k = k_cache, a.v = v_cache, a.len = len, a.out = out, a.lse = lse_out, a.tally = tally;
+    a.fresh = n_fresh, a.scale = scale;
+    return decode_run(s, a, false, 0, 0, ws, (hipStream_t)stream);
+}
+
+}  // extern "C"
