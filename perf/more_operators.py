@@ -226,6 +226,9 @@ def prepare(case, seed):
     if own:
         from paper_2605_28640_amd import binding as rs
         s["rs"] = rs
+        for n in ("k4", "v4"):  # a cache of bytes, which the calls ask for
+            if n in s:
+                s[n] = s[n].to(torch.uint8)
         s["shape"] = shape = rs.make_shape(s["B"], s["Hq"], s["Hkv"], s["D"], s["cap"], s["P"], _dt(case))
         if case["kind"] == "attn":
             lists = s["idx"].shape[1:] if case["pages"] else (0, 0)
