@@ -1,30 +1,69 @@
 // Sequences that have outgrown their budget: of every KV head's rows those with the largest tallies stay, and the first and the newest ones.
-// Which rows stay is decided by a workgroup for each (sequence, KV head): the n_keep-th largest key by a radix search, ties to the lower row.
+// Which rows stay is decided by a workgroup for each (sequence, KV head): the n_keep-th largest key by a radix search (11, 11 and 10 bits), ties
+// to the lower row; where only a few rows go, as in a decode step, by taking the smallest that often.
 // Rows do not have to lie in the order of their positions, so only those kept rows move that lie behind the first n_keep, to the places
-// of the dropped ones before it: the i-th of them to the i-th hole.  Sources and destinations are apart, so they move in any order (a second
-// launch, all CUs).
+// of the dropped ones before it: the i-th of them to the i-th hole.  Sources and destinations are apart, so they move in any order: a few by the
+// deciding workgroup, many by a second launch on all CUs.
 #include "check.h"
 #include "common.h"
 
 namespace rs {
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
+constexpr int kFewGo = 8;       // up to so many dropped rows are looked for one by one
+constexpr int kMovedHere = 64;  // up to so many rows are moved by the workgroup that chose them
+constexpr int kTurn = 256;      // rows that a wave looks at together
+constexpr int kBins = 2048, kCopies = 2;
+constexpr int kMostHeld = 34816;  // keys that fit in LDS beside the bins
+constexpr uint32_t kStays = 0xffffffffu;  // the key of a row that stays whatever its tally (+inf: 0xff800000)
+
+struct MovedRows {
+    char *rows[4];  // K and V, or their codes and scale bytes
+    int bytes[4];   // a row
+    int n;
+};
 
 struct EvictParams {
     float *tally;
     int32_t *pos, *mark, *len;
-    int32_t *state, *count;  // [B, 2] length afterwards (-1: as it is), tokens seen; [B Hkv] rows that move
-    int2 *pairs;             // [B Hkv, most] (from, to)
-    uint32_t *keys;          // [B Hkv, Tcap]
-    long most;
+    int32_t *count;      // [B Hkv] rows that the second launch moves
+    uint32_t *arrived;   // [B] workgroups of a sequence that are done; zero before and after
+    int2 *pairs;         // [B Hkv, most] (from, to)
+    uint32_t *keys;      // [B Hkv, key_row], of caches with more rows than LDS holds
+    long most, key_row;
+    MovedRows moved;
     int Hkv, Tcap, keep, first, recent, slack;
 };
 
-// inclusive prefix sums of one number a wave: *before gets those of the waves before this one, the return value is the sum of all
+// pieces of U bytes
+template <typename U>
+__device__ __forceinline__ void move_rows(char *rows, int bytes, const int2 *pairs, int n, long at, long step)
+{
+    const int per = bytes / (int)sizeof(U);
+    for (long i = at; i < (long)n * per; i += step) {
+        const int2 p = pairs[i / per];
+        const int c = (int)(i % per);
+        reinterpret_cast<U *>(rows + (long)p.y * bytes)[c] = reinterpret_cast<const U *>(rows + (long)p.x * bytes)[c];
+    }
+}
+__device__ __forceinline__ void move_all(const MovedRows &m, long first_row, const int2 *pairs, int n, long at, long step)
+{
+    for (int i = 0; i < m.n; ++i) {
+        char *rows = m.rows[i] + first_row * m.bytes[i];
+        if (m.bytes[i] % 16 == 0) move_rows<uint4>(rows, m.bytes[i], pairs, n, at, step);
+        else move_rows<uint16_t>(rows, m.bytes[i], pairs, n, at, step);
+    }
+}
+
+__device__ __forceinline__ int lanes_below(uint64_t ballot)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(ballot >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ballot, 0u));
+}
+
+// inclusive sums over the waves: `before` gets what the waves before this one hold, the return value is all.  lds: not in use by an earlier call
 __device__ __forceinline__ int wave_offsets(int x, int *lds, int &before)
 {
     const int wave = threadIdx.x / kWave;
-    __syncthreads();
     if (lane_id() == 0) lds[wave] = x;
     __syncthreads();
     int sum = 0;
@@ -37,162 +76,273 @@ __device__ __forceinline__ int wave_offsets(int x, int *lds, int &before)
     return sum;
 }
 
+template <typename F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t x, F f)
+{
+#pragma unroll
+    for (int m = kWave / 2; m >= 1; m >>= 1) x = f(x, (uint32_t)__shfl_xor((int)x, m, kWave));
+    return x;
+}
+
+// Keys are looked at several times: from LDS, where HELD of them fit, or (0) from memory.  A wave takes neighbouring rows, 256 a turn, four neighbours
+// a thread.  (Keys in registers instead, 32 a thread, made loops of 32 copies and spilled: 36 us for 16384 rows of 32 heads, 57 from memory.)
+template <int HELD>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParams a)
 {
-    constexpr int COPIES = 16;
-    __shared__ uint32_t hist[256][COPIES];
-    __shared__ int lds[kWaves];
+    __shared__ __attribute__((aligned(16))) uint32_t held[HELD > 0 ? HELD : 4];
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins][kCopies];
+    __shared__ int lds[3][kWaves];
+    __shared__ __attribute__((aligned(16))) int4 counts[kWaves];
     __shared__ int found[2];
-    const int bh = blockIdx.x, b = bh / a.Hkv, lane = lane_id(), wave = threadIdx.x / kWave;
+    __shared__ uint32_t least[2][kWaves][2];
+    __shared__ int2 few[kMovedHere];
+    const int bh = blockIdx.x, b = bh / a.Hkv, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int L = min(a.len[b], a.Tcap);
     const int known = max(0, min(a.mark[2 * b], L)), before = a.mark[2 * b + 1];
     const bool over = L > a.keep && L - a.keep > a.slack;
-    const int total = before + L - known;
-    if (threadIdx.x == 0) {
-        if (bh == b * a.Hkv) a.state[2 * b] = over ? a.keep : -1, a.state[2 * b + 1] = total;
-        if (!over) a.count[bh] = 0;
+    if (!over) {
+        if (threadIdx.x == 0) a.count[bh] = 0;
+        return;
     }
-    if (!over) return;
+    const int total = before + L - known, n_go = L - a.keep;
     float *const tally = a.tally + (long)bh * a.Tcap;
     int32_t *const pos = a.pos + (long)bh * a.Tcap;
-    uint32_t *const keys = a.keys + (long)bh * a.Tcap;
+    int2 *const pairs = a.pairs + bh * a.most;
+    uint32_t *const keys = HELD > 0 ? held : a.keys + bh * a.key_row;
     auto position = [&](int t) { return t < known ? pos[t] : before + (t - known); };
-    // a wave's rows: a multiple of 64 of them
-    const int each = (L + kThreads - 1) / kThreads * kWave, from = min(L, wave * each), to = min(L, from + each);
-    for (int t = from + lane; t < to; t += kWave) {
-        const int p = position(t);
-        const float x = tally[t];
-        keys[t] = p < a.first || p >= total - a.recent ? 0xffffffffu : x != x ? 0u : float_to_key(x);
-    }
-    // ---- the keep-th largest key ----
-    uint32_t prefix = 0;
-    int left = a.keep;  // of the keys that begin with the prefix, the left-th largest
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < 256 * COPIES; i += kThreads) (&hist[0][0])[i] = 0;
-        __syncthreads();
-        for (int t = from + lane; t < to; t += kWave) {
-            const uint32_t k = keys[t];
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u][lane % COPIES], 1u);
-        }
-        __syncthreads();
-        if (wave < 4) {  // digit 255 - threadIdx.x: those above it come first
-            const int d = 255 - threadIdx.x;
-            int n = 0;
+    const int turns = (L + kWaves * kTurn - 1) / (kWaves * kTurn), from = min(L, wave * turns * kTurn), to = min(L, from + turns * kTurn);
+    // ---- the keys; rows up to a whole turn that there are not stay ----
+    for (int t0 = from; t0 < to; t0 += 2 * kTurn) {
+        float x[8];
+        int p[8];
 #pragma unroll
-            for (int c = 0; c < COPIES; ++c) n += (int)hist[d][(c + d) % COPIES];
-            int incl = wave_scan_i(n);
-            if (lane == kWave - 1) lds[wave] = incl;
-            hist[d][0] = (uint32_t)incl;
-            hist[d][1] = (uint32_t)n;
+        for (int i = 0; i < 8; ++i) {
+            const int t = t0 + i * kWave + lane;
+            x[i] = t < to ? tally[t] : 0.f;
+            p[i] = t < to ? position(t) : -0x7fffffff;
         }
-        __syncthreads();
-        if (wave < 4) {
-            const int d = 255 - threadIdx.x, n = (int)hist[d][1];
-            int incl = (int)hist[d][0];
-            for (int w = 0; w < wave; ++w) incl += lds[w];
-            if (incl >= left && incl - n < left) found[0] = d, found[1] = left - (incl - n);
-        }
-        __syncthreads();
-        prefix |= (uint32_t)found[0] << shift;
-        left = found[1];
-    }
-    // keys above the prefix stay, and of those equal to it the first `left`
-    int mine = 0;
-    for (int t0 = from; t0 < to; t0 += kWave) mine += __popcll(__ballot(t0 + lane < to && keys[min(t0 + lane, L - 1)] == prefix));
-    int equal;
-    wave_offsets(mine, lds, equal);
-    // rows before `keep` that go, and rows behind it that stay: a wave's numbers, then their places
-    int n_holes = 0, n_movers = 0, holes, movers;
-    for (int round = 0; round < 2; ++round) {
-        int eq = equal, h = 0, m = 0;
-        for (int t0 = from; t0 < to; t0 += kWave) {
-            const int t = t0 + lane;
-            const bool real = t < to;
-            const uint32_t k = real ? keys[t] : 0u;
-            const uint64_t same = __ballot(real && k == prefix);
-            const int rank = eq + __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0u));
-            const bool stays = real && (k > prefix || (k == prefix && rank < left));
-            const bool hole = real && t < a.keep && !stays, mover = t >= a.keep && stays;
-            const uint64_t hm = __ballot(hole), mm = __ballot(mover);
-            if (round) {
-                if (hole) a.pairs[bh * a.most + holes + h + __builtin_amdgcn_mbcnt_hi((uint32_t)(hm >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hm, 0u))].y = t;
-                if (mover) a.pairs[bh * a.most + movers + m + __builtin_amdgcn_mbcnt_hi((uint32_t)(mm >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mm, 0u))].x = t;
-                if (stays && t < a.keep && t >= known) pos[t] = position(t);
-            }
-            eq += __popcll(same);
-            h += __popcll(hm);
-            m += __popcll(mm);
-        }
-        if (!round) {
-            n_holes = wave_offsets(h, lds, holes);
-            n_movers = wave_offsets(m, lds, movers);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = t0 + i * kWave + lane;
+            const uint32_t k = p[i] < a.first || p[i] >= total - a.recent ? kStays : x[i] != x[i] ? 0u : float_to_key(x[i]);
+            if (i < 4 || t0 + kTurn < to) keys[t] = t < to ? k : kStays;
         }
     }
-    (void)n_holes;  // as many as movers
-    if (threadIdx.x == 0) a.count[bh] = n_movers;
+    for (int i = threadIdx.x; i < kBins * kCopies; i += kThreads) (&hist[0][0])[i] = 0;
     __syncthreads();
+    auto load4 = [&](int t0) { return *reinterpret_cast<const uint4 *>(keys + t0 + 4 * lane); };
+    int n_movers;
+    if (HELD > 0 && n_go <= kFewGo) {
+        int gone[kFewGo];
+#pragma unroll
+        for (int i = 0; i < kFewGo; ++i) {
+            gone[i] = 0x7fffffff;
+            if (i >= n_go) continue;
+            // the smallest key, and of equal ones the last row (never a kStays: more rows than n_go are not protected)
+            uint32_t k = kStays;
+            int at = -1;
+            for (int t0 = from; t0 < to; t0 += kTurn) {
+                const uint4 x = load4(t0);
+                const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (v[c] <= k && v[c] != kStays) k = v[c], at = t0 + 4 * lane + c;
+            }
+            const uint32_t wk = wave_reduce(k, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+            const uint32_t wt = wave_reduce(k == wk ? (uint32_t)(at + 1) : 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+            if (lane == 0) least[i & 1][wave][0] = wk, least[i & 1][wave][1] = wt;
+            __syncthreads();
+            uint32_t gk = kStays, gt = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t x = least[i & 1][w][0], t = least[i & 1][w][1];
+                if (x < gk || (x == gk && t > gt)) gk = x, gt = t;
+            }
+            gone[i] = (int)gt - 1;
+            if (gone[i] >= from && gone[i] < to) keys[gone[i]] = kStays;  // (its own wave, which alone looks at it)
+        }
+        // every thread has all of them: thread i works out the i-th hole and the i-th mover
+        n_movers = 0;
+#pragma unroll
+        for (int i = 0; i < kFewGo; ++i) n_movers += gone[i] < a.keep;
+        if (threadIdx.x < kFewGo) {
+#pragma unroll
+            for (int i = 0; i < kFewGo; ++i) {  // hole: as many smaller ones as this thread's number
+                int rank = 0;
+#pragma unroll
+                for (int j = 0; j < kFewGo; ++j) rank += gone[j] < gone[i];
+                if (gone[i] < a.keep && rank == (int)threadIdx.x) few[threadIdx.x].y = gone[i];
+            }
+            const int t = a.keep + (int)threadIdx.x;
+            int rank = 0;
+            bool stays = t < L;
+#pragma unroll
+            for (int j = 0; j < kFewGo; ++j) stays &= gone[j] != t, rank += gone[j] >= a.keep && gone[j] < t;
+            if (stays) few[(int)threadIdx.x - rank].x = t;
+        }
+        for (int t = known + threadIdx.x; t < a.keep; t += kThreads) {
+            bool hole = false;
+#pragma unroll
+            for (int i = 0; i < kFewGo; ++i) hole |= gone[i] == t;
+            if (!hole) pos[t] = before + (t - known);
+        }
+    } else {
+        // ---- the keep-th largest key ----
+        uint32_t prefix = 0;
+        int left = a.keep + (kTurn - 1 - (L + kTurn - 1) % kTurn);  // of the keys that begin with the prefix, the left-th largest (rows that there are not count in)
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+            for (int t0 = from; t0 < to; t0 += kTurn) {
+                const uint4 x = load4(t0);
+                const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (pass == 0 || (v[c] >> (shift + bits)) == (prefix >> (shift + bits))) atomicAdd(&hist[(v[c] >> shift) & ((1u << bits) - 1u)][lane % kCopies], 1u);
+            }
+            __syncthreads();
+            // the bins from the top, two a thread, which leaves them empty for the next pass
+            int n[2], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t *const bin = hist[kBins - 1 - (2 * threadIdx.x + i)];
+                n[i] = 0;
+#pragma unroll
+                for (int c = 0; c < kCopies; ++c) n[i] += (int)bin[c], bin[c] = 0;
+                sum += n[i];
+            }
+            const int incl = wave_scan_i(sum);
+            int above;
+            wave_offsets(__builtin_amdgcn_readlane(incl, kWave - 1), lds[pass], above);
+            above += incl - sum;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (above < left && above + n[i] >= left) found[0] = kBins - 1 - (2 * threadIdx.x + i), found[1] = left - above;
+                above += n[i];
+            }
+            __syncthreads();
+            prefix |= (uint32_t)found[0] << shift;
+            left = found[1];
+        }
+        // Keys above the prefix stay, and of those equal to it the first `left`.  How many there are of both, before row `keep` and behind it, wave by wave:
+        // where each wave's holes (rows before `keep` that go) and movers (rows behind it that stay) come.
+        int4 mine = make_int4(0, 0, 0, 0);
+        for (int t0 = from; t0 < to; t0 += kTurn) {
+            const uint4 x = load4(t0);
+            const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int t = t0 + 4 * lane + c, above = v[c] > prefix, same = v[c] == prefix;
+                if (t < a.keep) mine.x += above, mine.y += same;
+                else if (t < L) mine.z += above, mine.w += same;
+            }
+        }
+        mine.x = wave_sum_i(mine.x), mine.y = wave_sum_i(mine.y), mine.z = wave_sum_i(mine.z), mine.w = wave_sum_i(mine.w);
+        if (lane == 0) counts[wave] = mine;
+        __syncthreads();
+        int eq = 0, holes = 0, movers = 0, e = 0;
+        n_movers = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            const int4 c = counts[w];
+            if (w == wave) eq = e, movers = n_movers;
+            const int f = min(L, w * turns * kTurn), before_keep = max(0, min(a.keep, min(L, f + turns * kTurn)) - f);
+            const int kept0 = max(0, min(left - e, c.y)), kept1 = max(0, min(left - e - c.y, c.w));
+            if (w < wave) holes += before_keep - c.x - kept0;
+            n_movers += c.z + kept1;
+            e += c.y + c.w;
+        }
+        int2 *const to_pairs = n_movers <= kMovedHere ? few : pairs;
+        for (int t0 = from; t0 < to; t0 += kTurn) {
+            const uint4 x = load4(t0);
+            const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+            const int t = t0 + 4 * lane;
+            uint64_t same[4];
+            int n_same = 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) same[c] = __ballot(v[c] == prefix && t + c < L), n_same += __popcll(same[c]);
+            bool stays[4];
+            int rank = eq;
+            if (eq < left && eq + n_same > left) {  // (the turn in which the equal ones that stay end)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) rank += lanes_below(same[c]);
+            } else if (eq >= left) {
+                rank = left;
+            } else {
+                rank = left - 4;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                stays[c] = v[c] > prefix || (v[c] == prefix && rank < left);
+                rank += v[c] == prefix;
+            }
+            eq += n_same;
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                if (side == 0 ? t0 >= a.keep : t0 + kTurn <= a.keep) continue;
+                uint64_t out[4];
+                int at = side == 0 ? holes : movers, all = 0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    out[c] = __ballot(t + c < L && (side == 0 ? t + c < a.keep && !stays[c] : t + c >= a.keep && stays[c]));
+                    at += lanes_below(out[c]);
+                    all += __popcll(out[c]);
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if ((out[c] >> lane) & 1) {
+                        if (side == 0) to_pairs[at].y = t + c;
+                        else to_pairs[at].x = t + c;
+                        ++at;
+                    }
+                if (side == 0) holes += all;
+                else movers += all;
+            }
+            if (t0 < a.keep && t0 + kTurn > known)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (stays[c] && t + c < a.keep && t + c >= known) pos[t + c] = before + (t + c - known);
+        }
+    }
+    __syncthreads();
+    const bool here = n_movers <= kMovedHere;
     for (int i = threadIdx.x; i < n_movers; i += kThreads) {
-        const int2 p = a.pairs[bh * a.most + i];
+        const int2 p = here ? few[i] : pairs[i];
         tally[p.y] = tally[p.x];
         pos[p.y] = position(p.x);
     }
-}
-
-struct MoveParams {
-    char *rows[4];   // K and V, or their codes and scale bytes
-    int row_bytes[4];
-    int n;
-    const int2 *pairs;
-    const int32_t *count, *state;
-    int32_t *len, *mark;
-    long most;
-    int Hkv, Tcap, keep;
-};
-
-// pieces of U bytes
-template <typename U>
-__device__ __forceinline__ void move_rows(char *rows, int bytes, const int2 *pairs, int n, int part, int parts)
-{
-    const int per = bytes / (int)sizeof(U);
-    for (long i = (long)part * blockDim.x + threadIdx.x; i < (long)n * per; i += (long)parts * blockDim.x) {
-        const int2 p = pairs[i / per];
-        const int c = (int)(i % per);
-        reinterpret_cast<U *>(rows + (long)p.y * bytes)[c] = reinterpret_cast<const U *>(rows + (long)p.x * bytes)[c];
+    if (here) move_all(a.moved, (long)bh * a.Tcap, few, n_movers, threadIdx.x, kThreads);
+    if (threadIdx.x == 0) {
+        a.count[bh] = here ? 0 : n_movers;
+        // the last of the sequence's workgroups, all of which have read its length by now
+        if (atomicAdd(a.arrived + b, 1u) == (uint32_t)a.Hkv - 1u) {
+            a.arrived[b] = 0u;
+            a.len[b] = a.keep;
+            a.mark[2 * b] = a.keep;
+            a.mark[2 * b + 1] = total;
+        }
     }
 }
 
-__global__ __launch_bounds__(256) void evict_move_kernel(const MoveParams a)
+__global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams a)
 {
-    const int bh = blockIdx.y, b = bh / a.Hkv;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && bh == b * a.Hkv && a.state[2 * b] >= 0) {
-        a.len[b] = a.keep;
-        a.mark[2 * b] = a.keep;
-        a.mark[2 * b + 1] = a.state[2 * b + 1];
-    }
-    const int n = a.count[bh];
-    const int2 *pairs = a.pairs + bh * a.most;
-    for (int i = 0; i < a.n; ++i) {
-        char *rows = a.rows[i] + (long)bh * a.Tcap * a.row_bytes[i];
-        if (a.row_bytes[i] % 16 == 0) move_rows<uint4>(rows, a.row_bytes[i], pairs, n, blockIdx.x, gridDim.x);
-        else move_rows<uint16_t>(rows, a.row_bytes[i], pairs, n, blockIdx.x, gridDim.x);
-    }
+    const int bh = blockIdx.y;
+    move_all(a.moved, (long)bh * a.Tcap, a.pairs + bh * a.most, a.count[bh], (long)blockIdx.x * blockDim.x + threadIdx.x, (long)gridDim.x * blockDim.x);
 }
 
 struct EvictLayout {
-    size_t state, count, pairs, keys, total;
-    long most;
+    size_t count, pairs, keys, total;
+    long most, key_row;
 };
 static EvictLayout evict_layout(const rs_shape *s, int keep)
 {
     EvictLayout x;
     const size_t BH = (size_t)s->B * s->Hkv;
     x.most = keep < s->Tcap - keep ? keep : s->Tcap - keep;
-    x.state = RS_WS_CTRL_BYTES;
-    x.count = x.state + align256((size_t)s->B * 8);
+    x.key_row = s->Tcap > kMostHeld ? ((long)s->Tcap + kTurn - 1) / kTurn * kTurn : 0;
+    x.count = RS_WS_CTRL_BYTES;
     x.pairs = x.count + align256(BH * 4);
     x.keys = x.pairs + align256(BH * (size_t)x.most * 8);
-    x.total = x.keys + align256(BH * (size_t)s->Tcap * 4);
+    x.total = x.keys + BH * (size_t)x.key_row * 4;
     return x;
 }
 
@@ -201,11 +351,11 @@ static int check_evict(const rs_shape *s, int keep)
     const int st = check_rows(s, false);
     if (st != RS_OK) return st;
     if (keep < 1 || keep > s->Tcap) return RS_INVALID_ARG;
-    return (long)s->B * s->Hkv > 65535 || s->Tcap > (1 << 30) ? RS_UNSUPPORTED : RS_OK;
+    return (long)s->B * s->Hkv > 65535 || s->B > 2 * kMaxUnits || s->Tcap > (1 << 30) ? RS_UNSUPPORTED : RS_OK;
 }
 
-static int evict_run(const rs_shape *s, MoveParams m, float *tally, int32_t *pos, int32_t *mark, int32_t *len, int keep, int first, int recent, int slack,
-                     void *ws, size_t ws_bytes, hipStream_t stream)
+static int evict_run(const rs_shape *s, const MovedRows &m, float *tally, int32_t *pos, int32_t *mark, int32_t *len, int keep, int first, int recent,
+                     int slack, void *ws, size_t ws_bytes, hipStream_t stream)
 {
     for (const void *x : {(const void *)tally, (const void *)pos, (const void *)mark, (const void *)len})
         if (!x || !aligned16(x)) return RS_INVALID_ARG;
@@ -216,15 +366,17 @@ static int evict_run(const rs_shape *s, MoveParams m, float *tally, int32_t *pos
     if (!ws || !aligned16(ws) || ws_bytes < x.total) return RS_WORKSPACE_TOO_SMALL;
     char *const w = (char *)ws;
     const int BH = s->B * s->Hkv;
-    const EvictParams a{tally, pos, mark, len, (int32_t *)(w + x.state), (int32_t *)(w + x.count), (int2 *)(w + x.pairs), (uint32_t *)(w + x.keys), x.most,
-                        s->Hkv, s->Tcap, keep, first, recent, slack};
-    evict_select_kernel<<<BH, kThreads, 0, stream>>>(a);
-    m.pairs = a.pairs, m.count = a.count, m.state = a.state, m.len = len, m.mark = mark, m.most = x.most;
-    m.Hkv = s->Hkv, m.Tcap = s->Tcap, m.keep = keep;
+    const EvictParams a{tally, pos, mark, len, (int32_t *)(w + x.count), (uint32_t *)ws + kCtrlUnit0, (int2 *)(w + x.pairs), (uint32_t *)(w + x.keys),
+                        x.most, x.key_row, m, s->Hkv, s->Tcap, keep, first, recent, slack};
+    if (s->Tcap <= 8704) evict_select_kernel<8704><<<BH, kThreads, 0, stream>>>(a);
+    else if (s->Tcap <= 17408) evict_select_kernel<17408><<<BH, kThreads, 0, stream>>>(a);
+    else if (s->Tcap <= kMostHeld) evict_select_kernel<kMostHeld><<<BH, kThreads, 0, stream>>>(a);
+    else evict_select_kernel<0><<<BH, kThreads, 0, stream>>>(a);
+    if (x.most <= kMovedHere) return launch_status();  // no call on this cache has more to move
     // about 2048 workgroups, and not more than have 4 KB to move
-    long parts = (2048 + BH - 1) / BH, need = (x.most * m.row_bytes[0] + 4095) / 4096;
+    long parts = (2048 + BH - 1) / BH, need = (x.most * m.bytes[0] + 4095) / 4096;
     if (parts > need) parts = need < 1 ? 1 : need;
-    evict_move_kernel<<<dim3((unsigned)parts, (unsigned)BH), 256, 0, stream>>>(m);
+    evict_move_kernel<<<dim3((unsigned)parts, (unsigned)BH), 256, 0, stream>>>(a);
     return launch_status();
 }
 
@@ -241,11 +393,11 @@ int32_t cache_evict(const rs_shape *s, void *k_cache, void *v_cache, float *tall
 {
     const int st = check_evict(s, n_keep);
     if (st != RS_OK) return st;
-    MoveParams m = {};
+    MovedRows m = {};
     const int row = s->D * (int)esize(s->dtype);
     m.n = 2;
     m.rows[0] = (char *)k_cache, m.rows[1] = (char *)v_cache;
-    m.row_bytes[0] = m.row_bytes[1] = row;
+    m.bytes[0] = m.bytes[1] = row;
     return evict_run(s, m, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws, ws_bytes, (hipStream_t)stream);
 }
 
@@ -254,11 +406,11 @@ int32_t kv4_evict(const rs_shape *s, uint8_t *k4, uint8_t *k4_scale, uint8_t *v4
 {
     const int st = check_evict(s, n_keep);
     if (st != RS_OK) return st;
-    MoveParams m = {};
+    MovedRows m = {};
     m.n = 4;
     m.rows[0] = (char *)k4, m.rows[1] = (char *)v4, m.rows[2] = (char *)k4_scale, m.rows[3] = (char *)v4_scale;
-    m.row_bytes[0] = m.row_bytes[1] = s->D / 2;
-    m.row_bytes[2] = m.row_bytes[3] = s->D / 32;
+    m.bytes[0] = m.bytes[1] = s->D / 2;
+    m.bytes[2] = m.bytes[3] = s->D / 32;
     return evict_run(s, m, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws, ws_bytes, (hipStream_t)stream);
 }
 
