@@ -102,6 +102,7 @@ SIGNATURES = {
 # those of them that native.cpp takes apart too, in the order in which it is told their addresses
 _POOL_CALLS = ("page_pool_reserve", "page_pool_fork", "page_pool_free", "page_pool_compact", "page_pool_share", "page_copy",
                "rat_state_copy", "rat_append_paged", "attn_paged")
+_CACHE_CALLS = ("kv4_append", "kv4_page_meta", "kv4_fetch", "kv4_attn_decode", "attn_decode_tally", "cache_evict", "kv4_evict")
 
 
 def load():
@@ -123,6 +124,7 @@ def load():
         native.setup(*(ctypes.cast(getattr(lib, name), _vp).value for name in ("rat_scan", "sparse_attn_decode", "rat_decode_step")),
                      _check, torch._C._cuda_getCurrentRawStream, torch.cuda.current_device, rs_shape, Workspace)
         native.setup_pool(*(ctypes.cast(getattr(lib, name), _vp).value for name in _POOL_CALLS), rs_pool)
+        native.setup_cache(*(ctypes.cast(getattr(lib, name), _vp).value for name in _CACHE_CALLS))
         _native = native
         _lib = lib  # last: another thread that finds it set goes on without a look at the rest
     return _lib
@@ -473,6 +475,8 @@ def _bounds(s, meta):
 
 def kv4_append(s, k, v, t_src, len, n_new, T_new, k4, k4_scale, v4, v4_scale, meta):
     """k, v [B, Hkv, T_src, D]: the new tokens are rows t_src .. t_src + T_new - 1."""
+    if _calls().kv4_append(s, k, v, t_src, len, n_new, T_new, k4, k4_scale, v4, v4_scale, meta):
+        return
     T_src = k.shape[2] if k.dim() == 4 else 0
     src = (_type(s), s.B, s.Hkv, T_src, s.D)
     _check(load().kv4_append(ctypes.byref(s), _need(k, *src), _need(v, *src), T_src, t_src, _need(len, torch.int32, s.B), _need(n_new, torch.int32, s.B),
@@ -480,12 +484,16 @@ def kv4_append(s, k, v, t_src, len, n_new, T_new, k4, k4_scale, v4, v4_scale, me
 
 
 def kv4_page_meta(s, k4, k4_scale, len, n_new, T_new, meta):
+    if _calls().kv4_page_meta(s, k4, k4_scale, len, n_new, T_new, meta):
+        return
     kc, ks, _, _ = _four(s, k4, k4_scale, None, None)
     _check(load().kv4_page_meta(ctypes.byref(s), kc, ks, _need(len, torch.int32, s.B), _need(n_new, torch.int32, s.B), T_new, _bounds(s, meta),
                                 _stream()))
 
 
 def kv4_fetch(s, k4, k4_scale, v4, v4_scale, len, t0, T, k_out, v_out):
+    if _calls().kv4_fetch(s, k4, k4_scale, v4, v4_scale, len, t0, T, k_out, v_out):
+        return
     to = (_type(s), s.B, s.Hkv, T, s.D)
     _check(load().kv4_fetch(ctypes.byref(s), *_four(s, k4, k4_scale, v4, v4_scale), _need(len, torch.int32, s.B), t0, T, _need(k_out, *to),
                             _need(v_out, *to), _stream()))
@@ -497,6 +505,8 @@ def kv4_attn_decode_workspace_bytes(s, H_idx, K, with_tally):
 
 def kv4_attn_decode(s, q, k4, k4_scale, v4, v4_scale, len, scale, idx, tally, n_fresh, out, lse_out, ws):
     """idx: [B, Hq or Hkv, K] pages or None."""
+    if _calls().kv4_attn_decode(s, q, k4, k4_scale, v4, v4_scale, len, scale, idx, tally, n_fresh, out, lse_out, ws):
+        return
     H, K = (idx.shape[1], idx.shape[2]) if idx is not None and idx.dim() == 3 else (0, 0)
     rows = (s.B, s.Hq)
     _check(load().kv4_attn_decode(ctypes.byref(s), _need(q, _type(s), *rows, s.D), *_four(s, k4, k4_scale, v4, v4_scale), _need(len, torch.int32, s.B),
@@ -509,6 +519,8 @@ def attn_decode_tally_workspace_bytes(s):
 
 
 def attn_decode_tally(s, q, k_cache, v_cache, len, scale, tally, n_fresh, out, lse_out, ws):
+    if _calls().attn_decode_tally(s, q, k_cache, v_cache, len, scale, tally, n_fresh, out, lse_out, ws):
+        return
     dt, rows, cache = _type(s), (s.B, s.Hq), (s.B, s.Hkv, s.Tcap)
     _check(load().attn_decode_tally(ctypes.byref(s), _need(q, dt, *rows, s.D), _need(k_cache, dt, *cache, s.D), _need(v_cache, dt, *cache, s.D),
                                     _need(len, torch.int32, s.B), scale, _need(tally, torch.float32, *cache), n_fresh, _need(out, dt, *rows, s.D),
@@ -525,11 +537,15 @@ def _kept(s, tally, pos, mark, len):
 
 
 def cache_evict(s, k_cache, v_cache, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws):
+    if _calls().cache_evict(s, k_cache, v_cache, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws):
+        return
     rows = (_type(s), s.B, s.Hkv, s.Tcap, s.D)
     _check(load().cache_evict(ctypes.byref(s), _need(k_cache, *rows), _need(v_cache, *rows), *_kept(s, tally, pos, mark, len), n_keep, n_first, n_recent,
                               n_slack, *_scratch(ws), _stream()))
 
 
 def kv4_evict(s, k4, k4_scale, v4, v4_scale, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws):
+    if _calls().kv4_evict(s, k4, k4_scale, v4, v4_scale, tally, pos, mark, len, n_keep, n_first, n_recent, n_slack, ws):
+        return
     _check(load().kv4_evict(ctypes.byref(s), *_four(s, k4, k4_scale, v4, v4_scale), *_kept(s, tally, pos, mark, len), n_keep, n_first, n_recent, n_slack,
                             *_scratch(ws), _stream()))

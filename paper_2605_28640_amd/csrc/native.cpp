@@ -1,4 +1,4 @@
-// The per-token calls of the binding (append, decode, replayable step, those around a pool of pages) with their arguments taken apart in C++: ctypes and a
+// The per-token calls of the binding (append, decode, replayable step, those around a pool of pages, a 4-bit cache and eviction) with their arguments taken apart in C++: ctypes and a
 // Python function per tensor cost the host more than the launch itself.  Only arguments of exactly the types that a program
 // ordinarily passes are taken here: rs_shape, contiguous device tensors (torch.Tensor or Parameter) or None, int, float, Workspace.
 // Anything else leaves the call unmade and the function answers False: binding.py then makes it through ctypes, which
@@ -27,6 +27,13 @@ decltype(&page_copy) f_copy;
 decltype(&rat_state_copy) f_state;
 decltype(&rat_append_paged) f_append;
 decltype(&attn_paged) f_attn;
+decltype(&kv4_append) f_kv4_append;
+decltype(&kv4_page_meta) f_kv4_meta;
+decltype(&kv4_fetch) f_kv4_fetch;
+decltype(&kv4_attn_decode) f_kv4_attn;
+decltype(&attn_decode_tally) f_tally;
+decltype(&cache_evict) f_evict;
+decltype(&kv4_evict) f_kv4_evict;
 PyObject *g_check, *g_stream_of, *g_device, *g_shape, *g_workspace;  // binding._check, torch's two, binding.rs_shape, .Workspace
 PyObject *g_pool;                                                    // binding.rs_pool
 PyObject *s_buf;
@@ -419,6 +426,143 @@ PyObject *py_setup_pool(PyObject *, PyObject *const *a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// ---- a cache in 4 bits, and caches that give up rows ----
+struct Four {
+    uint8_t *k, *ks, *v, *vs;
+};
+uint8_t *bytes(Args &x, const rs_shape &s, int i, int channels) { return (uint8_t *)x.typed(i, at::kByte, {s.B, s.Hkv, s.Tcap, s.D / channels}); }
+Four four(Args &x, const rs_shape &s, int i) { return Four{bytes(x, s, i, 2), bytes(x, s, i + 1, 32), bytes(x, s, i + 2, 2), bytes(x, s, i + 3, 32)}; }
+void *bounds(Args &x, const rs_shape &s, int i) { return x.typed(i, type_of(s), {s.B, s.Hkv, s.P > 0 ? s.Tcap / s.P : 0, 2, s.D}); }
+float *per_row(Args &x, const rs_shape &s, int i) { return (float *)x.typed(i, at::kFloat, {s.B, s.Hkv, s.Tcap}); }
+
+PyObject *py_kv4_append(PyObject *, PyObject *const *a, Py_ssize_t na)
+{
+    if (!expect(na, 12)) return nullptr;
+    Args x{a};
+    const rs_shape s = x.shape(0);
+    const int64_t T_src = x.size(1, 2), t_src = x.integer(3);
+    const void *k = x.typed(1, type_of(s), {s.B, s.Hkv, T_src, s.D}), *v = x.typed(2, type_of(s), {s.B, s.Hkv, T_src, s.D});
+    const int32_t *len = x.ints(4, {s.B}), *n_new = x.ints(5, {s.B});
+    const int T = (int)x.integer(6);
+    const Four c = four(x, s, 7);
+    void *meta = bounds(x, s, 11);
+    return run(x, [&](void *st) { return f_kv4_append(&s, k, v, T_src, t_src, len, n_new, T, c.k, c.ks, c.v, c.vs, meta, st); });
+}
+
+PyObject *py_kv4_page_meta(PyObject *, PyObject *const *a, Py_ssize_t na)
+{
+    if (!expect(na, 7)) return nullptr;
+    Args x{a};
+    const rs_shape s = x.shape(0);
+    const uint8_t *k = bytes(x, s, 1, 2), *ks = bytes(x, s, 2, 32);
+    const int32_t *len = x.ints(3, {s.B}), *n_new = x.ints(4, {s.B});
+    const int T = (int)x.integer(5);
+    void *meta = bounds(x, s, 6);
+    return run(x, [&](void *st) { return f_kv4_meta(&s, k, ks, len, n_new, T, meta, st); });
+}
+
+PyObject *py_kv4_fetch(PyObject *, PyObject *const *a, Py_ssize_t na)
+{
+    if (!expect(na, 10)) return nullptr;
+    Args x{a};
+    const rs_shape s = x.shape(0);
+    const Four c = four(x, s, 1);
+    const int32_t *len = x.ints(5, {s.B});
+    const int64_t t0 = x.integer(6);
+    const int T = (int)x.integer(7);
+    void *k = x.typed(8, type_of(s), {s.B, s.Hkv, T, s.D}), *v = x.typed(9, type_of(s), {s.B, s.Hkv, T, s.D});
+    return run(x, [&](void *st) { return f_kv4_fetch(&s, c.k, c.ks, c.v, c.vs, len, t0, T, k, v, st); });
+}
+
+PyObject *py_kv4_attn_decode(PyObject *, PyObject *const *a, Py_ssize_t na)
+{
+    if (!expect(na, 14)) return nullptr;
+    Args x{a};
+    const rs_shape s = x.shape(0);
+    const void *q = x.typed(1, type_of(s), {s.B, s.Hq, s.D});
+    const Four c = four(x, s, 2);
+    const int32_t *len = x.ints(6, {s.B});
+    const float scale = x.real(7);
+    const int64_t H = a[8] == Py_None ? 0 : x.size(8, 1), K = a[8] == Py_None ? 0 : x.size(8, 2);
+    const int32_t *idx = x.ints(8, {s.B, H, K});
+    float *tally = per_row(x, s, 9);
+    const int fresh = (int)x.integer(10);
+    void *out = x.typed(11, type_of(s), {s.B, s.Hq, s.D});
+    float *lse = (float *)x.typed(12, at::kFloat, {s.B, s.Hq});
+    size_t nb = 0;
+    void *ws = x.workspace(13, nb);
+    return run(x, [&](void *st) {
+        return f_kv4_attn(&s, q, c.k, c.ks, c.v, c.vs, len, scale, idx, (int)H, (int)K, tally, fresh, out, lse, ws, nb, st);
+    });
+}
+
+PyObject *py_attn_decode_tally(PyObject *, PyObject *const *a, Py_ssize_t na)
+{
+    if (!expect(na, 11)) return nullptr;
+    Args x{a};
+    const rs_shape s = x.shape(0);
+    const at::ScalarType dt = type_of(s);
+    const void *q = x.typed(1, dt, {s.B, s.Hq, s.D}), *k = x.typed(2, dt, {s.B, s.Hkv, s.Tcap, s.D}), *v = x.typed(3, dt, {s.B, s.Hkv, s.Tcap, s.D});
+    const int32_t *len = x.ints(4, {s.B});
+    const float scale = x.real(5);
+    float *tally = per_row(x, s, 6);
+    const int fresh = (int)x.integer(7);
+    void *out = x.typed(8, dt, {s.B, s.Hq, s.D});
+    float *lse = (float *)x.typed(9, at::kFloat, {s.B, s.Hq});
+    size_t nb = 0;
+    void *ws = x.workspace(10, nb);
+    return run(x, [&](void *st) { return f_tally(&s, q, k, v, len, scale, tally, fresh, out, lse, ws, nb, st); });
+}
+
+// what both evictions take after the cache: tally, pos, mark, len, the four numbers, the workspace
+template <typename F>
+PyObject *evict(Args &x, const rs_shape &s, int i, F f)
+{
+    float *tally = per_row(x, s, i);
+    int32_t *pos = x.ints(i + 1, {s.B, s.Hkv, s.Tcap}), *mark = x.ints(i + 2, {s.B, 2}), *len = x.ints(i + 3, {s.B});
+    const int keep = (int)x.integer(i + 4), first = (int)x.integer(i + 5), recent = (int)x.integer(i + 6), slack = (int)x.integer(i + 7);
+    size_t nb = 0;
+    void *ws = x.workspace(i + 8, nb);
+    return run(x, [&](void *st) { return f(tally, pos, mark, len, keep, first, recent, slack, ws, nb, st); });
+}
+
+PyObject *py_cache_evict(PyObject *, PyObject *const *a, Py_ssize_t na)
+{
+    if (!expect(na, 12)) return nullptr;
+    Args x{a};
+    const rs_shape s = x.shape(0);
+    void *k = x.typed(1, type_of(s), {s.B, s.Hkv, s.Tcap, s.D}), *v = x.typed(2, type_of(s), {s.B, s.Hkv, s.Tcap, s.D});
+    return evict(x, s, 3, [&](auto... more) { return f_evict(&s, k, v, more...); });
+}
+
+PyObject *py_kv4_evict(PyObject *, PyObject *const *a, Py_ssize_t na)
+{
+    if (!expect(na, 14)) return nullptr;
+    Args x{a};
+    const rs_shape s = x.shape(0);
+    const Four c = four(x, s, 1);
+    return evict(x, s, 5, [&](auto... more) { return f_kv4_evict(&s, c.k, c.ks, c.v, c.vs, more...); });
+}
+
+// setup_cache(the seven functions' addresses in the order of their definitions above)
+PyObject *py_setup_cache(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 7)) return nullptr;
+    Args x{a};
+    f_kv4_append = (decltype(f_kv4_append))x.integer(0);
+    f_kv4_meta = (decltype(f_kv4_meta))x.integer(1);
+    f_kv4_fetch = (decltype(f_kv4_fetch))x.integer(2);
+    f_kv4_attn = (decltype(f_kv4_attn))x.integer(3);
+    f_tally = (decltype(f_tally))x.integer(4);
+    f_evict = (decltype(f_evict))x.integer(5);
+    f_kv4_evict = (decltype(f_kv4_evict))x.integer(6);
+    if (!x.plain) {
+        PyErr_SetString(PyExc_TypeError, "setup_cache: seven addresses expected");
+        return nullptr;
+    }
+    Py_RETURN_NONE;
+}
+
 // setup(address of rat_scan, of sparse_attn_decode, of rat_decode_step, _check, stream of a device, current device,
 // rs_shape, Workspace)
 PyObject *py_setup(PyObject *, PyObject *const *a, Py_ssize_t n)
@@ -456,6 +600,14 @@ PyMethodDef methods[] = {{"setup", FAST(py_setup)},
                          {"rat_state_copy", FAST(py_rat_state_copy)},
                          {"rat_append_paged", FAST(py_rat_append_paged)},
                          {"attn_paged", FAST(py_attn_paged)},
+                         {"setup_cache", FAST(py_setup_cache)},
+                         {"kv4_append", FAST(py_kv4_append)},
+                         {"kv4_page_meta", FAST(py_kv4_page_meta)},
+                         {"kv4_fetch", FAST(py_kv4_fetch)},
+                         {"kv4_attn_decode", FAST(py_kv4_attn_decode)},
+                         {"attn_decode_tally", FAST(py_attn_decode_tally)},
+                         {"cache_evict", FAST(py_cache_evict)},
+                         {"kv4_evict", FAST(py_kv4_evict)},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -111,6 +111,14 @@ def test_workspaces():
 ])
 def test_signatures(name, names):
     assert list(inspect.signature(getattr(rs, name)).parameters) == names.split()
+    if name.endswith("_bytes"):
+        return
+    # as native.cpp takes it: the same number of arguments; what is not of its plain type is left unmade
+    fast, n = getattr(rs._calls(), name), len(names.split())
+    assert fast(*[0.5] * n) is False
+    for wrong in (n - 1, n + 1):
+        with pytest.raises(TypeError):
+            fast(*[None] * wrong)
 
 
 def test_binding_looks_at_types_and_shapes():
