@@ -2,11 +2,11 @@
 // same over whole or listed pages of a 4-bit cache.
 //   z_t = scale q . k_t,  m = max z,  l = sum e^(z_t - m),  out = sum e^(z_t - m) v_t / l,  tally_t += sum over a KV head's queries of e^(z_t - m) / l
 // Work: a tile is a KV head's (listed pages of a query head: the query head's) up to 16 queries of one sequence; its tokens, in units of 64, lie on a
-// line, tile after tile, sequence after sequence.  The line is divided evenly among the workgroups, whatever the lengths, which every
-// workgroup reads for itself.  A workgroup takes the units of its share four at a time, one a wave; the four waves' results are put
-// together in LDS, and are the tile's result or, where the line is cut inside the tile, a record that a second launch joins with the others.
-// The order of every sum follows from the lengths alone.  The tally needs the weights' sum over all tokens, so the scores (float32) go to
-// the workspace and the second launch turns them into weights.
+// line, tile after tile, sequence after sequence.  The line is divided evenly among the waves, whatever the lengths, which every workgroup reads
+// for itself.  A wave goes through its share without a pause: the next step's rows and, where a tile begins, its queries are on their way before
+// the present step is done.  A tile that lies in one share is done with it; one that is cut leaves records, which a second launch joins in their order
+// on the line (the four waves of a workgroup that is all inside one tile leave one).  So the order of every sum follows from the lengths alone.
+// The tally needs the weights' sum over all tokens, so the scores (float32) go to the workspace and the second launch turns them into weights.
 #include "check.h"
 #include "common.h"
 #include "kv4.h"
@@ -21,7 +21,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kQ = 16;         // queries of a tile, at most
 constexpr int kUnit = 64;      // tokens of a unit
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kGroups = 768;   // workgroups of the first launch, at most
 constexpr int kMaxB = 1024;
 constexpr float kSlack = 8.f;  // the reference point of a softmax moves when the maximum has grown by more (base-2 exponent): weights stay below 2^8
 
@@ -31,10 +30,10 @@ struct DecodeParams {
     const int32_t *len, *idx;
     void *out;
     float *lse, *tally;
-    float *rec_o, *rec_ml, *lse2, *z;  // records [2 kGroups, kQ, D], [.., 2]; base-2 log-sum-exps [B, Hq]; scores [B, Hq, z_row]
+    float *rec_o, *rec_ml, *lse2, *z;  // records [2 a wave, rows, D], [.., 2]; base-2 log-sum-exps [B, Hq]; scores [B, Hq, z_row]
     int *start;                   // [B + 1] units of the sequences before
     int B, Hq, Hkv, H, G, RT, D;  // H: heads with tiles of their own, G queries each, in RT tiles
-    int Tcap, K, shift, list_units, z_row, groups, fresh;
+    int Tcap, K, shift, list_units, z_row, groups, rows, fresh;
     float scale;
 };
 
@@ -57,73 +56,98 @@ __device__ __forceinline__ int length_of(const DecodeParams &a, int b)
     const int n = a.len[b];
     return n < 0 ? 0 : n > a.Tcap ? a.Tcap : n;
 }
-__device__ __forceinline__ int units_of(const DecodeParams &a, int b)
-{
-    const int n = length_of(a, b);
-    return a.idx ? (n > 0 ? a.list_units : 0) : (n + kUnit - 1) / kUnit;
-}
+__device__ __forceinline__ int units_of(const DecodeParams &a, int n) { return a.idx ? (n > 0 ? a.list_units : 0) : (n + kUnit - 1) / kUnit; }
 
-// the line's shares
+// the line's shares, one a wave
 struct LineShares {
     int total, n;
     __device__ __forceinline__ LineShares(int sum, int heads, int groups)
     {
         total = sum * heads;
-        n = (total + kWaves - 1) / kWaves;
-        if (n > groups) n = groups;
+        n = total < groups * kWaves ? total : groups * kWaves;
     }
     __device__ __forceinline__ int begin(int i) const { return (int)((long)i * total / n); }
     __device__ __forceinline__ int of(int unit) const { return (int)((((long)unit + 1) * n - 1) / total); }  // whose a unit is
 };
 
-// units of the sequences before each, in LDS
-__device__ __forceinline__ void make_start(const DecodeParams &a, int *start, int *wave_tot)
-{
-    constexpr int EACH = kMaxB / kThreads;
-    const int t = threadIdx.x, lane = lane_id(), wave = t / kWave;
-    int x[EACH], sum = 0;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int b = t * EACH + i;
-        x[i] = b < a.B ? units_of(a, b) : 0;
-        sum += x[i];
-    }
-    const int incl = wave_scan_i(sum);
-    if (lane == kWave - 1) wave_tot[wave] = incl;
-    __syncthreads();
-    int at = incl - sum;
-    for (int w = 0; w < wave; ++w) at += wave_tot[w];
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int b = t * EACH + i;
-        if (b <= a.B) start[b] = at;
-        at += x[i];
-    }
-    if (t == kThreads - 1 && a.B == kMaxB) start[kMaxB] = at;
-    __syncthreads();
-}
-
 struct LineTile {
-    int b, h, rt, s0, s1;  // sequence, head, 16 queries of it, its units on the line
+    int b, h, rt, s0, s1, L;  // sequence, head, 16 queries of it, its units on the line; tokens of the sequence
 };
-__device__ __forceinline__ LineTile find_tile(const DecodeParams &a, const int *start, int unit)
-{
-    const int HR = a.H * a.RT;
-    int lo = 0, hi = a.B;  // the last b with start[b] HR <= unit
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (scalar(start[mid]) * HR <= unit) lo = mid;
-        else hi = mid;
+
+// Where the sequences' units begin.  Up to 64 sequences: a lane of every wave each, nothing but the lengths' trip to memory; more: in LDS.
+struct LinePlan {
+    int first, units, len;  // of sequence lane_id()
+    const int *start;       // [B + 1] in LDS, or nullptr
+    int sum;
+
+    __device__ __forceinline__ void make(const DecodeParams &a, int *lds, int *wave_tot)
+    {
+        if (a.B <= kWave) {
+            const int b = lane_id();
+            len = b < a.B ? length_of(a, b) : 0;
+            units = units_of(a, len);
+            const int incl = wave_scan_i(units);
+            first = incl - units;
+            sum = __builtin_amdgcn_readlane(incl, kWave - 1);
+            start = nullptr;
+            return;
+        }
+        constexpr int EACH = kMaxB / kThreads;
+        const int t = threadIdx.x, lane = lane_id(), wave = t / kWave;
+        int x[EACH], all = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int b = t * EACH + i;
+            x[i] = b < a.B ? units_of(a, length_of(a, b)) : 0;
+            all += x[i];
+        }
+        const int incl = wave_scan_i(all);
+        if (lane == kWave - 1) wave_tot[wave] = incl;
+        __syncthreads();
+        int at = incl - all;
+        for (int w = 0; w < wave; ++w) at += wave_tot[w];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int b = t * EACH + i;
+            if (b <= a.B) lds[b] = at;
+            at += x[i];
+        }
+        if (t == kThreads - 1 && a.B == kMaxB) lds[kMaxB] = at;
+        __syncthreads();
+        start = lds;
+        sum = scalar(lds[a.B]);
     }
-    LineTile w;
-    const int first = scalar(start[lo]), n = scalar(start[lo + 1]) - first, hr = (unit - first * HR) / n;
-    w.b = lo;
-    w.h = hr / a.RT;
-    w.rt = hr - w.h * a.RT;
-    w.s0 = first * HR + hr * n;
-    w.s1 = w.s0 + n;
-    return w;
-}
+    __device__ __forceinline__ int begin(int b) const { return start ? start[b] : __shfl(first, b, kWave); }  // (b < B)
+    __device__ __forceinline__ LineTile find(const DecodeParams &a, int unit) const
+    {
+        const int HR = a.H * a.RT;
+        LineTile w;
+        int from, n;  // the last sequence that does not begin behind the unit
+        if (!start) {
+            w.b = 63 - __builtin_clzll(__ballot(lane_id() < a.B && first * HR <= unit));
+            from = __builtin_amdgcn_readlane(first, w.b);
+            n = __builtin_amdgcn_readlane(units, w.b);
+            w.L = __builtin_amdgcn_readlane(len, w.b);
+        } else {
+            int lo = 0, hi = a.B;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (scalar(start[mid]) * HR <= unit) lo = mid;
+                else hi = mid;
+            }
+            w.b = lo;
+            from = scalar(start[lo]);
+            n = scalar(start[lo + 1]) - from;
+            w.L = scalar(length_of(a, lo));
+        }
+        const int hr = (unit - from * HR) / n;
+        w.h = a.RT == 1 ? hr : hr / a.RT;
+        w.rt = a.RT == 1 ? 0 : hr - w.h * a.RT;
+        w.s0 = from * HR + hr * n;
+        w.s1 = w.s0 + n;
+        return w;
+    }
+};
 
 // the token row that a query's first 16 tokens of a unit begin at, and how many of them there are
 template <int NH>
@@ -357,8 +381,13 @@ __device__ __forceinline__ void put(const DecodeParams &a, long row, int c, cons
     }
 }
 
+// Waves to a SIMD that the registers are shared out for, and so workgroups of the first launch: all that are on the CUs together.  What the waves of
+// a CU have on their way decides (4 bits, 128 channels: 8.7 KB a wave in 168 registers).
+constexpr int occupancy(bool four, int bytes, int D) { return D == 64 ? (four && bytes == 4 ? 3 : 4) : four && bytes == 2 ? 3 : 2; }
+
 template <bool FOUR, typename ST, int D, bool LISTED, bool TALLY>
-__global__ __launch_bounds__(kThreads) void decode_attend_kernel(const DecodeParams a)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(occupancy(FOUR, sizeof(ST), D), occupancy(FOUR, sizeof(ST), D)))) void
+decode_attend_kernel(const DecodeParams a)
 {
     using R = StepRows<FOUR, ST, D>;
     constexpr int NH = R::NH, STEP = 16 * NH, SPU = kUnit / STEP, C4 = D / 4;
@@ -366,131 +395,175 @@ __global__ __launch_bounds__(kThreads) void decode_attend_kernel(const DecodePar
     __shared__ float ml[kWaves][kQ][2];
     __shared__ int start[kMaxB + 1];
     __shared__ int wave_tot[kWaves];
-    make_start(a, start, wave_tot);
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= a.B; b += kThreads) a.start[b] = start[b];
-    const LineShares sh(scalar(start[a.B]), a.H * a.RT, a.groups);
-    if ((int)blockIdx.x >= sh.n) return;
-    const int wave = scalar(threadIdx.x / kWave);
+    LinePlan plan;
+    plan.make(a, start, wave_tot);
+    const LineShares sh(plan.sum, a.H * a.RT, a.groups);
+    if (blockIdx.x == 0) {  // for the second launch
+        for (int b = threadIdx.x; b < a.B; b += kThreads) a.start[b] = plan.begin(b);
+        if (threadIdx.x == 0) a.start[a.B] = plan.sum;
+    }
+    const int wave = scalar(threadIdx.x / kWave), me = blockIdx.x * kWaves + wave;
+    if (me >= sh.n) return;  // (a workgroup with such a wave has no results put together)
+    const int u0 = sh.begin(me), n_steps = (sh.begin(me + 1) - u0) * SPU;
     R r;
     r.lane = lane_id(), r.l16 = r.lane & 15, r.lg = r.lane >> 4;
     char *const tile = tiles[wave];
     const float cs = a.scale * kLog2e;
-    int at = sh.begin(blockIdx.x);
-    const int end = sh.begin(blockIdx.x + 1);
-#pragma unroll 1
-    while (at < end) {
-        const LineTile w = find_tile(a, start, at);
-        const int from = at - w.s0, to = min(end, w.s1) - w.s0;  // the tile's units that are this workgroup's
-        at = w.s0 + to;
-        const int L = scalar(length_of(a, w.b)), rows = min(a.G - w.rt * kQ, kQ);
-        const long base = (long)(w.b * a.Hkv + w.h / (a.H / a.Hkv)) * a.Tcap;
-        const long row0 = (long)w.b * a.Hq + w.h * a.G + w.rt * kQ;  // of the queries
-        const bool real = r.l16 < rows;
+
+    auto base_of = [&](const LineTile &w) { return (long)(w.b * a.Hkv + w.h / (a.H / a.Hkv)) * a.Tcap; };
+    auto query_of = [&](const LineTile &w) { return (long)w.b * a.Hq + w.h * a.G + w.rt * kQ; };  // the first one's row
+    auto rows_of = [&](const LineTile &w) { return min(a.G - w.rt * kQ, kQ); };
+    auto token_of = [&](const LineTile &w, int i) { return (u0 + i / SPU - w.s0) * kUnit + i % SPU * STEP; };
+    auto look_up = [&](const LineTile &w, int i) -> StepWhere<NH> {  // (past the last step: no rows)
+        StepWhere<NH> x;
+        const int t = token_of(w, i);
         const int32_t *list = LISTED ? a.idx + (long)(w.b * a.H + w.h) * a.K : nullptr;
-        const int n_units = to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0, n_steps = n_units * SPU;
-        auto token_of = [&](int i) { return (from + wave + kWaves * (i / SPU)) * kUnit + i % SPU * STEP; };
-        auto look_up = [&](int i) -> StepWhere<NH> {  // (past the last step: no rows)
-            StepWhere<NH> x;
-            const int t = token_of(i);
 #pragma unroll
-            for (int h = 0; h < NH; ++h) {
-                int row = t + 16 * h;
-                if constexpr (LISTED) {
-                    const int slot = row >> a.shift, page = i < n_steps && slot < a.K ? scalar(list[slot]) : -1;
-                    row = page < 0 || page >= (a.Tcap >> a.shift) ? a.Tcap : (page << a.shift) + (row & ((1 << a.shift) - 1));
-                }
-                const int left = L - row;
-                x.valid[h] = scalar(i >= n_steps || left < 0 ? 0 : left < 16 ? left : 16);
-                x.at[h] = scalar(x.valid[h] ? row : 0);
+        for (int h = 0; h < NH; ++h) {
+            int row = t + 16 * h;
+            if constexpr (LISTED) {
+                const int slot = row >> a.shift, page = i < n_steps && slot < a.K ? scalar(list[slot]) : -1;
+                row = page < 0 || page >= (a.Tcap >> a.shift) ? a.Tcap : (page << a.shift) + (row & ((1 << a.shift) - 1));
             }
-            return x;
-        };
-        r.load_q((const ST *)a.q + (real ? row0 + r.l16 : row0) * D, real);
-        StepWhere<NH> x = look_up(0);
-        r.load_k(a, base, x);
-        r.load_v(a, base, x);
-        f32x4 o[D / 16];
+            const int left = w.L - row;
+            x.valid[h] = scalar(i >= n_steps || left < 0 ? 0 : left < 16 ? left : 16);
+            x.at[h] = scalar(x.valid[h] ? row : 0);
+        }
+        return x;
+    };
+    LineTile w = plan.find(a, u0);
+    StepWhere<NH> x = look_up(w, 0);
+    r.load_k(a, base_of(w), x);
+    r.load_q((const ST *)a.q + (query_of(w) + (r.l16 < rows_of(w) ? r.l16 : 0)) * D, r.l16 < rows_of(w));
+    r.load_v(a, base_of(w), x);
+    // all four shares of the workgroup in one tile: their results are put together
+    const bool together = (int)(blockIdx.x + 1) * kWaves <= sh.n && sh.begin(blockIdx.x * kWaves) >= w.s0 && sh.begin((blockIdx.x + 1) * kWaves) <= w.s1;
+    f32x4 o[D / 16];
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;
+    for (int dt = 0; dt < D / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
 #pragma unroll 1
-        for (int i = 0; i < n_steps; ++i) {
-            f32x4 s[NH];
+    for (int i = 0; i < n_steps; ++i) {
+        const int rows = rows_of(w);
+        const long q_row = query_of(w);
+        f32x4 s[NH];
 #pragma unroll
-            for (int h = 0; h < NH; ++h) s[h] = r.scores(h) * cs;
-            const StepWhere<NH> next = look_up(i + 1);
-            r.load_k(a, base, next);
-            float mx = -INFINITY;
-#pragma unroll
-            for (int h = 0; h < NH; ++h) {
-                const int sees = x.valid[h] - 4 * r.lg;  // of the lane's four
-                if (x.valid[h] < 16) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[h][j] = j < sees ? s[h][j] : -INFINITY;
-                }
-                if constexpr (TALLY) {
-                    if (real) *reinterpret_cast<f32x4 *>(a.z + (row0 + r.l16) * a.z_row + token_of(i) + 16 * h + 4 * r.lg) = s[h];
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[h][j]);
-            }
-            mx = quad_max(mx);
-            if (__any(mx - m > kSlack)) {  // (-inf from -inf compares false)
-                const float top = (mx - m > kSlack) ? mx : m, f = (m == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m - top);
-                l *= f;
-#pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) o[dt] *= f;
-                m = top;
-            }
-            const float bias = (m == -INFINITY) ? 0.f : m;
-#pragma unroll
-            for (int h = 0; h < NH; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[h][j] = __builtin_amdgcn_exp2f(s[h][j] - bias);
-                    l += s[h][j];
-                }
-            r.values(tile, s, o);
-            x = next;
-            r.load_v(a, base, x);
+        for (int h = 0; h < NH; ++h) s[h] = r.scores(h) * cs;
+        const bool ends = i + 1 == n_steps || u0 + (i + 1) / SPU >= w.s1;  // the tile, or the share
+        LineTile then = w;
+        if (ends && i + 1 < n_steps) {
+            then = plan.find(a, u0 + (i + 1) / SPU);
+            r.load_q((const ST *)a.q + (query_of(then) + (r.l16 < rows_of(then) ? r.l16 : 0)) * D, r.l16 < rows_of(then));
         }
-        // the four waves' parts
+        const StepWhere<NH> next = look_up(then, i + 1);
+        r.load_k(a, base_of(then), next);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const int sees = x.valid[h] - 4 * r.lg;  // of the lane's four
+            if (x.valid[h] < 16) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[h][j] = j < sees ? s[h][j] : -INFINITY;
+            }
+            if constexpr (TALLY) {
+                if (r.l16 < rows) *reinterpret_cast<f32x4 *>(a.z + (q_row + r.l16) * a.z_row + token_of(w, i) + 16 * h + 4 * r.lg) = s[h];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[h][j]);
+        }
+        mx = quad_max(mx);
+        if (__any(mx - m > kSlack)) {  // (-inf from -inf compares false)
+            const float top = (mx - m > kSlack) ? mx : m, f = (m == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            l *= f;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) o[dt] *= f;
+            m = top;
+        }
+        const float bias = (m == -INFINITY) ? 0.f : m;
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[h][j] = __builtin_amdgcn_exp2f(s[h][j] - bias);
+                l += s[h][j];
+            }
+        r.values(tile, s, o);
+        x = next;
+        r.load_v(a, base_of(then), x);
+        if (!ends) continue;
         l = quad_sum(l);
-        if (r.lg == 0) ml[wave][r.l16][0] = m, ml[wave][r.l16][1] = l;
+        if (!together) {
+            const int from = max(u0, w.s0), to = u0 + (i + 1) / SPU;
+            const long slot = 2l * me + (from == w.s0 ? 1 : 0);  // a tile that began in another share: the first of two records
+            if (r.l16 < rows) {
+                if (from == w.s0 && to == w.s1) {
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt)
-            *reinterpret_cast<f32x4 *>(tile + r.l16 * D * 4 + ((4 * dt + r.lg) ^ r.l16) * 16) = o[dt];
-        __syncthreads();
-        const bool whole = from == 0 && at == w.s1;
-        const long slot = 2l * blockIdx.x + (from == 0 ? 1 : 0);  // a tile that began in another share: the first of two records
-        for (int e = threadIdx.x; e < rows * C4; e += kThreads) {
-            const int row = e / C4, c4 = e % C4;
-            float top = -INFINITY, sum = 0.f;
+                    for (int dt = 0; dt < D / 16; ++dt) put<ST>(a, q_row + r.l16, 16 * dt + 4 * r.lg, o[dt], m, l);
+                } else {
 #pragma unroll
-            for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i][row][0]);
-            f32x4 out = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) {
-                const float mi = ml[i][row][0], li = ml[i][row][1];
-                if (mi == -INFINITY && li == 0.f) continue;  // saw nothing
-                const float f = mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
-                sum += li * f;
-                out += *reinterpret_cast<const f32x4 *>(tiles[i] + row * D * 4 + (c4 ^ row) * 16) * f;
+                    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4 *>(a.rec_o + (slot * a.rows + r.l16) * D + 16 * dt + 4 * r.lg) = o[dt];
+                    if (r.lg == 0) *reinterpret_cast<float2 *>(a.rec_ml + (slot * a.rows + r.l16) * 2) = make_float2(m, l);
+                }
             }
-            if (whole) {
-                put<ST>(a, row0 + row, 4 * c4, out, top, sum);
-            } else {
-                *reinterpret_cast<f32x4 *>(a.rec_o + (slot * kQ + row) * D + 4 * c4) = out;
-                if (c4 == 0) *reinterpret_cast<float2 *>(a.rec_ml + (slot * kQ + row) * 2) = make_float2(top, sum);
+            if (i + 1 < n_steps) {
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                m = -INFINITY, l = 0.f;
             }
         }
-        __syncthreads();
+        w = then;
+    }
+    if (!together) return;
+    if (r.lg == 0) ml[wave][r.l16][0] = m, ml[wave][r.l16][1] = l;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4 *>(tile + r.l16 * D * 4 + ((4 * dt + r.lg) ^ r.l16) * 16) = o[dt];
+    __syncthreads();
+    const bool whole = sh.begin(blockIdx.x * kWaves) == w.s0 && sh.begin((blockIdx.x + 1) * kWaves) == w.s1;
+    const long slot = 2l * kWaves * blockIdx.x;
+    for (int e = threadIdx.x; e < rows_of(w) * C4; e += kThreads) {
+        const int row = e / C4, c4 = e % C4;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i][row][0]);
+        f32x4 out = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            const float mi = ml[i][row][0], li = ml[i][row][1];
+            if (mi == -INFINITY && li == 0.f) continue;  // saw nothing
+            const float f = mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
+            sum += li * f;
+            out += *reinterpret_cast<const f32x4 *>(tiles[i] + row * D * 4 + (c4 ^ row) * 16) * f;
+        }
+        if (whole) {
+            put<ST>(a, query_of(w) + row, 4 * c4, out, top, sum);
+        } else {
+            *reinterpret_cast<f32x4 *>(a.rec_o + (slot * a.rows + row) * D + 4 * c4) = out;
+            if (c4 == 0) *reinterpret_cast<float2 *>(a.rec_ml + (slot * a.rows + row) * 2) = make_float2(top, sum);
+        }
     }
 }
 
-// the records of a tile: that of share first is its workgroup's second, those of the shares after it are their first
-__device__ __forceinline__ long record_of(int share, int first) { return 2l * share + (share == first ? 1 : 0); }
+// The records of the tile of units s0 .. s1 - 1, in their order: of single waves, of workgroups that are all inside it, of single waves.
+struct TileRecords {
+    int first, count, whole0, whole1;  // whole0 .. whole1 - 1: the workgroups inside
+
+    __device__ __forceinline__ TileRecords(const LineShares &sh, int s0, int s1)
+    {
+        first = sh.of(s0);
+        const int last = sh.of(s1 - 1);
+        const int from = sh.begin(first) >= s0 ? first : first + 1, to = sh.begin(last + 1) <= s1 ? last + 1 : last;  // shares inside
+        whole0 = (from + kWaves - 1) / kWaves, whole1 = to / kWaves;
+        if (whole0 >= whole1) whole0 = whole1 = 1 << 28;  // none
+        count = whole1 == 1 << 28 ? last - first + 1 : whole0 * kWaves - first + whole1 - whole0 + last + 1 - whole1 * kWaves;
+    }
+    __device__ __forceinline__ long slot(int i) const
+    {
+        const int singles = whole0 * kWaves - first;
+        if (i >= singles && i < singles + whole1 - whole0) return 2l * kWaves * (whole0 + i - singles);
+        const int share = i < singles ? first + i : whole1 * kWaves + i - (singles + whole1 - whole0);
+        return 2l * share + (share == first ? 1 : 0);
+    }
+};
 
 __device__ __forceinline__ void join(float &m, float &l, f32x4 &o, float m1, float l1, const f32x4 &o1)
 {
@@ -521,18 +594,18 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
             if (grp == 0) put<ST>(a, row, 4 * c4, o, m, l);
             return;
         }
-        const int first = sh.of(s0), last = sh.of(s0 + n - 1);
-        if (first == last) return;  // written as it is
+        const TileRecords rec(sh, s0, s0 + n);
+        if (rec.count == 1) return;  // written as it is
         constexpr int AHEAD = 4;
-        for (int i = first + grp; i <= last; i += AHEAD * NG) {
+        for (int i = grp; i < rec.count; i += AHEAD * NG) {
             float2 x[AHEAD];
             f32x4 v[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 x[j] = make_float2(-INFINITY, 0.f);
                 v[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (i + j * NG <= last) {
-                    const long at = record_of(i + j * NG, first) * kQ + r;
+                if (i + j * NG < rec.count) {
+                    const long at = rec.slot(i + j * NG) * a.rows + r;
                     x[j] = *reinterpret_cast<const float2 *>(a.rec_ml + at * 2);
                     v[j] = *reinterpret_cast<const f32x4 *>(a.rec_o + at * D + 4 * c4);
                 }
@@ -561,14 +634,15 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
         const int n_g = min(a.G - g0, kThreads);
         for (int i = wave; i < n_g; i += kWaves) {
             const int g = g0 + i, rt = g / kQ, r = g % kQ;
-            const int s0 = a.start[b] * HR + (h * a.RT + rt) * n, first = sh.of(s0), last = sh.of(s0 + n - 1);
+            const int s0 = a.start[b] * HR + (h * a.RT + rt) * n;
+            const TileRecords rec(sh, s0, s0 + n);
             float z;
-            if (first == last) {
+            if (rec.count == 1) {
                 z = a.lse2[(long)b * a.Hq + h * a.G + g];
             } else {
                 float m = -INFINITY, l = 0.f;
-                for (int x = first + lane; x <= last; x += kWave) {
-                    const float2 y = *reinterpret_cast<const float2 *>(a.rec_ml + (record_of(x, first) * kQ + r) * 2);
+                for (int x = lane; x < rec.count; x += kWave) {
+                    const float2 y = *reinterpret_cast<const float2 *>(a.rec_ml + (rec.slot(x) * a.rows + r) * 2);
                     f32x4 none = {0.f, 0.f, 0.f, 0.f};
                     join(m, l, none, y.x, y.y, none);
                 }
@@ -602,14 +676,21 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
 
 struct DecodeLayout {
     size_t ml, lse2, start, z, total;
-    int z_row;
+    int z_row, groups, rows;  // rows: of a record
 };
-static DecodeLayout decode_layout(const rs_shape *s, bool tally)
+// H, K: heads and pages of the lists; 0, 0: none
+static DecodeLayout decode_layout(const rs_shape *s, bool four, int H, int K, bool tally)
 {
     DecodeLayout x;
+    const int heads = H ? H : s->Hkv, G = s->Hq / heads;
+    x.rows = G < kQ ? G : kQ;
+    const long units = (long)s->B * heads * ((G + kQ - 1) / kQ) * (((H ? (long)K * s->P : (long)s->Tcap) + kUnit - 1) / kUnit);
+    const long most = 256l * occupancy(four, (int)esize(s->dtype), s->D), need = (units + kWaves - 1) / kWaves;
+    x.groups = (int)(need < most ? need : most);
+    const size_t records = (size_t)2 * x.groups * kWaves * x.rows;
     x.z_row = tally ? (s->Tcap + kUnit - 1) / kUnit * kUnit : 0;
-    x.ml = RS_WS_CTRL_BYTES + (size_t)2 * kGroups * kQ * s->D * 4;
-    x.lse2 = x.ml + (size_t)2 * kGroups * kQ * 8;
+    x.ml = RS_WS_CTRL_BYTES + align256(records * s->D * 4);
+    x.lse2 = x.ml + align256(records * 8);
     x.start = x.lse2 + align256((size_t)s->B * s->Hq * 4);
     x.z = x.start + align256((size_t)(s->B + 1) * 4);
     x.total = x.z + (size_t)s->B * s->Hq * x.z_row * 4;
@@ -646,7 +727,7 @@ static void decode_launch(const DecodeParams &a, hipStream_t stream)
 
 static int decode_run(const rs_shape *s, DecodeParams a, bool four, int H, int K, void *ws, hipStream_t stream)
 {
-    const DecodeLayout x = decode_layout(s, a.tally != nullptr);
+    const DecodeLayout x = decode_layout(s, four, H, K, a.tally != nullptr);
     char *const w = (char *)ws;
     a.rec_o = (float *)(w + RS_WS_CTRL_BYTES), a.rec_ml = (float *)(w + x.ml), a.lse2 = (float *)(w + x.lse2);
     a.start = (int *)(w + x.start), a.z = (float *)(w + x.z), a.z_row = x.z_row;
@@ -654,8 +735,7 @@ static int decode_run(const rs_shape *s, DecodeParams a, bool four, int H, int K
     a.H = a.idx ? H : s->Hkv, a.G = s->Hq / a.H, a.RT = (a.G + kQ - 1) / kQ, a.K = K;
     a.shift = a.idx ? __builtin_ctz((unsigned)s->P) : 0;
     a.list_units = a.idx ? (int)(((long)K * s->P + kUnit - 1) / kUnit) : 0;
-    const long most = (long)s->B * a.H * a.RT * (a.idx ? a.list_units : (s->Tcap + kUnit - 1) / kUnit);
-    a.groups = (int)((most + kWaves - 1) / kWaves < kGroups ? (most + kWaves - 1) / kWaves : kGroups);
+    a.groups = x.groups, a.rows = x.rows;
     const bool bf = s->dtype == RS_BF16;
     if (four) {
         if (bf && s->D == 128) decode_launch<true, bf16, 128>(a, stream);
@@ -679,7 +759,7 @@ extern "C" {
 
 size_t kv4_attn_decode_workspace_bytes(const rs_shape *s, int32_t H_idx, int32_t K, int32_t with_tally)
 {
-    return check_decode(s, H_idx, K) == RS_OK ? decode_layout(s, with_tally != 0).total : 0;
+    return check_decode(s, H_idx, K) == RS_OK ? decode_layout(s, true, H_idx, K, with_tally != 0).total : 0;
 }
 
 int32_t kv4_attn_decode(const rs_shape *s, const void *q, const uint8_t *k4, const uint8_t *k4_scale, const uint8_t *v4, const uint8_t *v4_scale,
@@ -694,14 +774,14 @@ int32_t kv4_attn_decode(const rs_shape *s, const void *q, const uint8_t *k4, con
     for (const void *x : {q, (const void *)k4, (const void *)k4_scale, (const void *)v4, (const void *)v4_scale, (const void *)len, (const void *)idx,
                           (const void *)tally, (const void *)out, (const void *)lse_out})
         if (!aligned16(x)) return RS_INVALID_ARG;
-    if (!ws || !aligned16(ws) || ws_bytes < decode_layout(s, tally != nullptr).total) return RS_WORKSPACE_TOO_SMALL;
+    if (!ws || !aligned16(ws) || ws_bytes < decode_layout(s, true, H_idx, K, tally != nullptr).total) return RS_WORKSPACE_TOO_SMALL;
     DecodeParams a = {};
     a.q = q, a.k = k4, a.v = v4, a.ks = k4_scale, a.vs = v4_scale, a.len = len, a.idx = idx, a.out = out, a.lse = lse_out, a.tally = tally;
     a.fresh = n_fresh, a.scale = scale;
     return decode_run(s, a, true, H_idx, K, ws, (hipStream_t)stream);
 }
 
-size_t attn_decode_tally_workspace_bytes(const rs_shape *s) { return check_decode(s, 0, 0) == RS_OK ? decode_layout(s, true).total : 0; }
+size_t attn_decode_tally_workspace_bytes(const rs_shape *s) { return check_decode(s, 0, 0) == RS_OK ? decode_layout(s, false, 0, 0, true).total : 0; }
 
 int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache, const void *v_cache, const int32_t *len, float scale, float *tally,
                           int32_t n_fresh, void *out, float *lse_out, void *ws, size_t ws_bytes, void *stream)
@@ -711,7 +791,7 @@ int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache,
     if (!q || !k_cache || !v_cache || !len || !tally || !out || n_fresh < 0) return RS_INVALID_ARG;
     for (const void *x : {q, k_cache, v_cache, (const void *)len, (const void *)tally, (const void *)out, (const void *)lse_out})
         if (!aligned16(x)) return RS_INVALID_ARG;
-    if (!ws || !aligned16(ws) || ws_bytes < decode_layout(s, true).total) return RS_WORKSPACE_TOO_SMALL;
+    if (!ws || !aligned16(ws) || ws_bytes < decode_layout(s, false, 0, 0, true).total) return RS_WORKSPACE_TOO_SMALL;
     DecodeParams a = {};
     a.q = q, a.k = k_cache, a.v = v_cache, a.len = len, a.out = out, a.lse = lse_out, a.tally = tally;
     a.fresh = n_fresh, a.scale = scale;
