@@ -1,7 +1,8 @@
 // One token's dense attention over caches of sequences of different lengths, with a tally of the weight that every row has had, and the
 // same over whole or listed pages of a 4-bit cache.
 //   z_t = scale q . k_t,  m = max z,  l = sum e^(z_t - m),  out = sum e^(z_t - m) v_t / l,  tally_t += sum over a KV head's queries of e^(z_t - m) / l
-// Work: a tile is a KV head's (listed pages of a query head: the query head's) up to 16 queries of one sequence; its tokens, in units of 64, lie on a
+// Work: a tile is a KV head's (listed pages of a query head: the query head's) up to 16 queries of one sequence; its tokens, in units of a wave's step (4 bits: 64,
+// bfloat16: 32, float32: 16), lie on a
 // line, tile after tile, sequence after sequence.  The line is divided evenly among the waves, whatever the lengths, which every workgroup reads
 // for itself.  A wave goes through its share without a pause: the next step's rows and, where a tile begins, its queries are on their way before
 // the present step is done.  A tile that lies in one share is done with it; one that is cut leaves records, which a second launch joins in their order
@@ -19,7 +20,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kQ = 16;         // queries of a tile, at most
-constexpr int kUnit = 64;      // tokens of a unit
+constexpr int kUnit = 64;      // tokens of the largest unit
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kMaxB = 1024;
 constexpr float kSlack = 8.f;  // the reference point of a softmax moves when the maximum has grown by more (base-2 exponent): weights stay below 2^8
@@ -33,7 +34,8 @@ struct DecodeParams {
     float *rec_o, *rec_ml, *lse2, *z;  // records [2 a wave, rows, D], [.., 2]; base-2 log-sum-exps [B, Hq]; scores [B, Hq, z_row]
     int *start;                   // [B + 1] units of the sequences before
     int B, Hq, Hkv, H, G, RT, D;  // H: heads with tiles of their own, G queries each, in RT tiles
-    int Tcap, K, shift, list_units, z_row, groups, rows, fresh;
+    int Tcap, K, shift, list_units, z_row, groups, rows, fresh, unit;  // unit: tokens of one, a wave's step
+    bool three;  // workgroups to a CU
     float scale;
 };
 
@@ -56,18 +58,43 @@ __device__ __forceinline__ int length_of(const DecodeParams &a, int b)
     const int n = a.len[b];
     return n < 0 ? 0 : n > a.Tcap ? a.Tcap : n;
 }
-__device__ __forceinline__ int units_of(const DecodeParams &a, int n) { return a.idx ? (n > 0 ? a.list_units : 0) : (n + kUnit - 1) / kUnit; }
+__device__ __forceinline__ int units_of(const DecodeParams &a, int n) { return a.idx ? (n > 0 ? a.list_units : 0) : (n + a.unit - 1) / a.unit; }
 
-// the line's shares, one a wave
+// a b / c for whole numbers whose product is below 2^53: the rounded quotient is a whole number only where the exact one is (another one is at least 1 / c away
+// from it), so cutting it off is exact.  (Divisions of 64-bit integers, which a wave begins with several of, made every call 20 us longer.)
+__device__ __forceinline__ int product_over(int a, double b, double c) { return (int)((double)a * b / c); }
+
+// The line's shares, one a wave.  Of the workgroups on a CU the one that came first gets most of what the CU asks of memory: with equal shares of 4 x 32 heads
+// of 64K tokens the first 256 workgroups were done after 122 us, the others after 143 and 168.  So where three fit on a CU and every wave has
+// some steps to go, the shares are weighted (182 -> 172 us; two or four to a CU: no gain).
+constexpr int kTurn = 256 * kWaves;                  // waves of a workgroup on every CU
+constexpr int kWeight[3] = {54, 43, 31};             // they add up to 128
 struct LineShares {
     int total, n;
-    __device__ __forceinline__ LineShares(int sum, int heads, int groups)
+    bool weighted;
+
+    __device__ __forceinline__ LineShares(int sum, int heads, int groups, bool three)
     {
         total = sum * heads;
         n = total < groups * kWaves ? total : groups * kWaves;
+        weighted = three && total >= 8 * kTurn;  // (the smallest has a unit or more: none is empty)
     }
-    __device__ __forceinline__ int begin(int i) const { return (int)((long)i * total / n); }
-    __device__ __forceinline__ int of(int unit) const { return (int)((((long)unit + 1) * n - 1) / total); }  // whose a unit is
+    __device__ __forceinline__ int begin(int i) const
+    {
+        if (!weighted) return product_over(i, total, n);
+        const int at = i <= kTurn ? kWeight[0] * i
+                                  : i <= 2 * kTurn ? kWeight[0] * kTurn + kWeight[1] * (i - kTurn)
+                                                   : (kWeight[0] + kWeight[1]) * kTurn + kWeight[2] * (i - 2 * kTurn);
+        return (int)((long)at * total / (128 * kTurn));
+    }
+    __device__ __forceinline__ int of(int unit) const  // whose a unit is
+    {
+        if (!weighted) return (int)((((double)unit + 1) * n - 1) / total);
+        const int at = (int)((((double)unit + 1) * (128 * kTurn) - 1) / total);
+        if (at < kWeight[0] * kTurn) return at / kWeight[0];
+        if (at < (kWeight[0] + kWeight[1]) * kTurn) return kTurn + (at - kWeight[0] * kTurn) / kWeight[1];
+        return 2 * kTurn + (at - (kWeight[0] + kWeight[1]) * kTurn) / kWeight[2];
+    }
 };
 
 struct LineTile {
@@ -390,21 +417,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(occupa
 decode_attend_kernel(const DecodeParams a)
 {
     using R = StepRows<FOUR, ST, D>;
-    constexpr int NH = R::NH, STEP = 16 * NH, SPU = kUnit / STEP, C4 = D / 4;
+    constexpr int NH = R::NH, STEP = 16 * NH, C4 = D / 4;  // a step: a unit
     __shared__ __attribute__((aligned(1024))) char tiles[kWaves][64 * D];
     __shared__ float ml[kWaves][kQ][2];
     __shared__ int start[kMaxB + 1];
     __shared__ int wave_tot[kWaves];
     LinePlan plan;
     plan.make(a, start, wave_tot);
-    const LineShares sh(plan.sum, a.H * a.RT, a.groups);
+    const LineShares sh(plan.sum, a.H * a.RT, a.groups, a.three);
     if (blockIdx.x == 0) {  // for the second launch
         for (int b = threadIdx.x; b < a.B; b += kThreads) a.start[b] = plan.begin(b);
         if (threadIdx.x == 0) a.start[a.B] = plan.sum;
     }
     const int wave = scalar(threadIdx.x / kWave), me = blockIdx.x * kWaves + wave;
     if (me >= sh.n) return;  // (a workgroup with such a wave has no results put together)
-    const int u0 = sh.begin(me), n_steps = (sh.begin(me + 1) - u0) * SPU;
+    const int u0 = sh.begin(me), n_steps = sh.begin(me + 1) - u0;
     R r;
     r.lane = lane_id(), r.l16 = r.lane & 15, r.lg = r.lane >> 4;
     char *const tile = tiles[wave];
@@ -413,7 +440,7 @@ decode_attend_kernel(const DecodeParams a)
     auto base_of = [&](const LineTile &w) { return (long)(w.b * a.Hkv + w.h / (a.H / a.Hkv)) * a.Tcap; };
     auto query_of = [&](const LineTile &w) { return (long)w.b * a.Hq + w.h * a.G + w.rt * kQ; };  // the first one's row
     auto rows_of = [&](const LineTile &w) { return min(a.G - w.rt * kQ, kQ); };
-    auto token_of = [&](const LineTile &w, int i) { return (u0 + i / SPU - w.s0) * kUnit + i % SPU * STEP; };
+    auto token_of = [&](const LineTile &w, int i) { return (u0 + i - w.s0) * STEP; };
     auto look_up = [&](const LineTile &w, int i) -> StepWhere<NH> {  // (past the last step: no rows)
         StepWhere<NH> x;
         const int t = token_of(w, i);
@@ -449,10 +476,10 @@ decode_attend_kernel(const DecodeParams a)
         f32x4 s[NH];
 #pragma unroll
         for (int h = 0; h < NH; ++h) s[h] = r.scores(h) * cs;
-        const bool ends = i + 1 == n_steps || u0 + (i + 1) / SPU >= w.s1;  // the tile, or the share
+        const bool ends = i + 1 == n_steps || u0 + i + 1 >= w.s1;  // the tile, or the share
         LineTile then = w;
         if (ends && i + 1 < n_steps) {
-            then = plan.find(a, u0 + (i + 1) / SPU);
+            then = plan.find(a, u0 + i + 1);
             r.load_q((const ST *)a.q + (query_of(then) + (r.l16 < rows_of(then) ? r.l16 : 0)) * D, r.l16 < rows_of(then));
         }
         const StepWhere<NH> next = look_up(then, i + 1);
@@ -493,7 +520,7 @@ decode_attend_kernel(const DecodeParams a)
         if (!ends) continue;
         l = quad_sum(l);
         if (!together) {
-            const int from = max(u0, w.s0), to = u0 + (i + 1) / SPU;
+            const int from = max(u0, w.s0), to = u0 + i + 1;
             const long slot = 2l * me + (from == w.s0 ? 1 : 0);  // a tile that began in another share: the first of two records
             if (r.l16 < rows) {
                 if (from == w.s0 && to == w.s1) {
@@ -582,7 +609,7 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
     __shared__ float part[NG][D], part_ml[NG][2];
     __shared__ float lse2[kThreads];
     const int HR = a.H * a.RT;
-    const LineShares sh(a.start[a.B], HR, a.groups);
+    const LineShares sh(a.start[a.B], HR, a.groups, a.three);
     const int rows = a.B * a.Hq;
     if ((int)blockIdx.x < rows) {
         const int row = blockIdx.x, b = row / a.Hq, hq = row - b * a.Hq, h = hq / a.G, g = hq - h * a.G, rt = g / kQ, r = g % kQ;
@@ -676,7 +703,8 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
 
 struct DecodeLayout {
     size_t ml, lse2, start, z, total;
-    int z_row, groups, rows;  // rows: of a record
+    int z_row, groups, rows, unit;  // workgroups of the first launch; rows of a record
+    bool three;
 };
 // H, K: heads and pages of the lists; 0, 0: none
 static DecodeLayout decode_layout(const rs_shape *s, bool four, int H, int K, bool tally)
@@ -684,9 +712,11 @@ static DecodeLayout decode_layout(const rs_shape *s, bool four, int H, int K, bo
     DecodeLayout x;
     const int heads = H ? H : s->Hkv, G = s->Hq / heads;
     x.rows = G < kQ ? G : kQ;
-    const long units = (long)s->B * heads * ((G + kQ - 1) / kQ) * (((H ? (long)K * s->P : (long)s->Tcap) + kUnit - 1) / kUnit);
+    x.unit = four ? 64 : s->dtype == RS_BF16 ? 32 : 16;
+    const long units = (long)s->B * heads * ((G + kQ - 1) / kQ) * (((H ? (long)K * s->P : (long)s->Tcap) + x.unit - 1) / x.unit);
     const long most = 256l * occupancy(four, (int)esize(s->dtype), s->D), need = (units + kWaves - 1) / kWaves;
     x.groups = (int)(need < most ? need : most);
+    x.three = need >= most && most == 3 * 256;
     const size_t records = (size_t)2 * x.groups * kWaves * x.rows;
     x.z_row = tally ? (s->Tcap + kUnit - 1) / kUnit * kUnit : 0;
     x.ml = RS_WS_CTRL_BYTES + align256(records * s->D * 4);
@@ -707,7 +737,7 @@ static int check_decode(const rs_shape *s, int H, int K)
     if (s->B > kMaxB || s->Tcap > (1 << 30)) return RS_UNSUPPORTED;
     const double heads = listed ? H : s->Hkv, tiles = heads * ((s->Hq / heads + kQ - 1) / kQ), tokens = listed ? (double)K * s->P : s->Tcap;
     // units of the line, and workgroups of the second launch
-    if (s->B * tiles * (tokens / kUnit + 1) > 2e9 || (double)s->B * s->Hq + (double)s->B * s->Hkv * (s->Tcap / 1024. + 1) > 2e9) return RS_UNSUPPORTED;
+    if (s->B * tiles * (tokens / 16 + 1) > 2e9 || (double)s->B * s->Hq + (double)s->B * s->Hkv * (s->Tcap / 1024. + 1) > 2e9) return RS_UNSUPPORTED;
     return RS_OK;
 }
 
@@ -734,8 +764,8 @@ static int decode_run(const rs_shape *s, DecodeParams a, bool four, int H, int K
     a.B = s->B, a.Hq = s->Hq, a.Hkv = s->Hkv, a.D = s->D, a.Tcap = s->Tcap;
     a.H = a.idx ? H : s->Hkv, a.G = s->Hq / a.H, a.RT = (a.G + kQ - 1) / kQ, a.K = K;
     a.shift = a.idx ? __builtin_ctz((unsigned)s->P) : 0;
-    a.list_units = a.idx ? (int)(((long)K * s->P + kUnit - 1) / kUnit) : 0;
-    a.groups = x.groups, a.rows = x.rows;
+    a.list_units = a.idx ? (int)(((long)K * s->P + x.unit - 1) / x.unit) : 0;
+    a.groups = x.groups, a.three = x.three, a.rows = x.rows, a.unit = x.unit;
     const bool bf = s->dtype == RS_BF16;
     if (four) {
         if (bf && s->D == 128) decode_launch<true, bf16, 128>(a, stream);
