@@ -656,7 +656,21 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
     if (t0 >= L) return;
     const int n = a.start[b + 1] - a.start[b], lane = lane_id(), wave = threadIdx.x / kWave;
     const int t = t0 + 4 * threadIdx.x;
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    float w[4] = {0.f, 0.f, 0.f, 0.f}, had[4];
+    float *const to = a.tally + (long)bh * a.Tcap + t;
+    // what does not depend on the log-sum-exps is on its way before they are worked out: the tally and the scores of the first queries
+    constexpr int AHEAD = 4;
+    float4 scores[AHEAD];
+    const float *const z0 = a.z + ((long)b * a.Hq + h * a.G) * a.z_row + t;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) scores[i] = t < L && i < a.G ? *reinterpret_cast<const float4 *>(z0 + (long)i * a.z_row) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) had[j] = t + j < L - a.fresh ? to[j] : 0.f;
+    auto add = [&](const float4 &x, float z) {
+        const float s = z == -INFINITY ? 0.f : z;
+        w[0] += __builtin_amdgcn_exp2f(x.x - s), w[1] += __builtin_amdgcn_exp2f(x.y - s);
+        w[2] += __builtin_amdgcn_exp2f(x.z - s), w[3] += __builtin_amdgcn_exp2f(x.w - s);
+    };
     for (int g0 = 0; g0 < a.G; g0 += kThreads) {  // (more than 256 queries to a KV head: by turns)
         const int n_g = min(a.G - g0, kThreads);
         for (int i = wave; i < n_g; i += kWaves) {
@@ -685,20 +699,19 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
         }
         __syncthreads();
         if (t < L) {
-            const float *z = a.z + ((long)b * a.Hq + h * a.G + g0) * a.z_row + t;
-            for (int i = 0; i < n_g; ++i) {
-                const float4 x = *reinterpret_cast<const float4 *>(z + (long)i * a.z_row);
-                const float s = lse2[i] == -INFINITY ? 0.f : lse2[i];
-                w[0] += __builtin_amdgcn_exp2f(x.x - s), w[1] += __builtin_amdgcn_exp2f(x.y - s);
-                w[2] += __builtin_amdgcn_exp2f(x.z - s), w[3] += __builtin_amdgcn_exp2f(x.w - s);
+            if (g0 == 0) {
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+                    if (i < n_g) add(scores[i], lse2[i]);
             }
+#pragma unroll 4
+            for (int i = g0 == 0 ? AHEAD : 0; i < n_g; ++i) add(*reinterpret_cast<const float4 *>(z0 + (long)(g0 + i) * a.z_row), lse2[i]);
         }
         __syncthreads();
     }
-    float *to = a.tally + (long)bh * a.Tcap + t;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (t + j < L) to[j] = (t + j >= L - a.fresh ? 0.f : to[j]) + w[j];
+        if (t + j < L) to[j] = had[j] + w[j];
 }
 
 struct DecodeLayout {
