@@ -26,9 +26,9 @@ struct MovedRows {
 struct EvictParams {
     float *tally;
     int32_t *pos, *mark, *len;
-    int32_t *count;      // [B Hkv] rows that the second launch moves
+    int4 *count;         // [B Hkv] rows that the second launch moves; rows whose position is on record, tokens seen up to them
     uint32_t *arrived;   // [B] workgroups of a sequence that are done; zero before and after
-    int2 *pairs;         // [B Hkv, most] (from, to)
+    int32_t *from, *to;  // [B Hkv, most] rows that move, and where
     uint32_t *keys;      // [B Hkv, key_row], of caches with more rows than LDS holds
     long most, key_row;
     MovedRows moved;
@@ -37,28 +37,32 @@ struct EvictParams {
 
 // pieces of U bytes
 template <typename U>
-__device__ __forceinline__ void move_rows(char *rows, int bytes, const int2 *pairs, int n, long at, long step)
+__device__ __forceinline__ void move_rows(char *rows, int bytes, const int32_t *from, const int32_t *to, int n, long at, long step)
 {
     const int per = bytes / (int)sizeof(U);
     for (long i = at; i < (long)n * per; i += step) {
-        const int2 p = pairs[i / per];
-        const int c = (int)(i % per);
-        reinterpret_cast<U *>(rows + (long)p.y * bytes)[c] = reinterpret_cast<const U *>(rows + (long)p.x * bytes)[c];
+        const int r = (int)(i / per), c = (int)(i - (long)r * per);
+        reinterpret_cast<U *>(rows + (long)to[r] * bytes)[c] = reinterpret_cast<const U *>(rows + (long)from[r] * bytes)[c];
     }
 }
-__device__ __forceinline__ void move_all(const MovedRows &m, long first_row, const int2 *pairs, int n, long at, long step)
+__device__ __forceinline__ void move_all(const EvictParams &a, int bh, int known, int before, const int32_t *from, const int32_t *to, int n, long at, long step)
 {
-    for (int i = 0; i < m.n; ++i) {
-        char *rows = m.rows[i] + first_row * m.bytes[i];
-        if (m.bytes[i] % 16 == 0) move_rows<uint4>(rows, m.bytes[i], pairs, n, at, step);
-        else move_rows<uint16_t>(rows, m.bytes[i], pairs, n, at, step);
+    float *const tally = a.tally + (long)bh * a.Tcap;
+    int32_t *const pos = a.pos + (long)bh * a.Tcap;
+    for (long i = at; i < n; i += step) {
+        const int f = from[i], t = to[i];
+        tally[t] = tally[f];
+        pos[t] = f < known ? pos[f] : before + (f - known);
+    }
+    for (int i = 0; i < a.moved.n; ++i) {
+        char *rows = a.moved.rows[i] + (long)bh * a.Tcap * a.moved.bytes[i];
+        if (a.moved.bytes[i] % 16 == 0) move_rows<uint4>(rows, a.moved.bytes[i], from, to, n, at, step);
+        else move_rows<uint16_t>(rows, a.moved.bytes[i], from, to, n, at, step);
     }
 }
 
-__device__ __forceinline__ int lanes_below(uint64_t ballot)
-{
-    return __builtin_amdgcn_mbcnt_hi((uint32_t)(ballot >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ballot, 0u));
-}
+// sum over the wave, in every lane
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan_i(x), kWave - 1); }
 
 // inclusive sums over the waves: `before` gets what the waves before this one hold, the return value is all.  lds: not in use by an earlier call
 __device__ __forceinline__ int wave_offsets(int x, int *lds, int &before)
@@ -95,37 +99,37 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
     __shared__ __attribute__((aligned(16))) int4 counts[kWaves];
     __shared__ int found[2];
     __shared__ uint32_t least[2][kWaves][2];
-    __shared__ int2 few[kMovedHere];
+    __shared__ int32_t few_from[kMovedHere], few_to[kMovedHere];
     const int bh = blockIdx.x, b = bh / a.Hkv, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int L = min(a.len[b], a.Tcap);
     const int known = max(0, min(a.mark[2 * b], L)), before = a.mark[2 * b + 1];
     const bool over = L > a.keep && L - a.keep > a.slack;
     if (!over) {
-        if (threadIdx.x == 0) a.count[bh] = 0;
+        if (threadIdx.x == 0) a.count[bh] = make_int4(0, 0, 0, 0);
         return;
     }
     const int total = before + L - known, n_go = L - a.keep;
     float *const tally = a.tally + (long)bh * a.Tcap;
     int32_t *const pos = a.pos + (long)bh * a.Tcap;
-    int2 *const pairs = a.pairs + bh * a.most;
     uint32_t *const keys = HELD > 0 ? held : a.keys + bh * a.key_row;
     auto position = [&](int t) { return t < known ? pos[t] : before + (t - known); };
     const int turns = (L + kWaves * kTurn - 1) / (kWaves * kTurn), from = min(L, wave * turns * kTurn), to = min(L, from + turns * kTurn);
     // ---- the keys; rows up to a whole turn that there are not stay ----
-    for (int t0 = from; t0 < to; t0 += 2 * kTurn) {
-        float x[8];
-        int p[8];
+    constexpr int AHEAD = 16;  // loads of a thread on their way together
+    for (int t0 = from; t0 < to; t0 += AHEAD * kWave) {
+        float x[AHEAD];
+        int p[AHEAD];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < AHEAD; ++i) {
             const int t = t0 + i * kWave + lane;
             x[i] = t < to ? tally[t] : 0.f;
-            p[i] = t < to ? position(t) : -0x7fffffff;
+            p[i] = t < to ? position(t) : 0;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < AHEAD; ++i) {
             const int t = t0 + i * kWave + lane;
-            const uint32_t k = p[i] < a.first || p[i] >= total - a.recent ? kStays : x[i] != x[i] ? 0u : float_to_key(x[i]);
-            if (i < 4 || t0 + kTurn < to) keys[t] = t < to ? k : kStays;
+            const uint32_t k = t >= to || p[i] < a.first || p[i] >= total - a.recent ? kStays : x[i] != x[i] ? 0u : float_to_key(x[i]);
+            if (t0 + i / 4 * kTurn < to) keys[t] = k;
         }
     }
     for (int i = threadIdx.x; i < kBins * kCopies; i += kThreads) (&hist[0][0])[i] = 0;
@@ -171,14 +175,14 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
                 int rank = 0;
 #pragma unroll
                 for (int j = 0; j < kFewGo; ++j) rank += gone[j] < gone[i];
-                if (gone[i] < a.keep && rank == (int)threadIdx.x) few[threadIdx.x].y = gone[i];
+                if (gone[i] < a.keep && rank == (int)threadIdx.x) few_to[threadIdx.x] = gone[i];
             }
             const int t = a.keep + (int)threadIdx.x;
             int rank = 0;
             bool stays = t < L;
 #pragma unroll
             for (int j = 0; j < kFewGo; ++j) stays &= gone[j] != t, rank += gone[j] >= a.keep && gone[j] < t;
-            if (stays) few[(int)threadIdx.x - rank].x = t;
+            if (stays) few_from[(int)threadIdx.x - rank] = t;
         }
         for (int t = known + threadIdx.x; t < a.keep; t += kThreads) {
             bool hole = false;
@@ -237,7 +241,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
                 else if (t < L) mine.z += above, mine.w += same;
             }
         }
-        mine.x = wave_sum_i(mine.x), mine.y = wave_sum_i(mine.y), mine.z = wave_sum_i(mine.z), mine.w = wave_sum_i(mine.w);
+        mine = make_int4(wave_total(mine.x), wave_total(mine.y), wave_total(mine.z), wave_total(mine.w));
         if (lane == 0) counts[wave] = mine;
         __syncthreads();
         int eq = 0, holes = 0, movers = 0, e = 0;
@@ -251,68 +255,52 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
             n_movers += c.z + kept1;
             e += c.y + c.w;
         }
-        int2 *const to_pairs = n_movers <= kMovedHere ? few : pairs;
+        const bool fit = n_movers <= kMovedHere;
+        int32_t *const hole = fit ? few_to : a.to + bh * a.most, *const mover = fit ? few_from : a.from + bh * a.most;
         for (int t0 = from; t0 < to; t0 += kTurn) {
             const uint4 x = load4(t0);
             const uint32_t v[4] = {x.x, x.y, x.z, x.w};
             const int t = t0 + 4 * lane;
-            uint64_t same[4];
-            int n_same = 0;
+            uint32_t stays = 0;  // four bits
 #pragma unroll
-            for (int c = 0; c < 4; ++c) same[c] = __ballot(v[c] == prefix && t + c < L), n_same += __popcll(same[c]);
-            bool stays[4];
-            int rank = eq;
-            if (eq < left && eq + n_same > left) {  // (the turn in which the equal ones that stay end)
+            for (int c = 0; c < 4; ++c) stays |= (v[c] > prefix ? 1u : 0u) << c;
+            if (mine.y + mine.w > 0) {  // the wave has rows that are equal to the last one that stays
+                uint32_t same = 0;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) rank += lanes_below(same[c]);
-            } else if (eq >= left) {
-                rank = left;
-            } else {
-                rank = left - 4;
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                stays[c] = v[c] > prefix || (v[c] == prefix && rank < left);
-                rank += v[c] == prefix;
-            }
-            eq += n_same;
-#pragma unroll
-            for (int side = 0; side < 2; ++side) {
-                if (side == 0 ? t0 >= a.keep : t0 + kTurn <= a.keep) continue;
-                uint64_t out[4];
-                int at = side == 0 ? holes : movers, all = 0;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    out[c] = __ballot(t + c < L && (side == 0 ? t + c < a.keep && !stays[c] : t + c >= a.keep && stays[c]));
-                    at += lanes_below(out[c]);
-                    all += __popcll(out[c]);
-                }
+                for (int c = 0; c < 4; ++c) same |= (v[c] == prefix && t + c < L ? 1u : 0u) << c;
+                const int incl = wave_scan_i(__popc(same));
+                int rank = eq + incl - __popc(same);
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    if ((out[c] >> lane) & 1) {
-                        if (side == 0) to_pairs[at].y = t + c;
-                        else to_pairs[at].x = t + c;
-                        ++at;
+                    if ((same >> c) & 1) {
+                        if (rank < left) stays |= 1u << c;
+                        ++rank;
                     }
-                if (side == 0) holes += all;
-                else movers += all;
+                eq += __builtin_amdgcn_readlane(incl, kWave - 1);
             }
-            if (t0 < a.keep && t0 + kTurn > known)
+            const uint32_t real = L - t >= 4 ? 15u : L > t ? (1u << (L - t)) - 1u : 0u, front = a.keep - t >= 4 ? 15u : a.keep > t ? (1u << (a.keep - t)) - 1u : 0u;
+            auto put = [&](uint32_t which, int32_t *list, int &at) {
+                const int incl = wave_scan_i(__popc(which));
+                int i = at + incl - __popc(which);
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    if (stays[c] && t + c < a.keep && t + c >= known) pos[t + c] = before + (t + c - known);
+                    if ((which >> c) & 1) list[i++] = t + c;
+                at += __builtin_amdgcn_readlane(incl, kWave - 1);
+            };
+            if (t0 < a.keep) put(~stays & real & front, hole, holes);
+            if (t0 + kTurn > a.keep) put(stays & real & ~front, mover, movers);
+            if (t0 < a.keep && t0 + kTurn > known) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (((stays & front) >> c) & 1 && t + c >= known) pos[t + c] = before + (t + c - known);
+            }
         }
     }
     __syncthreads();
     const bool here = n_movers <= kMovedHere;
-    for (int i = threadIdx.x; i < n_movers; i += kThreads) {
-        const int2 p = here ? few[i] : pairs[i];
-        tally[p.y] = tally[p.x];
-        pos[p.y] = position(p.x);
-    }
-    if (here) move_all(a.moved, (long)bh * a.Tcap, few, n_movers, threadIdx.x, kThreads);
+    if (here) move_all(a, bh, known, before, few_from, few_to, n_movers, threadIdx.x, kThreads);
     if (threadIdx.x == 0) {
-        a.count[bh] = here ? 0 : n_movers;
+        a.count[bh] = make_int4(here ? 0 : n_movers, known, before, 0);
         // the last of the sequence's workgroups, all of which have read its length by now
         if (atomicAdd(a.arrived + b, 1u) == (uint32_t)a.Hkv - 1u) {
             a.arrived[b] = 0u;
@@ -326,11 +314,12 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams a)
 {
     const int bh = blockIdx.y;
-    move_all(a.moved, (long)bh * a.Tcap, a.pairs + bh * a.most, a.count[bh], (long)blockIdx.x * blockDim.x + threadIdx.x, (long)gridDim.x * blockDim.x);
+    const int4 c = a.count[bh];
+    move_all(a, bh, c.y, c.z, a.from + bh * a.most, a.to + bh * a.most, c.x, (long)blockIdx.x * blockDim.x + threadIdx.x, (long)gridDim.x * blockDim.x);
 }
 
 struct EvictLayout {
-    size_t count, pairs, keys, total;
+    size_t count, from, to, keys, total;
     long most, key_row;
 };
 static EvictLayout evict_layout(const rs_shape *s, int keep)
@@ -340,8 +329,9 @@ static EvictLayout evict_layout(const rs_shape *s, int keep)
     x.most = keep < s->Tcap - keep ? keep : s->Tcap - keep;
     x.key_row = s->Tcap > kMostHeld ? ((long)s->Tcap + kTurn - 1) / kTurn * kTurn : 0;
     x.count = RS_WS_CTRL_BYTES;
-    x.pairs = x.count + align256(BH * 4);
-    x.keys = x.pairs + align256(BH * (size_t)x.most * 8);
+    x.from = x.count + align256(BH * 16);
+    x.to = x.from + align256(BH * (size_t)x.most * 4);
+    x.keys = x.to + align256(BH * (size_t)x.most * 4);
     x.total = x.keys + BH * (size_t)x.key_row * 4;
     return x;
 }
@@ -366,7 +356,7 @@ static int evict_run(const rs_shape *s, const MovedRows &m, float *tally, int32_
     if (!ws || !aligned16(ws) || ws_bytes < x.total) return RS_WORKSPACE_TOO_SMALL;
     char *const w = (char *)ws;
     const int BH = s->B * s->Hkv;
-    const EvictParams a{tally, pos, mark, len, (int32_t *)(w + x.count), (uint32_t *)ws + kCtrlUnit0, (int2 *)(w + x.pairs), (uint32_t *)(w + x.keys),
+    const EvictParams a{tally, pos, mark, len, (int4 *)(w + x.count), (uint32_t *)ws + kCtrlUnit0, (int32_t *)(w + x.from), (int32_t *)(w + x.to), (uint32_t *)(w + x.keys),
                         x.most, x.key_row, m, s->Hkv, s->Tcap, keep, first, recent, slack};
     if (s->Tcap <= 8704) evict_select_kernel<8704><<<BH, kThreads, 0, stream>>>(a);
     else if (s->Tcap <= 17408) evict_select_kernel<17408><<<BH, kThreads, 0, stream>>>(a);
