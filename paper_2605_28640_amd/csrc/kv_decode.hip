@@ -8,6 +8,7 @@
 // the present step is done.  A tile that lies in one share is done with it; one that is cut leaves records, which a second launch joins in their order
 // on the line (the four waves of a workgroup that is all inside one tile leave one).  So the order of every sum follows from the lengths alone.
 // The tally needs the weights' sum over all tokens, so the scores (float32) go to the workspace and the second launch turns them into weights.
+// Caches that are a few steps long take a workgroup a tile and one launch.
 #include "check.h"
 #include "common.h"
 #include "kv4.h"
@@ -73,6 +74,7 @@ struct LineShares {
     int total, n;
     bool weighted;
 
+    LineShares() = default;
     __device__ __forceinline__ LineShares(int sum, int heads, int groups, bool three)
     {
         total = sum * heads;
@@ -412,7 +414,8 @@ __device__ __forceinline__ void put(const DecodeParams &a, long row, int c, cons
 // a CU have on their way decides (4 bits, 128 channels: 8.7 KB a wave in 168 registers).
 constexpr int occupancy(bool four, int bytes, int D) { return D == 64 ? (four && bytes == 4 ? 3 : 4) : four && bytes == 2 ? 3 : 2; }
 
-template <bool FOUR, typename ST, int D, bool LISTED, bool TALLY>
+// SOLO: a workgroup a tile and no second launch, for caches that are a few steps long
+template <bool FOUR, typename ST, int D, bool LISTED, bool TALLY, bool SOLO>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(occupancy(FOUR, sizeof(ST), D), occupancy(FOUR, sizeof(ST), D)))) void
 decode_attend_kernel(const DecodeParams a)
 {
@@ -420,18 +423,31 @@ decode_attend_kernel(const DecodeParams a)
     constexpr int NH = R::NH, STEP = 16 * NH, C4 = D / 4;  // a step: a unit
     __shared__ __attribute__((aligned(1024))) char tiles[kWaves][64 * D];
     __shared__ float ml[kWaves][kQ][2];
-    __shared__ int start[kMaxB + 1];
+    __shared__ int start[SOLO ? 1 : kMaxB + 1];
     __shared__ int wave_tot[kWaves];
-    LinePlan plan;
-    plan.make(a, start, wave_tot);
-    const LineShares sh(plan.sum, a.H * a.RT, a.groups, a.three);
-    if (blockIdx.x == 0) {  // for the second launch
-        for (int b = threadIdx.x; b < a.B; b += kThreads) a.start[b] = plan.begin(b);
-        if (threadIdx.x == 0) a.start[a.B] = plan.sum;
-    }
+    __shared__ float lse2[SOLO && TALLY ? kQ : 1];
     const int wave = scalar(threadIdx.x / kWave), me = blockIdx.x * kWaves + wave;
-    if (me >= sh.n) return;  // (a workgroup with such a wave has no results put together)
-    const int u0 = sh.begin(me), n_steps = sh.begin(me + 1) - u0;
+    LinePlan plan;
+    LineTile w;
+    int u0, n_steps;
+    LineShares sh;
+    if constexpr (SOLO) {
+        const int HR = a.H * a.RT, hr = blockIdx.x % HR;
+        w.b = blockIdx.x / HR, w.h = hr / a.RT, w.rt = hr % a.RT;
+        w.L = scalar(length_of(a, w.b));
+        w.s0 = 0, w.s1 = units_of(a, w.L);
+        u0 = wave * w.s1 / kWaves, n_steps = (wave + 1) * w.s1 / kWaves - u0;
+    } else {
+        plan.make(a, start, wave_tot);
+        sh = LineShares(plan.sum, a.H * a.RT, a.groups, a.three);
+        if (blockIdx.x == 0) {  // for the second launch
+            for (int b = threadIdx.x; b < a.B; b += kThreads) a.start[b] = plan.begin(b);
+            if (threadIdx.x == 0) a.start[a.B] = plan.sum;
+        }
+        if (me >= sh.n) return;  // (a workgroup with such a wave has no results put together)
+        u0 = sh.begin(me), n_steps = sh.begin(me + 1) - u0;
+        w = plan.find(a, u0);
+    }
     R r;
     r.lane = lane_id(), r.l16 = r.lane & 15, r.lg = r.lane >> 4;
     char *const tile = tiles[wave];
@@ -458,13 +474,17 @@ decode_attend_kernel(const DecodeParams a)
         }
         return x;
     };
-    LineTile w = plan.find(a, u0);
     StepWhere<NH> x = look_up(w, 0);
     r.load_k(a, base_of(w), x);
     r.load_q((const ST *)a.q + (query_of(w) + (r.l16 < rows_of(w) ? r.l16 : 0)) * D, r.l16 < rows_of(w));
     r.load_v(a, base_of(w), x);
-    // all four shares of the workgroup in one tile: their results are put together
-    const bool together = (int)(blockIdx.x + 1) * kWaves <= sh.n && sh.begin(blockIdx.x * kWaves) >= w.s0 && sh.begin((blockIdx.x + 1) * kWaves) <= w.s1;
+    // (now that the first rows are on their way) whether the workgroup's four shares are in one tile, so that their results are put together, and all of it
+    bool together = true, whole = true;
+    if constexpr (!SOLO) {
+        const int g0 = sh.begin(blockIdx.x * kWaves), g1 = sh.begin((blockIdx.x + 1) * kWaves);
+        together = (int)(blockIdx.x + 1) * kWaves <= sh.n && g0 >= w.s0 && g1 <= w.s1;
+        whole = g0 == w.s0 && g1 == w.s1;
+    }
     f32x4 o[D / 16];
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -478,7 +498,7 @@ decode_attend_kernel(const DecodeParams a)
         for (int h = 0; h < NH; ++h) s[h] = r.scores(h) * cs;
         const bool ends = i + 1 == n_steps || u0 + i + 1 >= w.s1;  // the tile, or the share
         LineTile then = w;
-        if (ends && i + 1 < n_steps) {
+        if (!SOLO && ends && i + 1 < n_steps) {
             then = plan.find(a, u0 + i + 1);
             r.load_q((const ST *)a.q + (query_of(then) + (r.l16 < rows_of(then) ? r.l16 : 0)) * D, r.l16 < rows_of(then));
         }
@@ -517,9 +537,9 @@ decode_attend_kernel(const DecodeParams a)
         r.values(tile, s, o);
         x = next;
         r.load_v(a, base_of(then), x);
-        if (!ends) continue;
-        l = quad_sum(l);
+        if (SOLO || !ends) continue;
         if (!together) {
+            l = quad_sum(l);
             const int from = max(u0, w.s0), to = u0 + i + 1;
             const long slot = 2l * me + (from == w.s0 ? 1 : 0);  // a tile that began in another share: the first of two records
             if (r.l16 < rows) {
@@ -541,11 +561,11 @@ decode_attend_kernel(const DecodeParams a)
         w = then;
     }
     if (!together) return;
+    l = quad_sum(l);
     if (r.lg == 0) ml[wave][r.l16][0] = m, ml[wave][r.l16][1] = l;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4 *>(tile + r.l16 * D * 4 + ((4 * dt + r.lg) ^ r.l16) * 16) = o[dt];
     __syncthreads();
-    const bool whole = sh.begin(blockIdx.x * kWaves) == w.s0 && sh.begin((blockIdx.x + 1) * kWaves) == w.s1;
     const long slot = 2l * kWaves * blockIdx.x;
     for (int e = threadIdx.x; e < rows_of(w) * C4; e += kThreads) {
         const int row = e / C4, c4 = e % C4;
@@ -566,6 +586,24 @@ decode_attend_kernel(const DecodeParams a)
         } else {
             *reinterpret_cast<f32x4 *>(a.rec_o + (slot * a.rows + row) * D + 4 * c4) = out;
             if (c4 == 0) *reinterpret_cast<float2 *>(a.rec_ml + (slot * a.rows + row) * 2) = make_float2(top, sum);
+        }
+        if (SOLO && TALLY && c4 == 0) lse2[row] = sum == 0.f ? 0.f : top + __builtin_amdgcn_logf(sum);  // (0: of scores that are all -inf)
+    }
+    if constexpr (SOLO && TALLY) {  // all of the KV head's queries are here (RT = 1)
+        __syncthreads();
+        const int rows = rows_of(w);
+        float *const to = a.tally + (long)(w.b * a.Hkv + w.h) * a.Tcap;
+        for (int t = 4 * threadIdx.x; t < w.L; t += 4 * kThreads) {
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int g = 0; g < rows; ++g) {
+                const f32x4 z = *reinterpret_cast<const f32x4 *>(a.z + (query_of(w) + g) * a.z_row + t) - lse2[g];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += __builtin_amdgcn_exp2f(z[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (t + j < w.L) to[t + j] = (t + j >= w.L - a.fresh ? 0.f : to[t + j]) + sum[j];
         }
     }
 }
@@ -717,7 +755,7 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
 struct DecodeLayout {
     size_t ml, lse2, start, z, total;
     int z_row, groups, rows, unit;  // workgroups of the first launch; rows of a record
-    bool three;
+    bool three, solo;
 };
 // H, K: heads and pages of the lists; 0, 0: none
 static DecodeLayout decode_layout(const rs_shape *s, bool four, int H, int K, bool tally)
@@ -726,10 +764,14 @@ static DecodeLayout decode_layout(const rs_shape *s, bool four, int H, int K, bo
     const int heads = H ? H : s->Hkv, G = s->Hq / heads;
     x.rows = G < kQ ? G : kQ;
     x.unit = four ? 64 : s->dtype == RS_BF16 ? 32 : 16;
-    const long units = (long)s->B * heads * ((G + kQ - 1) / kQ) * (((H ? (long)K * s->P : (long)s->Tcap) + x.unit - 1) / x.unit);
+    const long tile = ((H ? (long)K * s->P : (long)s->Tcap) + x.unit - 1) / x.unit, tiles = (long)s->B * heads * ((G + kQ - 1) / kQ), units = tile * tiles;
     const long most = 256l * occupancy(four, (int)esize(s->dtype), s->D), need = (units + kWaves - 1) / kWaves;
     x.groups = (int)(need < most ? need : most);
     x.three = need >= most && most == 3 * 256;
+    // A workgroup a tile, four of its units at a time, against even shares and a second launch (32 over 8 heads of 128 channels, tiles of 8 / 16 / 32 units, us):
+    // 32 tiles, 4 bits 7.9 / 11.8 / 19.6 against 10.3 / 10.5 / 11.2, bfloat16 7.9 / 10.3 / 15.8 against 10.5 / 10.6 / 11.4; 512 tiles, 4 bits 10.7 / 16.8 / 27.3
+    // against 19.8 / 24.5 / 34.4, bfloat16 14.2 / 25.0 / 51.9 against 19.6 / 30.2 / 55.0.  Longer tiles would gain too where all are alike, and lose much where they are not.
+    x.solo = (tile <= 16 || (tile <= 32 && tiles >= 256)) && G <= kQ;  // (of a tile that is all of a KV head, the tally is its own too)
     const size_t records = (size_t)2 * x.groups * kWaves * x.rows;
     x.z_row = tally ? (s->Tcap + kUnit - 1) / kUnit * kUnit : 0;
     x.ml = RS_WS_CTRL_BYTES + align256(records * s->D * 4);
@@ -754,18 +796,28 @@ static int check_decode(const rs_shape *s, int H, int K)
     return RS_OK;
 }
 
+template <bool FOUR, typename ST, int D, bool LISTED, bool TALLY>
+static void decode_launch_form(const DecodeParams &a, bool solo, hipStream_t stream)
+{
+    if (solo) {
+        decode_attend_kernel<FOUR, ST, D, LISTED, TALLY, true><<<(unsigned)(a.B * a.H * a.RT), kThreads, 0, stream>>>(a);
+        return;
+    }
+    decode_attend_kernel<FOUR, ST, D, LISTED, TALLY, false><<<a.groups, kThreads, 0, stream>>>(a);
+    const long slices = TALLY ? (long)a.B * a.Hkv * ((a.Tcap + 1023) / 1024) : 0;
+    decode_join_kernel<ST, D><<<(unsigned)((long)a.B * a.Hq + slices), kThreads, 0, stream>>>(a);
+}
+
 template <bool FOUR, typename ST, int D>
-static void decode_launch(const DecodeParams &a, hipStream_t stream)
+static void decode_launch(const DecodeParams &a, bool solo, hipStream_t stream)
 {
     if constexpr (FOUR) {
-        if (a.idx) decode_attend_kernel<true, ST, D, true, false><<<a.groups, kThreads, 0, stream>>>(a);
-        else if (a.tally) decode_attend_kernel<true, ST, D, false, true><<<a.groups, kThreads, 0, stream>>>(a);
-        else decode_attend_kernel<true, ST, D, false, false><<<a.groups, kThreads, 0, stream>>>(a);
+        if (a.idx) decode_launch_form<true, ST, D, true, false>(a, solo, stream);
+        else if (a.tally) decode_launch_form<true, ST, D, false, true>(a, solo, stream);
+        else decode_launch_form<true, ST, D, false, false>(a, solo, stream);
     } else {
-        decode_attend_kernel<false, ST, D, false, true><<<a.groups, kThreads, 0, stream>>>(a);
+        decode_launch_form<false, ST, D, false, true>(a, solo, stream);
     }
-    const long slices = a.tally ? (long)a.B * a.Hkv * ((a.Tcap + 1023) / 1024) : 0;
-    decode_join_kernel<ST, D><<<(unsigned)((long)a.B * a.Hq + slices), kThreads, 0, stream>>>(a);
 }
 
 static int decode_run(const rs_shape *s, DecodeParams a, bool four, int H, int K, void *ws, hipStream_t stream)
@@ -781,15 +833,15 @@ static int decode_run(const rs_shape *s, DecodeParams a, bool four, int H, int K
     a.groups = x.groups, a.three = x.three, a.rows = x.rows, a.unit = x.unit;
     const bool bf = s->dtype == RS_BF16;
     if (four) {
-        if (bf && s->D == 128) decode_launch<true, bf16, 128>(a, stream);
-        else if (bf) decode_launch<true, bf16, 64>(a, stream);
-        else if (s->D == 128) decode_launch<true, float, 128>(a, stream);
-        else decode_launch<true, float, 64>(a, stream);
+        if (bf && s->D == 128) decode_launch<true, bf16, 128>(a, x.solo, stream);
+        else if (bf) decode_launch<true, bf16, 64>(a, x.solo, stream);
+        else if (s->D == 128) decode_launch<true, float, 128>(a, x.solo, stream);
+        else decode_launch<true, float, 64>(a, x.solo, stream);
     } else {
-        if (bf && s->D == 128) decode_launch<false, bf16, 128>(a, stream);
-        else if (bf) decode_launch<false, bf16, 64>(a, stream);
-        else if (s->D == 128) decode_launch<false, float, 128>(a, stream);
-        else decode_launch<false, float, 64>(a, stream);
+        if (bf && s->D == 128) decode_launch<false, bf16, 128>(a, x.solo, stream);
+        else if (bf) decode_launch<false, bf16, 64>(a, x.solo, stream);
+        else if (s->D == 128) decode_launch<false, float, 128>(a, x.solo, stream);
+        else decode_launch<false, float, 64>(a, x.solo, stream);
     }
     return launch_status();
 }
