@@ -8,13 +8,24 @@ namespace rs {
 constexpr int kThreads = 256;
 constexpr int kNoPages = 4;  // without bounds: rows go by 16
 
+// eight values of a row
+__device__ __forceinline__ void unpack_row(uint32_t codes, float scale, float (&x)[8])
+{
+    uint32_t p[4];
+    kv4_values(codes, scale, p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[2 * j] = __uint_as_float(p[j] << 16), x[2 * j + 1] = __uint_as_float(p[j] & 0xffff0000u);
+}
+// the value of the lane m (8, 16 or 32) away
+__device__ __forceinline__ float other_rows(float x, int m) { return shfl_xor_f(x, m); }
+
 struct Kv4Params {
     const void *k, *v;  // rows to be stored, T_src of them a head, or nullptr: only the bounds
     const int32_t *len, *n_new;
     uint8_t *k4, *ks, *v4, *vs;
     void *meta;
     long T_src, t_src;
-    int Hkv, Tcap, T_new, shift;  // shift: log2 of the page size
+    int Hkv, Tcap, T_new, shift, pages;  // shift: log2 of the page size; pages: that T_new neighbouring rows can lie in
 };
 
 // tokens of sequence b, and how many of them are new
@@ -23,17 +34,19 @@ __device__ __forceinline__ void sequence(const Kv4Params &a, int b, int &L, int 
     L = a.len[b];
     n = a.n_new ? a.n_new[b] : a.T_new;
     n = n < 0 ? 0 : n > a.T_new ? a.T_new : n;
-    if (L > a.Tcap) L = a.Tcap;
-    if (L < n) n = 0;  // (a length below 0 among them)
+    L = L < 0 ? 0 : L > a.Tcap ? a.Tcap : L;
+    if (L < n) n = 0;
 }
 
-// this lane's 8 channels of a row, in 4 bits; returned as the values that they stand for
-template <typename ST, int D>
-__device__ __forceinline__ void store_row(const ST *src, uint8_t *codes, uint8_t *scales, int c8, bool real, float (&x)[8])
+// 16 rows of a page
+struct Chunk {
+    int page, t0, t1;    // rows t0 .. t1 - 1 of the sequence; t1 <= t0: there are none
+    bool begins, ends;   // the page's first, or last, such rows
+};
+
+// this lane's 8 channels of a row in 4 bits; x: the channels, then the values that they are stored as
+__device__ __forceinline__ void store_row(float (&x)[8], bool real, uint8_t *codes, uint8_t *scales, int c8)
 {
-    if (real) Row8<ST>::load(src + 8 * c8, x);
-    else
-        for (int j = 0; j < 8; ++j) x[j] = 0.f;
     uint32_t top = 0u;
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
@@ -41,21 +54,26 @@ __device__ __forceinline__ void store_row(const ST *src, uint8_t *codes, uint8_t
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));  // quad_perm:[1,0,3,2]
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));  // quad_perm:[2,3,0,1]
     const uint32_t byte = kv4_scale_byte(top);
-    const float scale = kv4_scale(byte);
-    const uint32_t c = byte == kKv4Nan ? 0u : kv4_codes(x, scale);
+    const uint32_t c = byte == kKv4Nan ? 0u : kv4_codes(x, kv4_scale(byte));
     if (real) {
         reinterpret_cast<uint32_t *>(codes)[c8] = c;
         if ((c8 & 3) == 0) scales[c8 >> 2] = (uint8_t)byte;
     }
-    uint32_t p[4];
-    kv4_values(c, scale, p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[2 * j] = __uint_as_float(p[j] << 16), x[2 * j + 1] = __uint_as_float(p[j] & 0xffff0000u);
+    unpack_row(c, kv4_scale(byte), x);
 }
 
-// A workgroup for each (sequence, KV head, page with a new row): D / 8 threads a row.
+template <typename ST>
+__device__ __forceinline__ void load_row(const ST *src, bool real, int c8, float (&x)[8])
+{
+    if (real) Row8<ST>::load(src + 8 * c8, x);
+    else
+        for (int j = 0; j < 8; ++j) x[j] = 0.f;
+}
+
+// Short calls: a workgroup for each (sequence, KV head, page with a new row), D / 8 threads a row.  Nothing but trips to memory, so as many waves as there are
+// rows to look at.
 template <typename ST, int D>
-__global__ __launch_bounds__(kThreads) void kv4_append_kernel(const Kv4Params a)
+__global__ __launch_bounds__(kThreads) void kv4_append_short_kernel(const Kv4Params a)
 {
     using R = Kv4Row<D>;
     constexpr int CH = D / 8, RPB = kThreads / CH;  // threads a row, rows a turn
@@ -76,15 +94,14 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(const Kv4Params a)
         const long row = (long)bh * a.Tcap + t, src = ((long)bh * a.T_src + a.t_src + (t - first)) * D;
         float x[8];
         if (a.k) {
-            store_row<ST, D>((const ST *)a.v + src, a.v4 + row * R::CODES, a.vs + row * R::SCALES, c8, fresh, x);
-            store_row<ST, D>((const ST *)a.k + src, a.k4 + row * R::CODES, a.ks + row * R::SCALES, c8, fresh, x);
+            load_row((const ST *)a.v + src, fresh, c8, x);
+            store_row(x, fresh, a.v4 + row * R::CODES, a.vs + row * R::SCALES, c8);
+            load_row((const ST *)a.k + src, fresh, c8, x);
+            store_row(x, fresh, a.k4 + row * R::CODES, a.ks + row * R::SCALES, c8);
         }
         if (!a.meta || !real) continue;
         if (!fresh) {
-            uint32_t p[4];
-            kv4_values(reinterpret_cast<const uint32_t *>(a.k4 + row * R::CODES)[c8], kv4_scale(a.ks[row * R::SCALES + (c8 >> 2)]), p);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[2 * j] = __uint_as_float(p[j] << 16), x[2 * j + 1] = __uint_as_float(p[j] & 0xffff0000u);
+            unpack_row(reinterpret_cast<const uint32_t *>(a.k4 + row * R::CODES)[c8], kv4_scale(a.ks[row * R::SCALES + (c8 >> 2)]), x);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) lo[j] = fminf(lo[j], x[j]), hi[j] = fmaxf(hi[j], x[j]);
@@ -110,6 +127,114 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(const Kv4Params a)
     }
 }
 
+// Long calls: a wave takes 16 rows of a page at a time, the next ones, if it has more, on their way meanwhile; no other wave has a part in its pages' bounds.
+template <typename ST, int D>
+__global__ __launch_bounds__(kWave) __attribute__((amdgpu_waves_per_eu(4, 4))) void kv4_append_kernel(const Kv4Params a)
+{
+    using R = Kv4Row<D>;
+    using Raw = typename Row8<ST>::raw_t;
+    constexpr int CH = D / 8, RPL = kWave / CH, NG = 16 / RPL;  // lanes a row, rows a load, loads a chunk
+    const int lane = lane_id(), c8 = lane % CH, r0 = lane / CH;
+    const int bh = blockIdx.y;
+    int L, n, at = blockIdx.x;  // at: of the pages with new rows, this wave's
+    sequence(a, bh / a.Hkv, L, n);
+    const int first = L - n;  // the sequence's first new row
+    // the chunk that comes after c; begin: the wave's first
+    auto next = [&](Chunk c, bool begin) {
+        c.begins = begin || c.ends;
+        if (!c.begins) {
+            c.t0 += 16;
+        } else {
+            if (!begin) at += gridDim.x;
+            c.page = (first >> a.shift) + at;
+            const int row = c.page << a.shift;
+            c.t0 = a.meta ? row : max(row, first & ~15);
+            c.t1 = n > 0 && at < a.pages ? min(L, row + (1 << a.shift)) : c.t0;
+        }
+        c.ends = c.t0 + 16 >= c.t1;
+        return c;
+    };
+    auto load = [&](const void *src, const Chunk &c, Raw (&x)[NG]) {
+        const int f = max(c.t0, first), n = min(c.t1, c.t0 + 16) - f;  // new rows: f .. f + n - 1
+        const LdsSource d = lds_source_sized((const ST *)src + ((long)bh * a.T_src + a.t_src + (f - first)) * D, n > 0 ? n * D * (int)sizeof(ST) : 0);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) x[g] = load_row8<ST, 2>(d, (uint32_t)(((c.t0 + g * RPL + r0 - f) * D + 8 * c8) * (int)sizeof(ST)));
+    };
+    Raw kx[NG], vx[NG];
+    Chunk c = {};
+    c = next(c, true);
+    if (c.t1 <= c.t0) return;
+    if (a.k) load(a.v, c, vx), load(a.k, c, kx);
+    float lo[8], hi[8];
+    while (c.t1 > c.t0) {
+        const Chunk then = next(c, false);
+        if (c.begins) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lo[j] = INFINITY, hi[j] = -INFINITY;
+        }
+        const bool some_old = c.t0 < first || a.k == nullptr;
+        uint32_t old[NG];
+        float old_scale[NG];
+        if (a.meta && some_old) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const int t = c.t0 + g * RPL + r0;
+                const long row = (long)bh * a.Tcap + t;
+                const bool is = t < c.t1 && (t < first || a.k == nullptr);
+                old[g] = is ? reinterpret_cast<const uint32_t *>(a.k4 + row * R::CODES)[c8] : 0u;
+                old_scale[g] = is ? kv4_scale(a.ks[row * R::SCALES + (c8 >> 2)]) : 0.f;
+            }
+        }
+        if (a.k) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const int t = c.t0 + g * RPL + r0;
+                const long row = (long)bh * a.Tcap + t;
+                float x[8];
+                Row8<ST>::unpack(vx[g], x);
+                store_row(x, t >= first && t < c.t1, a.v4 + row * R::CODES, a.vs + row * R::SCALES, c8);
+            }
+            if (then.t1 > then.t0) load(a.v, then, vx);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const int t = c.t0 + g * RPL + r0;
+                const long row = (long)bh * a.Tcap + t;
+                const bool real = t >= first && t < c.t1;
+                float x[8];
+                Row8<ST>::unpack(kx[g], x);
+                store_row(x, real, a.k4 + row * R::CODES, a.ks + row * R::SCALES, c8);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (real) lo[j] = fminf(lo[j], x[j]), hi[j] = fmaxf(hi[j], x[j]);
+            }
+            if (then.t1 > then.t0) load(a.k, then, kx);
+        }
+        if (a.meta) {
+            if (some_old) {
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const int t = c.t0 + g * RPL + r0;
+                    float x[8];
+                    unpack_row(old[g], old_scale[g], x);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (t < c.t1 && (t < first || a.k == nullptr)) lo[j] = fminf(lo[j], x[j]), hi[j] = fmaxf(hi[j], x[j]);
+                }
+            }
+            if (c.ends) {  // over the wave's rows
+#pragma unroll
+                for (int m = CH; m < kWave; m <<= 1)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) lo[j] = fminf(lo[j], other_rows(lo[j], m)), hi[j] = fmaxf(hi[j], other_rows(hi[j], m));
+                ST *const to = (ST *)a.meta + ((long)bh * (a.Tcap >> a.shift) + c.page) * 2 * D + 8 * c8;
+                if (r0 == 0) Row8<ST>::store(to, lo);
+                if (r0 == 1) Row8<ST>::store(to + D, hi);
+            }
+        }
+        c = then;
+    }
+}
+
 // 8 channels a thread
 template <typename ST, int D>
 __global__ __launch_bounds__(kThreads) void kv4_fetch_kernel(const uint8_t *__restrict__ k4, const uint8_t *__restrict__ ks,
@@ -128,32 +253,33 @@ __global__ __launch_bounds__(kThreads) void kv4_fetch_kernel(const uint8_t *__re
         const long row = (long)bh * Tcap + t, to = ((long)bh * T + i) * D + 8 * c8;
         const uint32_t kc = reinterpret_cast<const uint32_t *>(k4 + row * R::CODES)[c8], vc = reinterpret_cast<const uint32_t *>(v4 + row * R::CODES)[c8];
         const float kf = kv4_scale(ks[row * R::SCALES + (c8 >> 2)]), vf = kv4_scale(vs[row * R::SCALES + (c8 >> 2)]);
-        uint32_t p[4];
         float x[8];
-        kv4_values(kc, kf, p);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[2 * j] = __uint_as_float(p[j] << 16), x[2 * j + 1] = __uint_as_float(p[j] & 0xffff0000u);
+        unpack_row(kc, kf, x);
         Row8<ST>::store(k_out + to, x);
-        kv4_values(vc, vf, p);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[2 * j] = __uint_as_float(p[j] << 16), x[2 * j + 1] = __uint_as_float(p[j] & 0xffff0000u);
+        unpack_row(vc, vf, x);
         Row8<ST>::store(v_out + to, x);
     }
 }
 
-template <typename ST, int D>
-static int append_launch(const Kv4Params &a, int BH, hipStream_t stream)
+static int append_dispatch(const rs_shape *s, Kv4Params a, hipStream_t stream)
 {
-    const int P = 1 << a.shift, pages = (int)(((long)a.T_new + 2l * P - 2) / P);  // that T_new neighbouring rows can lie in
-    kv4_append_kernel<ST, D><<<dim3((unsigned)pages, (unsigned)BH), kThreads, 0, stream>>>(a);
+    a.Hkv = s->Hkv, a.Tcap = s->Tcap;
+    a.pages = (int)(((long)a.T_new + (2l << a.shift) - 2) >> a.shift);
+    const int BH = s->B * s->Hkv, most = (65536 + BH - 1) / BH;
+    const bool stream_form = (long)BH * a.pages >= 4096;
+    const dim3 grid((unsigned)(!stream_form || a.pages < most ? a.pages : most), (unsigned)BH);
+    auto go = [&](auto long_kernel, auto short_kernel) {
+        if (stream_form) long_kernel<<<grid, kWave, 0, stream>>>(a);
+        else short_kernel<<<grid, kThreads, 0, stream>>>(a);
+    };
+    if (s->dtype == RS_BF16) {
+        if (s->D == 128) go(kv4_append_kernel<bf16, 128>, kv4_append_short_kernel<bf16, 128>);
+        else go(kv4_append_kernel<bf16, 64>, kv4_append_short_kernel<bf16, 64>);
+    } else {
+        if (s->D == 128) go(kv4_append_kernel<float, 128>, kv4_append_short_kernel<float, 128>);
+        else go(kv4_append_kernel<float, 64>, kv4_append_short_kernel<float, 64>);
+    }
     return launch_status();
-}
-
-static int append_dispatch(const rs_shape *s, const Kv4Params &a, hipStream_t stream)
-{
-    const int BH = s->B * s->Hkv;
-    if (s->dtype == RS_BF16) return s->D == 128 ? append_launch<bf16, 128>(a, BH, stream) : append_launch<bf16, 64>(a, BH, stream);
-    return s->D == 128 ? append_launch<float, 128>(a, BH, stream) : append_launch<float, 64>(a, BH, stream);
 }
 
 // what a shape has to be for the calls of a 4-bit cache that take a workgroup's row of the grid for every (sequence, KV head)
@@ -190,8 +316,10 @@ int32_t kv4_append(const rs_shape *s, const void *k, const void *v, int64_t T_sr
                           (const void *)meta})
         if (!aligned16(x)) return RS_INVALID_ARG;
     if (T_new < 1 || T_new > s->Tcap || T_src < 1 || t_src < 0 || t_src > T_src - T_new) return RS_INVALID_ARG;
-    return append_dispatch(s, Kv4Params{k, v, len, n_new, k4, k4_scale, v4, v4_scale, meta, T_src, t_src, s->Hkv, s->Tcap, T_new,
-                                        meta ? __builtin_ctz((unsigned)s->P) : kNoPages}, (hipStream_t)stream);
+    Kv4Params a = {};
+    a.k = k, a.v = v, a.len = len, a.n_new = n_new, a.k4 = k4, a.ks = k4_scale, a.v4 = v4, a.vs = v4_scale, a.meta = meta;
+    a.T_src = T_src, a.t_src = t_src, a.T_new = T_new, a.shift = meta ? __builtin_ctz((unsigned)s->P) : kNoPages;
+    return append_dispatch(s, a, (hipStream_t)stream);
 }
 
 int32_t kv4_page_meta(const rs_shape *s, const uint8_t *k4, const uint8_t *k4_scale, const int32_t *len, const int32_t *n_new, int32_t T_new, void *meta,
@@ -203,8 +331,10 @@ int32_t kv4_page_meta(const rs_shape *s, const uint8_t *k4, const uint8_t *k4_sc
     for (const void *x : {(const void *)k4, (const void *)k4_scale, (const void *)len, (const void *)n_new, (const void *)meta})
         if (!aligned16(x)) return RS_INVALID_ARG;
     if (T_new < 1 || T_new > s->Tcap) return RS_INVALID_ARG;
-    return append_dispatch(s, Kv4Params{nullptr, nullptr, len, n_new, const_cast<uint8_t *>(k4), const_cast<uint8_t *>(k4_scale), nullptr, nullptr, meta,
-                                        0, 0, s->Hkv, s->Tcap, T_new, __builtin_ctz((unsigned)s->P)}, (hipStream_t)stream);
+    Kv4Params a = {};
+    a.len = len, a.n_new = n_new, a.k4 = const_cast<uint8_t *>(k4), a.ks = const_cast<uint8_t *>(k4_scale), a.meta = meta;
+    a.T_new = T_new, a.shift = __builtin_ctz((unsigned)s->P);
+    return append_dispatch(s, a, (hipStream_t)stream);
 }
 
 int32_t kv4_fetch(const rs_shape *s, const uint8_t *k4, const uint8_t *k4_scale, const uint8_t *v4, const uint8_t *v4_scale, const int32_t *len,
