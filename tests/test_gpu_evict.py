@@ -84,6 +84,9 @@ CASES = [  # B, Hkv, D, Tcap, lengths, keep, first, recent, slack
     (2, 2, 64, 256, [-3, 256], 255, 1, 254, 0),
     (1, 1, 128, 300, [300], 300, 0, 0, 0),
     (1, 1, 64, 70000, [69999], 30011, 7, 1000, 0),
+    (1, 2, 64, 12000, [11999], 700, 0, 3, 0),
+    (5, 1, 64, 2000, [1999, 1995, 1991, 1992, 2000], 1991, 5, 1986, 0),   # up to nine rows go, of hardly more that may
+    (2, 2, 64, 34816, [34816, 34815], 34808, 0, 0, 0),
 ]
 
 

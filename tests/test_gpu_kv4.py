@@ -68,6 +68,11 @@ CASES = [  # B, Hkv, D, Tcap, P, dtype, lengths, new, T_new, rows of the source,
     (5, 2, 128, 320, 32, "bf16", [320, 40, 5, 400, -3], [100, 41, -2, 500, 1], 100, 100, 0),
     (1, 2, 128, 2048, 16, "bf16", [2003], None, 2003, 2048, 0),
     (2, 5, 64, 96, 16, "bf16", [77, 96], [77, 5], 96, 96, 0),
+    # calls long enough to go as a stream
+    (8, 32, 64, 320, 16, "bf16", [320, 319, 300, 17, 0, 1, 100, 257], [299, 16, 300, 17, 5, 1, 77, 30], 300, 300, 0),
+    (4, 24, 128, 768, 32, "f32", [768, 700, 33, 500], None, 700, 768, 40),
+    (4, 32, 128, 640, 32, "bf16", [640, 639, 555, 64], [640, 1, 33, 64], 640, 640, 0),
+    (64, 40, 64, 64, 64, "f32", [(5 * i) % 65 for i in range(64)], [(7 * i) % 41 for i in range(64)], 40, 40, 0),
 ]
 
 
@@ -207,3 +212,27 @@ def test_rows_far_into_a_long_cache(rs):
         want = M.values(*M.pack(x.double().numpy()))
         np.testing.assert_array_equal(y.double().cpu().numpy(), want)
         assert int(codes[:, :, L:].max()) == 0 and int(byte[:, :, L:].max()) == 0 and int(byte[:, :, L - T - 64:L - T].max()) == 0
+
+
+@pytest.mark.parametrize("D,P,dtype", [(64, 16, "bf16"), (128, 16, "f32"), (64, 64, "f32")])
+def test_a_stream_of_many_pages_a_wave(rs, D, P, dtype):
+    """A call so long that a wave takes several pages in turn stores what many short calls store, bounds included."""
+    B, Hkv, Tcap, T, T0 = 16, 64, 1280, 1117, 7
+    lens = [T0 + T - (5 * b) % 40 for b in range(B)]
+    new = [min(n, T) - (3 * b) % 50 for b, n in enumerate(lens)]
+    g = torch.Generator(device="cuda").manual_seed(D)
+    k, v = (torch.randn(B, Hkv, T, D, device="cuda", generator=g).to(tdtype(dtype)) for _ in "kv")
+    a, b = (Cache(rs, B, Hkv, D, Tcap, P, dtype, lens, seed=1) for _ in "ab")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    rs.kv4_append(a.s, k, v, 0, a.len, ints(new), T, *a.dev, a.meta)
+    for i in range(0, T, 32):
+        n = min(32, T - i)
+        some = [max(0, min(n, m - i)) for m in new]
+        ln = ints([x - m + i + s for x, m, s in zip(lens, new, some)])
+        rs.kv4_append(b.s, k, v, i, ln, ints(some), n, *b.dev, b.meta)
+    torch.cuda.synchronize()
+    for x, y in zip(a.dev + [a.meta], b.dev + [b.meta]):
+        assert torch.equal(x, y)
+    a.meta.fill_(3.0)
+    rs.kv4_page_meta(a.s, a.dev[0], a.dev[1], a.len, ints(new), T, a.meta)
+    assert torch.equal(a.meta, b.meta)

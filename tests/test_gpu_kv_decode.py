@@ -118,6 +118,10 @@ SHAPES = [  # B, Hq, Hkv, D, Tcap, lengths
     (1, 64, 1, 64, 150, [150]),
     (1, 4, 4, 128, 5000, [4999]),      # cut over many workgroups
     (70, 2, 2, 64, 320, [(37 * i) % 321 for i in range(70)]),
+    (70, 2, 1, 64, 2200, [(371 * i) % 2201 for i in range(70)]),  # more sequences than lanes, tiles of many steps
+    (3, 8, 8, 64, 1500, [1500, 0, 1]),
+    (1, 300, 1, 64, 1300, [1234]),     # 300 queries to a head
+    (2, 34, 2, 128, 2500, [2500, 1111]),
 ]
 
 
@@ -280,3 +284,108 @@ def test_a_long_cache(rs, kind):
     torch.cuda.synchronize()
     assert abs(float(lse) - 512) < 1e-3 and (out == 4).all()  # e^512 against 80 million e^0
     assert float(tally[0, 0, Tcap - 4]) == 1 and float(tally.sum()) == 1
+
+
+def _values(codes, byte):
+    """A 4-bit cache's values on the device, in 64 bits."""
+    grid = torch.tensor(np.concatenate([M.GRID, -M.GRID]), device="cuda")
+    x = torch.stack([grid[(codes & 15).int()], grid[(codes >> 4).int()]], -1).flatten(-2)
+    return x * ((byte.long() + 896) << 52).view(torch.float64).repeat_interleave(32, -1)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,lens", [(4, 16, 8, [20000, 19001, 17, 20016]), (130, 4, 4, None), (1024, 2, 1, None)])
+@pytest.mark.parametrize("tally", [False, True])
+def test_many_units_a_wave(rs, B, Hq, Hkv, lens, tally):
+    """More work than the line's shares are alike for (three workgroups a CU), and as many sequences as are taken."""
+    D, G = 128, Hq // Hkv
+    lens = lens or [(7919 * i) % 2600 for i in range(B)]
+    Tcap = max(lens) + 3
+    g = torch.Generator(device="cuda").manual_seed(B)
+    s = rs.make_shape(B, Hq, Hkv, D, Tcap, 16, torch.bfloat16)
+    dev = [torch.randint(lo, hi, (B, Hkv, Tcap, n), dtype=torch.uint8, device="cuda", generator=g) for lo, hi, n in
+           ((0, 256, 64), (121, 126, 4), (0, 256, 64), (121, 126, 4))]
+    q = torch.randn(B, Hq, D, device="cuda", generator=g).bfloat16()
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    before = torch.rand(B, Hkv, Tcap, device="cuda", generator=g)
+    got = before.clone()
+    out, lse = torch.zeros_like(q), torch.zeros(B, Hq, device="cuda")
+    ws = rs.Workspace(rs.kv4_attn_decode_workspace_bytes(s, 0, 0, tally))
+    rs.kv4_attn_decode(s, q, *dev, ln, 0.09, None, got if tally else None, 1, out, lse, ws)
+    first = out.clone()
+    rs.kv4_attn_decode(s, q, *dev, ln, 0.09, None, got.clone() if tally else None, 1, out, lse, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(first, out)
+    for b in range(B):
+        L = lens[b]
+        if L == 0:
+            assert (out[b] == 0).all() and (lse[b] == -float("inf")).all()
+            continue
+        k, v = _values(dev[0][b, :, :L], dev[1][b, :, :L]), _values(dev[2][b, :, :L], dev[3][b, :, :L])
+        qq = q[b].double().view(Hkv, G, D)
+        z = torch.matmul(qq, k.transpose(1, 2).contiguous()) * 0.09
+        want = torch.logsumexp(z, -1)
+        p = torch.exp(z - want[..., None])
+        o, a = torch.matmul(p, v).view(Hq, D), torch.matmul(p, v.abs()).view(Hq, D)
+        e = M.rounding(float((torch.matmul(qq.abs(), k.abs().transpose(1, 2).contiguous()) * 0.09).max()), L, D)
+        assert ((out[b].double() - o).abs() <= (e + 2.0 ** -8) * a + 2.0 ** -8 * o.abs()).all(), b
+        assert ((lse[b].double() - want.view(Hq)).abs() <= e + 2.0 ** -22 * want.view(Hq).abs()).all(), b
+        if tally:
+            base = before[b].double()
+            base[:, L - 1] = 0
+            w = base[:, :L] + p.sum(1)
+            assert ((got[b, :, :L].double() - w).abs() <= e * p.sum(1) + 2.0 ** -22 * w).all(), b
+            assert torch.equal(got[b, :, L:], before[b, :, L:])
+
+
+def test_quest_over_a_4_bit_cache(rs):
+    """Recurrence, append with bounds, page selection, attention of the listed pages, eviction and the bounds anew: together, as a decode loop has them."""
+    B, Hq, Hkv, D, P, Tcap, T0, steps, K = 2, 8, 4, 128, 16, 512, 333, 20, 9
+    dt = torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rand = lambda *n: torch.randn(*n, device="cuda", generator=g)
+    s, s1 = rs.make_shape(B, Hq, Hkv, D, Tcap, P, dt), rs.make_shape(B, Hq, Hkv, D, 16, 16, dt)
+    four = [torch.zeros(B, Hkv, Tcap, n, dtype=torch.uint8, device="cuda") for n in (64, 4, 64, 4)]
+    meta = torch.zeros(B, Hkv, Tcap // P, 2, D, device="cuda", dtype=dt)
+    sk, sv = torch.zeros(B, Hkv, D, device="cuda"), torch.zeros(B, Hkv, D, device="cuda")
+    full = [torch.zeros(B, Hkv, Tcap, D, device="cuda", dtype=dt) for _ in "kv"]
+    ws = rs.Workspace(max(rs.rat_scan_workspace_bytes(s, T0), rs.quest_select_decode_workspace_bytes(s, Tcap), rs.kv4_attn_decode_workspace_bytes(s, Hq, K, False),
+                          rs.kv4_attn_decode_workspace_bytes(s, 0, 0, True), rs.cache_evict_workspace_bytes(s, 200)))
+    rs.rat_scan(s, rand(B, Hkv, T0, D).to(dt), rand(B, Hkv, T0, D).to(dt), torch.sigmoid(rand(B, Hkv, T0, D) * 0.5 + 3), sk, sv, *full, 0, T0, ws)
+    length = torch.full((B,), T0, dtype=torch.int32, device="cuda")
+    rs.kv4_append(s, *full, 0, length, None, T0, *four, meta)
+    stage = [torch.zeros(B, Hkv, 16, D, device="cuda", dtype=dt) for _ in "kv"]
+    out, lse, idx = torch.zeros(B, Hq, D, device="cuda", dtype=dt), torch.zeros(B, Hq, device="cuda"), torch.zeros(B, Hq, K, device="cuda", dtype=torch.int32)
+    for i in range(steps):
+        T = T0 + i + 1
+        rs.rat_scan(s1, rand(B, Hkv, 1, D).to(dt), rand(B, Hkv, 1, D).to(dt), torch.sigmoid(rand(B, Hkv, 1, D) * 0.5 + 3), sk, sv, *stage, 0, 1)
+        length.add_(1)
+        rs.kv4_append(s, *stage, 0, length, None, 1, *four, meta)
+        q = (2 * rand(B, Hq, D)).to(dt)
+        rs.quest_select_decode(s, q, meta, T, K, 1, 1, idx, None, ws)
+        rs.kv4_attn_decode(s, q, *four, length, D ** -0.5, idx, None, 1, out, lse, ws)
+        torch.cuda.synchronize()
+        k, v = _values(*four[:2])[:, :, :T], _values(*four[2:])[:, :, :T]
+        pages = -(-T // P)
+        for p in range(pages):  # the bounds hold the values themselves
+            rows = k[:, :, p * P:p * P + P]
+            assert torch.equal(meta[:, :, p].double(), torch.stack([rows.amin(2), rows.amax(2)], 2))
+        for b in range(B):
+            for h in range(Hq):
+                t = (idx[b, h].cpu().numpy()[:, None] * P + np.arange(P)).ravel()
+                t = t[t < T]
+                assert len(set(t)) == len(t) and {0, T - 1} <= set(t)
+                o, z, _, a, most = M.attention(q[b, h:h + 1].double().cpu().numpy(), k[b, h // 2, t].cpu().numpy(), v[b, h // 2, t].cpu().numpy(), D ** -0.5)
+                e = M.rounding(most[0], len(t), D)
+                assert np.all(np.abs(out[b, h].double().cpu().numpy() - o[0]) <= (e + 2.0 ** -8) * a[0] + 2.0 ** -8 * np.abs(o[0]))
+    tally, pos = torch.zeros(B, Hkv, Tcap, device="cuda"), torch.zeros(B, Hkv, Tcap, device="cuda", dtype=torch.int32)
+    mark = torch.zeros(B, 2, device="cuda", dtype=torch.int32)
+    rs.kv4_attn_decode(s, q, *four, length, D ** -0.5, None, tally, 1, out, lse, ws)
+    rs.kv4_evict(s, *four, tally, pos, mark, length, 200, 4, 32, 0, ws)
+    rs.kv4_page_meta(s, *four[:2], length, length, Tcap, meta)
+    torch.cuda.synchronize()
+    assert length.tolist() == [200] * B
+    k2 = _values(*four[:2])[:, :, :200]
+    assert torch.equal(k2, k.gather(2, pos[:, :, :200, None].long().expand(-1, -1, -1, D)))  # a row is its position's token
+    for p in range(13):
+        rows = k2[:, :, p * P:min(200, p * P + P)]
+        assert torch.equal(meta[:, :, p].double(), torch.stack([rows.amin(2), rows.amax(2)], 2))
