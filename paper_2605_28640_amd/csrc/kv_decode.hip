@@ -52,6 +52,15 @@ __device__ __forceinline__ float quad_sum(float x)
     const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     return half_pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
+// over the wave, in every lane: within rows of 16 by rotations, then over the four rows
+__device__ __forceinline__ float wave_max(float x)
+{
+    x = fmaxf(x, dpp_f<0x128>(x));
+    x = fmaxf(x, dpp_f<0x124>(x));
+    x = fmaxf(x, dpp_f<0x122>(x));
+    return quad_max(fmaxf(x, dpp_f<0x121>(x)));
+}
+__device__ __forceinline__ float wave_sum(float x) { return quad_sum(group_sum<16>(x)); }
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 __device__ __forceinline__ int length_of(const DecodeParams &a, int b)
@@ -725,13 +734,9 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeParam
                     f32x4 none = {0.f, 0.f, 0.f, 0.f};
                     join(m, l, none, y.x, y.y, none);
                 }
-#pragma unroll
-                for (int k = kWave / 2; k >= 1; k >>= 1) {
-                    f32x4 none = {0.f, 0.f, 0.f, 0.f};
-                    const float m1 = shfl_xor_f(m, k), l1 = shfl_xor_f(l, k);
-                    join(m, l, none, m1, l1, none);
-                }
-                z = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+                const float top = wave_max(m);
+                l = wave_sum(l * __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top)));
+                z = l == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(l);
             }
             if (lane == 0) lse2[i] = z;
         }
