@@ -47,7 +47,8 @@
  *     words in the workspace from stale ones) and must be called, not replayed.
  *     rat_decode_step keeps its tag and the sequence length on the device and may be replayed, and
  *     so may all calls over a pool of pages (page_pool_*, page_copy, rat_state_copy,
- *     rat_append_paged, attn_paged): lengths, tables and counts live on the device.
+ *     rat_append_paged, attn_paged), of a 4-bit cache (kv4_*), attn_decode_tally and cache_evict:
+ *     lengths, tables and counts live on the device.
  */
 #ifndef RATSPARSE_H
 #define RATSPARSE_H
