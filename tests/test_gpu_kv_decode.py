@@ -146,7 +146,8 @@ def test_attention_and_tally(rs, kind, dtype, shape):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("shape", [(2, 4, 4, 64, 256, 16, 4, [256, 100]), (2, 8, 2, 128, 512, 32, 5, [512, 77]), (3, 4, 2, 128, 1024, 128, 3, [1000, 0, 130]),
-                                   (1, 4, 2, 64, 1024, 512, 2, [600]), (2, 32, 8, 128, 2048, 16, 40, [2047, 1999])])
+                                   (1, 4, 2, 64, 1024, 512, 2, [600]), (2, 32, 8, 128, 2048, 16, 40, [2047, 1999]),
+                                   (2, 40, 2, 128, 4096, 16, 200, [4096, 3001]), (3, 6, 3, 64, 2048, 64, 30, [2048, 0, 1333])])
 @pytest.mark.parametrize("shared", [False, True])
 def test_listed_pages(rs, dtype, shape, shared):
     B, Hq, Hkv, D, Tcap, P, K, lens = shape
