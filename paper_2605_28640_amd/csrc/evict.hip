@@ -9,7 +9,7 @@
 
 namespace rs {
 
-constexpr int kThreads = 1024, kWaves = kThreads / kWave;
+constexpr int kThreads = 1024;
 constexpr int kFewGo = 8;       // up to so many dropped rows are looked for one by one
 constexpr int kMovedHere = 64;  // up to so many rows are moved by the workgroup that chose them
 constexpr int kTurn = 256;      // rows that a wave looks at together
@@ -65,6 +65,7 @@ __device__ __forceinline__ void move_all(const EvictParams &a, int bh, int known
 __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan_i(x), kWave - 1); }
 
 // inclusive sums over the waves: `before` gets what the waves before this one hold, the return value is all.  lds: not in use by an earlier call
+template <int WAVES>
 __device__ __forceinline__ int wave_offsets(int x, int *lds, int &before)
 {
     const int wave = threadIdx.x / kWave;
@@ -73,7 +74,7 @@ __device__ __forceinline__ int wave_offsets(int x, int *lds, int &before)
     int sum = 0;
     before = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         if (w == wave) before = sum;
         sum += lds[w];
     }
@@ -90,15 +91,16 @@ __device__ __forceinline__ uint32_t wave_reduce(uint32_t x, F f)
 
 // Keys are looked at several times: from LDS, where HELD of them fit, or (0) from memory.  A wave takes neighbouring rows, 256 a turn, four neighbours
 // a thread.  (Keys in registers instead, 32 a thread, made loops of 32 copies and spilled: 36 us for 16384 rows of 32 heads, 57 from memory.)
-template <int HELD>
-__global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParams a)
+template <int HELD, int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams a)
 {
+    constexpr int WAVES = THREADS / kWave, EACH = kBins / THREADS;  // bins a thread
     __shared__ __attribute__((aligned(16))) uint32_t held[HELD > 0 ? HELD : 4];
     __shared__ __attribute__((aligned(16))) uint32_t hist[kBins][kCopies];
-    __shared__ int lds[3][kWaves];
-    __shared__ __attribute__((aligned(16))) int4 counts[kWaves];
+    __shared__ int lds[3][WAVES];
+    __shared__ __attribute__((aligned(16))) int4 counts[WAVES];
     __shared__ int found[2];
-    __shared__ uint32_t least[2][kWaves][2];
+    __shared__ uint32_t least[2][WAVES][2];
     __shared__ int32_t few_from[kMovedHere], few_to[kMovedHere];
     const int bh = blockIdx.x, b = bh / a.Hkv, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int L = min(a.len[b], a.Tcap);
@@ -113,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
     int32_t *const pos = a.pos + (long)bh * a.Tcap;
     uint32_t *const keys = HELD > 0 ? held : a.keys + bh * a.key_row;
     auto position = [&](int t) { return t < known ? pos[t] : before + (t - known); };
-    const int turns = (L + kWaves * kTurn - 1) / (kWaves * kTurn), from = min(L, wave * turns * kTurn), to = min(L, from + turns * kTurn);
+    const int turns = (L + WAVES * kTurn - 1) / (WAVES * kTurn), from = min(L, wave * turns * kTurn), to = min(L, from + turns * kTurn);
     // ---- the keys; rows up to a whole turn that there are not stay ----
     constexpr int AHEAD = 16;  // loads of a thread on their way together
     for (int t0 = from; t0 < to; t0 += AHEAD * kWave) {
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
             if (t0 + i / 4 * kTurn < to) keys[t] = k;
         }
     }
-    for (int i = threadIdx.x; i < kBins * kCopies; i += kThreads) (&hist[0][0])[i] = 0;
+    for (int i = threadIdx.x; i < kBins * kCopies; i += THREADS) (&hist[0][0])[i] = 0;
     __syncthreads();
     auto load4 = [&](int t0) { return *reinterpret_cast<const uint4 *>(keys + t0 + 4 * lane); };
     int n_movers;
@@ -158,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
             __syncthreads();
             uint32_t gk = kStays, gt = 0;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const uint32_t x = least[i & 1][w][0], t = least[i & 1][w][1];
                 if (x < gk || (x == gk && t > gt)) gk = x, gt = t;
             }
@@ -184,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
             for (int j = 0; j < kFewGo; ++j) stays &= gone[j] != t, rank += gone[j] >= a.keep && gone[j] < t;
             if (stays) few_from[(int)threadIdx.x - rank] = t;
         }
-        for (int t = known + threadIdx.x; t < a.keep; t += kThreads) {
+        for (int t = known + threadIdx.x; t < a.keep; t += THREADS) {
             bool hole = false;
 #pragma unroll
             for (int i = 0; i < kFewGo; ++i) hole |= gone[i] == t;
@@ -205,11 +207,11 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
                     if (pass == 0 || (v[c] >> (shift + bits)) == (prefix >> (shift + bits))) atomicAdd(&hist[(v[c] >> shift) & ((1u << bits) - 1u)][lane % kCopies], 1u);
             }
             __syncthreads();
-            // the bins from the top, two a thread, which leaves them empty for the next pass
-            int n[2], sum = 0;
+            // the bins from the top, EACH a thread, which leaves them empty for the next pass
+            int n[EACH], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                uint32_t *const bin = hist[kBins - 1 - (2 * threadIdx.x + i)];
+            for (int i = 0; i < EACH; ++i) {
+                uint32_t *const bin = hist[kBins - 1 - (EACH * threadIdx.x + i)];
                 n[i] = 0;
 #pragma unroll
                 for (int c = 0; c < kCopies; ++c) n[i] += (int)bin[c], bin[c] = 0;
@@ -217,11 +219,11 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
             }
             const int incl = wave_scan_i(sum);
             int above;
-            wave_offsets(__builtin_amdgcn_readlane(incl, kWave - 1), lds[pass], above);
+            wave_offsets<WAVES>(__builtin_amdgcn_readlane(incl, kWave - 1), lds[pass], above);
             above += incl - sum;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (above < left && above + n[i] >= left) found[0] = kBins - 1 - (2 * threadIdx.x + i), found[1] = left - above;
+            for (int i = 0; i < EACH; ++i) {
+                if (above < left && above + n[i] >= left) found[0] = kBins - 1 - (EACH * threadIdx.x + i), found[1] = left - above;
                 above += n[i];
             }
             __syncthreads();
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
         __syncthreads();
         int eq = 0, holes = 0, movers = 0, e = 0;
         n_movers = 0;
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const int4 c = counts[w];
             if (w == wave) eq = e, movers = n_movers;
             const int f = min(L, w * turns * kTurn), before_keep = max(0, min(a.keep, min(L, f + turns * kTurn)) - f);
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictParam
     }
     __syncthreads();
     const bool here = n_movers <= kMovedHere;
-    if (here) move_all(a, bh, known, before, few_from, few_to, n_movers, threadIdx.x, kThreads);
+    if (here) move_all(a, bh, known, before, few_from, few_to, n_movers, threadIdx.x, THREADS);
     if (threadIdx.x == 0) {
         a.count[bh] = make_int4(here ? 0 : n_movers, known, before, 0);
         // the last of the sequence's workgroups, all of which have read its length by now
@@ -358,10 +360,13 @@ static int evict_run(const rs_shape *s, const MovedRows &m, float *tally, int32_
     const int BH = s->B * s->Hkv;
     const EvictParams a{tally, pos, mark, len, (int4 *)(w + x.count), (uint32_t *)ws + kCtrlUnit0, (int32_t *)(w + x.from), (int32_t *)(w + x.to), (uint32_t *)(w + x.keys),
                         x.most, x.key_row, m, s->Hkv, s->Tcap, keep, first, recent, slack};
-    if (s->Tcap <= 8704) evict_select_kernel<8704><<<BH, kThreads, 0, stream>>>(a);
-    else if (s->Tcap <= 17408) evict_select_kernel<17408><<<BH, kThreads, 0, stream>>>(a);
-    else if (s->Tcap <= kMostHeld) evict_select_kernel<kMostHeld><<<BH, kThreads, 0, stream>>>(a);
-    else evict_select_kernel<0><<<BH, kThreads, 0, stream>>>(a);
+    // Short caches of more heads than compute units: four waves a head, of which a compute unit holds three at once.  1504 heads of 119 rows, 72 kept:
+    // 33 us, 57 with 16 waves; 500 rows less one: 24, 41; 2000, half kept: 211, 230.  With fewer heads the 16 waves win: 256 heads of 2000 rows 39 to 41.
+    if (s->Tcap <= 2304 && BH > 256) evict_select_kernel<2304, 256><<<BH, 256, 0, stream>>>(a);
+    else if (s->Tcap <= 8704) evict_select_kernel<8704, kThreads><<<BH, kThreads, 0, stream>>>(a);
+    else if (s->Tcap <= 17408) evict_select_kernel<17408, kThreads><<<BH, kThreads, 0, stream>>>(a);
+    else if (s->Tcap <= kMostHeld) evict_select_kernel<kMostHeld, kThreads><<<BH, kThreads, 0, stream>>>(a);
+    else evict_select_kernel<0, kThreads><<<BH, kThreads, 0, stream>>>(a);
     if (x.most <= kMovedHere) return launch_status();  // no call on this cache has more to move
     // about 2048 workgroups, and not more than have 4 KB to move
     long parts = (2048 + BH - 1) / BH, need = (x.most * m.bytes[0] + 4095) / 4096;

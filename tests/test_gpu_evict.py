@@ -87,6 +87,9 @@ CASES = [  # B, Hkv, D, Tcap, lengths, keep, first, recent, slack
     (1, 2, 64, 12000, [11999], 700, 0, 3, 0),
     (5, 1, 64, 2000, [1999, 1995, 1991, 1992, 2000], 1991, 5, 1986, 0),   # up to nine rows go, of hardly more that may
     (2, 2, 64, 34816, [34816, 34815], 34808, 0, 0, 0),
+    (9, 30, 64, 130, [130, 0, 66, 65, 64, 73, 74, 129, 1], 65, 3, 7, 0),   # more heads than compute units
+    (2, 131, 64, 2304, [2304, 2301], 1030, 3, 70, 0),
+    (3, 90, 64, 2305, [2305, 1025, 2049], 1024, 0, 1, 0),
 ]
 
 
