@@ -524,7 +524,8 @@ int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache,
  * rows are not in the order of their positions, which attention does not ask for.
  *   pos  [B, Hkv, Tcap] int32, in/out: position of the token in each row;  mark [B, 2] int32, in/out: the rows whose position is on record, the tokens
  *        that the sequence has had.  Zero mark (only it) when a sequence begins: rows that come after those on record get the positions
- *        that follow, and pos is written only here.
+ *        that follow, and pos is written only here.  (Where a pos of other contents repeats positions, so that more than n_keep rows
+ *        have to stay, the first n_keep of those do.)
  *   1 <= n_keep <= Tcap; n_first + n_recent <= n_keep
  * Quest bounds of a cache that has given up rows are formed anew (quest_page_meta, kv4_page_meta). */
 size_t cache_evict_workspace_bytes(const rs_shape *s, int32_t n_keep);

@@ -89,6 +89,7 @@ __device__ __forceinline__ uint32_t wave_reduce(uint32_t x, F f)
     return x;
 }
 
+// (Positions that repeat, of which more than `keep` rows could have to stay: the first `keep` of those do.)
 // Keys are looked at several times: from LDS, where HELD of them fit, or (0) from memory.  A wave takes neighbouring rows, 256 a turn, four neighbours
 // a thread.  (Keys in registers instead, 32 a thread, made loops of 32 copies and spilled: 36 us for 16384 rows of 32 heads, 57 from memory.)
 template <int HELD, int THREADS>
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams
         for (int i = 0; i < kFewGo; ++i) {
             gone[i] = 0x7fffffff;
             if (i >= n_go) continue;
-            // the smallest key, and of equal ones the last row (never a kStays: more rows than n_go are not protected)
+            // the smallest key, and of equal ones the last row (there is one unless positions repeat, see below)
             uint32_t k = kStays;
             int at = -1;
             for (int t0 = from; t0 < to; t0 += kTurn) {
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams
                 const uint32_t x = least[i & 1][w][0], t = least[i & 1][w][1];
                 if (x < gk || (x == gk && t > gt)) gk = x, gt = t;
             }
-            gone[i] = (int)gt - 1;
+            if (gt > 0) gone[i] = (int)gt - 1;
             if (gone[i] >= from && gone[i] < to) keys[gone[i]] = kStays;  // (its own wave, which alone looks at it)
         }
         // every thread has all of them: thread i works out the i-th hole and the i-th mover
@@ -195,7 +196,8 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams
     } else {
         // ---- the keep-th largest key ----
         uint32_t prefix = 0;
-        int left = a.keep + (kTurn - 1 - (L + kTurn - 1) % kTurn);  // of the keys that begin with the prefix, the left-th largest (rows that there are not count in)
+        const int no_rows = kTurn - 1 - (L + kTurn - 1) % kTurn;
+        int left = a.keep + no_rows;  // of the keys that begin with the prefix, the left-th largest (rows that there are not count in)
 #pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
@@ -230,6 +232,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams
             prefix |= (uint32_t)found[0] << shift;
             left = found[1];
         }
+        if (prefix == kStays) left -= no_rows;  // no rows but those that have to stay
         // Keys above the prefix stay, and of those equal to it the first `left`.  How many there are of both, before row `keep` and behind it, wave by wave:
         // where each wave's holes (rows before `keep` that go) and movers (rows behind it that stay) come.
         int4 mine = make_int4(0, 0, 0, 0);

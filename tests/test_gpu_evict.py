@@ -108,6 +108,22 @@ def test_evict(rs, four, dtype, case, tally):
 
 
 @pytest.mark.parametrize("four", [True, False])
+@pytest.mark.parametrize("B,Hkv,Tcap,L,keep", [(2, 2, 300, 300, 293), (2, 2, 300, 300, 40), (2, 2, 300, 299, 150), (1, 1, 35000, 34999, 900), (9, 30, 200, 193, 20),
+                                               (9, 30, 200, 200, 192)])
+@pytest.mark.parametrize("share", [1.0, 0.7])
+def test_positions_that_repeat(rs, four, B, Hkv, Tcap, L, keep, share):
+    """Positions cleared by mistake, so that more rows than n_keep have to stay: the first of them do, and nothing else is written."""
+    say("repeat", four, B, Hkv, Tcap, L, keep, share)
+    x = State(rs, four, "bf16", B, Hkv, 64, Tcap, [L] * B, seed=1)
+    r = np.random.default_rng(2)
+    x.pos.copy_(torch.from_numpy(np.where(r.random((B, Hkv, Tcap)) < share, 0, 20).astype(np.int32)))
+    x.mark[:] = L
+    want, _ = x.expect(x.copies(), keep, 1, 0, 0)
+    x.call(keep, 1, 0, 0)
+    x.check(want)
+
+
+@pytest.mark.parametrize("four", [True, False])
 def test_again_and_again(rs, four):
     """Sequences that grow by different numbers and give up rows as they go, positions and budgets that change among it, in a replayed graph too."""
     B, Hkv, D, Tcap = 3, 2, 64, 200
