@@ -507,6 +507,8 @@ def kv4_attn_decode(s, q, k4, k4_scale, v4, v4_scale, len, scale, idx, tally, n_
     """idx: [B, Hq or Hkv, K] pages or None."""
     if _calls().kv4_attn_decode(s, q, k4, k4_scale, v4, v4_scale, len, scale, idx, tally, n_fresh, out, lse_out, ws):
         return
+    if idx is not None and idx.numel() == 0:  # its address is null: not to be taken for no list
+        raise RatsparseError("a list of no pages")
     H, K = (idx.shape[1], idx.shape[2]) if idx is not None and idx.dim() == 3 else (0, 0)
     rows = (s.B, s.Hq)
     _check(load().kv4_attn_decode(ctypes.byref(s), _need(q, _type(s), *rows, s.D), *_four(s, k4, k4_scale, v4, v4_scale), _need(len, torch.int32, s.B),

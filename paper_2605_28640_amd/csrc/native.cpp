@@ -485,6 +485,7 @@ PyObject *py_kv4_attn_decode(PyObject *, PyObject *const *a, Py_ssize_t na)
     const float scale = x.real(7);
     const int64_t H = a[8] == Py_None ? 0 : x.size(8, 1), K = a[8] == Py_None ? 0 : x.size(8, 2);
     const int32_t *idx = x.ints(8, {s.B, H, K});
+    if (a[8] != Py_None && !idx) x.refuse();  // (an empty tensor's address: not to be taken for no list)
     float *tally = per_row(x, s, 9);
     const int fresh = (int)x.integer(10);
     void *out = x.typed(11, type_of(s), {s.B, s.Hq, s.D});

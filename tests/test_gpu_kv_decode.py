@@ -390,3 +390,15 @@ def test_quest_over_a_4_bit_cache(rs):
     for p in range(13):
         rows = k2[:, :, p * P:min(200, p * P + P)]
         assert torch.equal(meta[:, :, p].double(), torch.stack([rows.amin(2), rows.amax(2)], 2))
+
+
+def test_a_list_of_no_pages_is_refused(rs):
+    s = rs.make_shape(1, 2, 2, 64, 64, 16, torch.bfloat16)
+    four = [torch.zeros(1, 2, 64, n, dtype=torch.uint8, device="cuda") for n in (32, 2, 32, 2)]
+    length, q = torch.full((1,), 64, dtype=torch.int32, device="cuda"), torch.zeros(1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7)
+    ws = rs.Workspace(rs.kv4_attn_decode_workspace_bytes(s, 0, 0, False))
+    with pytest.raises(rs.RatsparseError, match="no pages"):
+        rs.kv4_attn_decode(s, q, *four, length, 0.1, torch.zeros(1, 2, 0, dtype=torch.int32, device="cuda"), None, 0, out, None, ws)
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())

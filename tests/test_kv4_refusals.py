@@ -141,6 +141,9 @@ def test_binding_looks_at_types_and_shapes():
         rs.cache_evict(s, z(2, 2, 32, 32, dtype=bf), None, None, None, None, ln, 4, 0, 0, 0, ws)
     with pytest.raises(wrong):
         rs.kv4_evict(s, four[1], *four[1:], None, None, None, ln, 4, 0, 0, 0, ws)
+    for shape in ((2, 2, 0), (2, 0, 4)):  # a list of no pages is not the same as none
+        with pytest.raises(wrong, match="no pages"):
+            rs.kv4_attn_decode(s, z(2, 4, 64, dtype=bf), *four, ln, 0.1, z(*shape, dtype=i32), None, 1, z(2, 4, 64, dtype=bf), None, ws)
     with pytest.raises(AssertionError):  # not on a device
         rs.kv4_page_meta(s, four[0], four[1], ln, None, 1, None)
 
