@@ -497,7 +497,7 @@ int32_t kv4_fetch(const rs_shape *s, const uint8_t *k4, const uint8_t *k4_scale,
  *   tally   [B, Hkv, Tcap] float32 or NULL (and with idx NULL): see attn_decode_tally
  *   out     [B, Hq, D] dtype, lse_out [B, Hq] float32 or NULL.  A row that sees nothing, or only scores of -inf, gets zeros and a
  *           log-sum-exp of -inf
- * The weights are rounded to bfloat16 for the product with bfloat16 results (half a step of 2^-8 each), and kept in float32 for float32 ones.
+ * Scores, weights and sums are float32 for results of either type, which are rounded once.
  * The order of every sum follows from the lengths: the same call gives the same bits. */
 size_t kv4_attn_decode_workspace_bytes(const rs_shape *s, int32_t H_idx, int32_t K, int32_t with_tally);
 int32_t kv4_attn_decode(const rs_shape *s, const void *q, const uint8_t *k4, const uint8_t *k4_scale, const uint8_t *v4, const uint8_t *v4_scale,
@@ -512,7 +512,7 @@ int32_t kv4_attn_decode(const rs_shape *s, const void *q, const uint8_t *k4, con
  *   tally [B, Hkv, Tcap] float32, in/out:  tally[b, h, t] += sum over the query heads of KV head h of their attention weight of row t, t < len[b].
  *         Rows len - n_fresh .. len - 1 are new since the last call: theirs is set, not added to (n_fresh = 1 in a decode loop).  Rows
  *         from len on are left as they were.  A prompt's tally may start from zeros or from votes_out of snapkv_compress.
- * float32 caches are attended in float32 throughout, of bfloat16 ones as kv4_attn_decode says. */
+ * Scores, weights and sums are float32 for caches of either type; a bfloat16 result is rounded once. */
 size_t attn_decode_tally_workspace_bytes(const rs_shape *s);
 int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache, const void *v_cache, const int32_t *len, float scale, float *tally,
                           int32_t n_fresh, void *out, float *lse_out, void *ws, size_t ws_bytes, void *stream);
