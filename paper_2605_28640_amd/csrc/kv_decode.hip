@@ -238,10 +238,10 @@ struct StepRows<true, ST, D> {
             for (int j = 0; j < 8; ++j) {
                 float rest = real ? x[j] : 0.f;
 #pragma unroll
-                for (int n = 0; n < TERMS; ++n) {  // float32 as the sum of three bfloat16 numbers: all of its 24 bits
-                    const __bf16 part = (__bf16)rest;
-                    qf[n][kk][j] = part;
-                    rest -= (float)part;
+                for (int n = 0; n < TERMS; ++n) {  // float32 as the sum of three bfloat16 numbers, all of its 24 bits: each cuts off (rounding up could make an infinity)
+                    const uint32_t u = __float_as_uint(rest);
+                    qf[n][kk][j] = __builtin_bit_cast(__bf16, (unsigned short)(u >> 16));
+                    rest = (u & 0x7fffffffu) == 0x7f800000u ? 0.f : rest - __uint_as_float(u & 0xffff0000u);  // (nothing is left of an infinity)
                 }
             }
         }

@@ -1,4 +1,5 @@
-"""One token's attention over caches in 4 bits, bfloat16 and float32: weights keep all of their bits.  Against a computation in 64 bits.
+"""One token's attention over caches in 4 bits, bfloat16 and float32: weights keep all of their bits, very large and
+infinite queries.  Against a computation in 64 bits.
 
 What is allowed: a score's rounding makes a weight off by M.rounding (relative to it, so the result by that times sum p |v|); a bfloat16 result is
 rounded once (2^-8 of it)."""
@@ -57,3 +58,36 @@ def test_weights_of_listed_pages_keep_their_bits(rs, dtype, shared, K):
     idx = torch.from_numpy(idx).cuda()
     d.run(tally=False, idx=idx)
     check(d, idx)
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Tcap,L", [(300, 300), (5000, 4999)])  # one launch, two
+@pytest.mark.parametrize("listed", [False, True])
+def test_very_large_and_infinite_queries_of_a_4_bit_cache(rs, dtype, Tcap, L, listed):
+    """A finite query channel next to the end of its type's range counts as it is (rows have nothing there); one of -inf against positive values: the row sees nothing;
+    one of +inf: NaN, as the formula has it."""
+    say("large queries", dtype, Tcap, listed)
+    Tcap = -(-Tcap // 16) * 16
+    d = Decode(rs, "four", dtype, 3, 2, 2, 64, Tcap, [L] * 3, seed=13)
+    codes = d.cache[0]
+    codes[:, :, :, 5 // 2] = codes[:, :, :, 5 // 2] & 0x0F        # channel 5: 0
+    codes[:, :, :, 7 // 2] = codes[:, :, :, 7 // 2] & 0x0F | 0x20  # channel 7: 1 times the scale
+    four = [x.cpu().numpy() for x in d.cache]
+    d.k, d.v = (M.values(M.from_bytes(c), f) for c, f in zip(four[0::2], four[1::2]))
+    d.q[0, :, 5] = torch.finfo(d.q.dtype).max
+    d.q[0, 1, 5] *= -1
+    d.q[1, 0, 7] = -float("inf")
+    d.q[2, 0, 7] = float("inf")
+    d.tally.zero_()
+    idx = torch.arange(L // 16, dtype=torch.int32, device="cuda").repeat(3, 2, 1) if listed else None
+    d.run(tally=not listed, fresh=0, idx=idx)
+    assert (d.out[1, 0] == 0).all() and d.lse[1, 0] == -float("inf") and (d.tally[1, 0] == 0).all()
+    assert d.out[2, 0].isnan().all() and d.lse[2, 0].isnan()
+    for b, h in ((0, 0), (0, 1), (1, 1), (2, 1)):
+        n = L // 16 * 16 if listed else L
+        q = d.q[b, h:h + 1].double().cpu().numpy()
+        o, z, p, a, most = M.attention(q, d.k[b, h, :n], d.v[b, h, :n], d.scale)
+        e = M.rounding(most[0], n, 64)
+        assert np.all(np.abs(d.out[b, h].double().cpu().numpy() - o[0]) <= e * a[0] + last_rounding(d.out) * np.abs(o[0])), (b, h)
+        assert abs(float(d.lse[b, h]) - z[0]) <= e + 2.0 ** -22 * abs(z[0]), (b, h)
+        if not listed:
+            assert np.all(np.abs(d.tally[b, h, :n].double().cpu().numpy() - p[0]) <= e * p[0] + 2.0 ** -22 * p[0]), (b, h)
