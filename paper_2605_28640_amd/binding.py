@@ -477,6 +477,8 @@ def kv4_append(s, k, v, t_src, len, n_new, T_new, k4, k4_scale, v4, v4_scale, me
     """k, v [B, Hkv, T_src, D]: the new tokens are rows t_src .. t_src + T_new - 1."""
     if _calls().kv4_append(s, k, v, t_src, len, n_new, T_new, k4, k4_scale, v4, v4_scale, meta):
         return
+    if meta is not None and meta.numel() == 0:  # its address is null: not to be taken for no bounds
+        raise RatsparseError("bounds of no pages")
     T_src = k.shape[2] if k.dim() == 4 else 0
     src = (_type(s), s.B, s.Hkv, T_src, s.D)
     _check(load().kv4_append(ctypes.byref(s), _need(k, *src), _need(v, *src), T_src, t_src, _need(len, torch.int32, s.B), _need(n_new, torch.int32, s.B),

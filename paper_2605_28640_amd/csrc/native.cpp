@@ -432,7 +432,11 @@ struct Four {
 };
 uint8_t *bytes(Args &x, const rs_shape &s, int i, int channels) { return (uint8_t *)x.typed(i, at::kByte, {s.B, s.Hkv, s.Tcap, s.D / channels}); }
 Four four(Args &x, const rs_shape &s, int i) { return Four{bytes(x, s, i, 2), bytes(x, s, i + 1, 32), bytes(x, s, i + 2, 2), bytes(x, s, i + 3, 32)}; }
-void *bounds(Args &x, const rs_shape &s, int i) { return x.typed(i, type_of(s), {s.B, s.Hkv, s.P > 0 ? s.Tcap / s.P : 0, 2, s.D}); }
+void *bounds(Args &x, const rs_shape &s, int i)
+{
+    void *p = x.typed(i, type_of(s), {s.B, s.Hkv, s.P > 0 ? s.Tcap / s.P : 0, 2, s.D});
+    return p || x.a[i] == Py_None ? p : x.refuse();  // (an empty tensor's address: not to be taken for no bounds)
+}
 float *per_row(Args &x, const rs_shape &s, int i) { return (float *)x.typed(i, at::kFloat, {s.B, s.Hkv, s.Tcap}); }
 
 PyObject *py_kv4_append(PyObject *, PyObject *const *a, Py_ssize_t na)

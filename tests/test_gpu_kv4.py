@@ -236,3 +236,16 @@ def test_a_stream_of_many_pages_a_wave(rs, D, P, dtype):
     a.meta.fill_(3.0)
     rs.kv4_page_meta(a.s, a.dev[0], a.dev[1], a.len, ints(new), T, a.meta)
     assert torch.equal(a.meta, b.meta)
+
+
+def test_bounds_of_no_pages_are_refused(rs):
+    s = rs.make_shape(1, 2, 2, 64, 32, 64, torch.bfloat16)  # a page is longer than the cache
+    four = [torch.full((1, 2, 32, n), 7, dtype=torch.uint8, device="cuda") for n in (32, 2, 32, 2)]
+    rows, length = torch.ones(1, 2, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.full((1,), 4, dtype=torch.int32, device="cuda")
+    with pytest.raises(rs.RatsparseError, match="no pages"):
+        rs.kv4_append(s, rows, rows, 0, length, None, 4, *four, torch.zeros(1, 2, 0, 2, 64, dtype=torch.bfloat16, device="cuda"))
+    torch.cuda.synchronize()
+    assert all(bool((x == 7).all()) for x in four)
+    rs.kv4_append(s, rows, rows, 0, length, None, 4, *four, None)
+    torch.cuda.synchronize()
+    assert bool((four[0][:, :, :4] != 7).all())

@@ -161,3 +161,11 @@ def test_the_model():
     pairs, at = M.evict([0, 1, np.nan, 7], [3, 0, 9, 0], 3, 10, 4, 2, 1, 1, 0)  # positions 3, 0, 9, 10: the first and the newest
     assert pairs == [(3, 0)] and at == [10, 0]
     assert M.evict([1.0] * 5, [0] * 5, 0, 0, 5, 4, 0, 0, 1) is None
+
+
+def test_bounds_of_no_pages_are_not_the_same_as_none():
+    s = rs.make_shape(2, 4, 2, 64, 32, 64, torch.bfloat16)  # a page is longer than the cache
+    z, bf = torch.zeros, torch.bfloat16
+    four = [z(2, 2, 32, n, dtype=torch.uint8) for n in (32, 2, 32, 2)]
+    with pytest.raises(rs.RatsparseError, match="no pages"):
+        rs.kv4_append(s, z(2, 2, 4, 64, dtype=bf), z(2, 2, 4, 64, dtype=bf), 0, z(2, dtype=torch.int32), None, 4, *four, z(2, 2, 0, 2, 64, dtype=bf))
