@@ -468,8 +468,9 @@ int32_t attn_paged(const rs_shape *s, const rs_pool *p, const void *q, const voi
  * and of rows that go in or come out.
  * Every sequence has a length of its own, in device memory (the library only reads it, but for cache_evict and kv4_evict):
  *   len [B] int32   tokens of the sequence, rows 0 .. len - 1; values above Tcap are taken as Tcap, below 0 as 0
- * All calls of this section and the next may be captured into a graph and replayed.  They take B Hkv <= 65535 and Tcap <= 2^30
- * (RS_UNSUPPORTED above), the attention B <= 1024; Hq <= 8160. */
+ * All calls of this section and the next may be captured into a graph and replayed.  RS_UNSUPPORTED above these limits: Tcap <= 2^30, Hq <= 8160;
+ * append, bounds, fetch and eviction B Hkv <= 65535; eviction B <= 16320 (a control word each); the attention B <= 1024, 2 10^9 units of 16 tokens over all
+ * its tiles (a KV head's, or list's, up to 16 queries of a sequence), and B Hq + B Hkv (Tcap / 1024 + 1) < 2^24. */
 
 /* The last n_new[b] tokens of sequence b (positions len - n_new .. len - 1) go into the cache.
  *   k, v  [B, Hkv, T_src, D] dtype   the i-th of them is row t_src + i (a staging buffer or a whole cache, as rat_scan leaves it);

@@ -363,7 +363,7 @@ static int evict_run(const rs_shape *s, const MovedRows &m, float *tally, int32_
     const int BH = s->B * s->Hkv;
     const EvictParams a{tally, pos, mark, len, (int4 *)(w + x.count), (uint32_t *)ws + kCtrlUnit0, (int32_t *)(w + x.from), (int32_t *)(w + x.to), (uint32_t *)(w + x.keys),
                         x.most, x.key_row, m, s->Hkv, s->Tcap, keep, first, recent, slack};
-    // Short caches of more heads than compute units: four waves a head, of which a compute unit holds three at once.  1504 heads of 119 rows, 72 kept:
+    // Short caches of more heads than compute units: four waves a head, of which a compute unit holds six at once (46 registers, 26 KB of LDS; only one with 16 waves).  1504 heads of 119 rows, 72 kept:
     // 33 us, 57 with 16 waves; 500 rows less one: 24, 41; 2000, half kept: 211, 230.  With fewer heads the 16 waves win: 256 heads of 2000 rows 39 to 41.
     if (s->Tcap <= 2304 && BH > 256) evict_select_kernel<2304, 256><<<BH, 256, 0, stream>>>(a);
     else if (s->Tcap <= 8704) evict_select_kernel<8704, kThreads><<<BH, kThreads, 0, stream>>>(a);

@@ -808,8 +808,8 @@ static int check_decode(const rs_shape *s, int H, int K)
     if (listed && ((H != s->Hq && H != s->Hkv) || K < 1 || K > s->Tcap / s->P)) return RS_INVALID_ARG;
     if (s->B > kMaxB || s->Tcap > (1 << 30)) return RS_UNSUPPORTED;
     const double heads = listed ? H : s->Hkv, tiles = heads * ((s->Hq / heads + kQ - 1) / kQ), tokens = listed ? (double)K * s->P : s->Tcap;
-    // units of the line, and workgroups of the second launch
-    if (s->B * tiles * (tokens / 16 + 1) > 2e9 || (double)s->B * s->Hq + (double)s->B * s->Hkv * (s->Tcap / 1024. + 1) > 2e9) return RS_UNSUPPORTED;
+    // units of the line, and workgroups of the second launch (2^32 threads are more than a launch takes)
+    if (s->B * tiles * (tokens / 16 + 1) > 2e9 || (double)s->B * s->Hq + (double)s->B * s->Hkv * (s->Tcap / 1024. + 1) >= 16777216.) return RS_UNSUPPORTED;
     return RS_OK;
 }
 

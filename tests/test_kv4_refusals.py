@@ -169,3 +169,14 @@ def test_bounds_of_no_pages_are_not_the_same_as_none():
     four = [z(2, 2, 32, n, dtype=torch.uint8) for n in (32, 2, 32, 2)]
     with pytest.raises(rs.RatsparseError, match="no pages"):
         rs.kv4_append(s, z(2, 2, 4, 64, dtype=bf), z(2, 2, 4, 64, dtype=bf), 0, z(2, dtype=torch.int32), None, 4, *four, z(2, 2, 0, 2, 64, dtype=bf))
+
+
+def test_limits():
+    lib = rs.load()
+    # an eviction's sequences: a control word each
+    for name in ("cache_evict", "kv4_evict"):
+        assert call(name, _shape(B=16320, Hq=1, Hkv=1), nb=0) == 3 and call(name, _shape(B=16321, Hq=1, Hkv=1)) == 2, name
+    assert lib.cache_evict_workspace_bytes(_shape(B=16320, Hq=1, Hkv=1), 40) > 0 == lib.cache_evict_workspace_bytes(_shape(B=16321, Hq=1, Hkv=1), 40)
+    # the attention's second launch: a workgroup a query, and 1024 rows of a KV head
+    for need in (lib.attn_decode_tally_workspace_bytes, lambda s: lib.kv4_attn_decode_workspace_bytes(s, 0, 0, 1)):
+        assert need(_shape(B=1, Hq=1600, Hkv=1600, Tcap=10 << 20)) > 0 == need(_shape(B=1, Hq=1700, Hkv=1700, Tcap=10 << 20))
