@@ -494,7 +494,8 @@ int32_t kv4_fetch(const rs_shape *s, const uint8_t *k4, const uint8_t *k4_scale,
 
 /* Attention of one token over the cache (Eq. 4): q [B, Hq, D] dtype over the tokens t < len[b], all of them or those of listed pages.
  *   idx     [B, H_idx, K] int32 or NULL (all tokens): pages, as quest_select_decode (H_idx = Hq) or quest_select_decode_group (H_idx = Hkv) list
- *           them; entries that name no page are skipped, each page at most once.  H_idx and K count for nothing without it
+ *           them; entries that name no page are skipped, each page at most once.  H_idx and K count for nothing without it.  (The selections
+ *           take one T_valid for the batch from the host, and are not replayed: a batch of different lengths is selected a sequence at a time)
  *   tally   [B, Hkv, Tcap] float32 or NULL (and with idx NULL): see attn_decode_tally
  *   out     [B, Hq, D] dtype, lse_out [B, Hq] float32 or NULL.  A row that sees nothing, or only scores of -inf, gets zeros and a
  *           log-sum-exp of -inf
@@ -512,7 +513,8 @@ int32_t kv4_attn_decode(const rs_shape *s, const void *q, const uint8_t *k4, con
  * Attention of one token over all rows, as sparse_attn_decode without a list, for sequences of len[b] tokens (see above), with the tally:
  *   tally [B, Hkv, Tcap] float32, in/out:  tally[b, h, t] += sum over the query heads of KV head h of their attention weight of row t, t < len[b].
  *         Rows len - n_fresh .. len - 1 are new since the last call: theirs is set, not added to (n_fresh = 1 in a decode loop).  Rows
- *         from len on are left as they were.  A prompt's tally may start from zeros or from votes_out of snapkv_compress.
+ *         from len on are left as they were.  A prompt's tally may start from zeros, or from the votes of snapkv_compress, which the caller copies:
+ *         row i < K_keep of kc_out has votes_out[b, h, idx_out[b, h, i]] (largest of its neighbours' window weights, no sum over the prompt).
  * Scores, weights and sums are float32 for caches of either type; a bfloat16 result is rounded once. */
 size_t attn_decode_tally_workspace_bytes(const rs_shape *s);
 int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache, const void *v_cache, const int32_t *len, float scale, float *tally,
@@ -528,7 +530,9 @@ int32_t attn_decode_tally(const rs_shape *s, const void *q, const void *k_cache,
  *        that follow, and pos is written only here.  (Where a pos of other contents repeats positions, so that more than n_keep rows
  *        have to stay, the first n_keep of those do.)
  *   1 <= n_keep <= Tcap; n_first + n_recent <= n_keep
- * Quest bounds of a cache that has given up rows are formed anew (quest_page_meta, kv4_page_meta). */
+ * Quest bounds of a cache that has given up rows are formed anew (quest_page_meta, kv4_page_meta).  The first n_first tokens are still its first rows, but
+ * the newest ones lie wherever rows were given up: n_local of the selections, which goes by rows, then protects the pages of the last rows, not of the newest
+ * tokens.  Where those have to be attended, list their pages by pos. */
 size_t cache_evict_workspace_bytes(const rs_shape *s, int32_t n_keep);
 int32_t cache_evict(const rs_shape *s, void *k_cache, void *v_cache, float *tally, int32_t *pos, int32_t *mark, int32_t *len, int32_t n_keep, int32_t n_first,
                     int32_t n_recent, int32_t n_slack, void *ws, size_t ws_bytes, void *stream);

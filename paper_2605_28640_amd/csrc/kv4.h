@@ -1,8 +1,8 @@
 // Rows in 4 bits: 32 neighbouring channels share a power of two 2^e (one byte, e + 127; 255: the group is NaN), a channel is one of
 // 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign, the lower of two channels in the low half of a byte.  These are the operand types
 // of the CDNA4 conversions: two channels of a row become a bfloat16 pair in one instruction, and exactly, since a value has two significant
-// bits.  (Checked against the definition over all bytes and the scales 2^-125 .. 2^125, and a million values rounded: no difference; an
-// infinite scale, which is what byte 255 gives, makes every value NaN.)
+// bits.  (The tests hold rows of every size of number, ties, both ends of the range, infinities and NaN against
+// the definition, byte for byte; an infinite scale, which is what byte 255 gives, makes every value NaN.)
 #pragma once
 
 #include "common.h"

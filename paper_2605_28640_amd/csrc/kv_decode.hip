@@ -76,7 +76,7 @@ __device__ __forceinline__ int product_over(int a, double b, double c) { return 
 
 // The line's shares, one a wave.  Of the workgroups on a CU the one that came first gets most of what the CU asks of memory: with equal shares of 4 x 32 heads
 // of 64K tokens the first 256 workgroups were done after 122 us, the others after 143 and 168.  So where three fit on a CU and every wave has
-// some steps to go, the shares are weighted (182 -> 172 us; two or four to a CU: no gain).
+// some steps to go, the shares are weighted (that call 185 -> 173 us, its 256 listed pages a head 26.9 -> 25.5; two or four to a CU: no gain).
 constexpr int kTurn = 256 * kWaves;                  // waves of a workgroup on every CU
 constexpr int kWeight[3] = {54, 43, 31};             // they add up to 128
 struct LineShares {
@@ -194,8 +194,8 @@ struct StepWhere {
 };
 
 // The weights of eight tokens as three bfloat16 operands whose sum they are, all 24 bits of them.  A term is what the ones before leave,
-// cut off after 8 bits: a mask, a difference, and a byte permute for two.  (With weights rounded to one bfloat16 term the first launch of 24 ragged sequences and that
-// of 256 listed pages a head take 1.1 us less of 39.7 and 25.7, the others nothing; but a result then has an error of its own besides its last rounding.)
+// cut off after 8 bits: a mask, a difference, and a byte permute for two.  (With weights rounded to one bfloat16 term 24 ragged sequences take 38.6 us instead of
+// 39.4 and 256 listed pages a head 24.7 instead of 25.6, 64K tokens 178 instead of 174; but a result then has an error of its own besides its last rounding.)
 __device__ __forceinline__ void split3(const f32x4 &p0, const f32x4 &p1, bf16x8 (&out)[3])
 {
     uint32_t w[3][4];
@@ -786,8 +786,8 @@ static DecodeLayout decode_layout(const rs_shape *s, bool four, int H, int K, bo
     x.groups = (int)(need < most ? need : most);
     x.three = need >= most && most == 3 * 256;
     // A workgroup a tile, four of its units at a time, against even shares and a second launch (32 over 8 heads of 128 channels, tiles of 8 / 16 / 32 units, us):
-    // 32 tiles, 4 bits 7.9 / 11.8 / 19.6 against 10.3 / 10.5 / 11.2, bfloat16 7.9 / 10.3 / 15.8 against 10.5 / 10.6 / 11.4; 512 tiles, 4 bits 10.7 / 16.8 / 27.3
-    // against 19.8 / 24.5 / 34.4, bfloat16 14.2 / 25.0 / 51.9 against 19.6 / 30.2 / 55.0.  Longer tiles would gain too where all are alike, and lose much where they are not.
+    // 32 tiles, 4 bits 7.1 / 11.1 / 19.1 against 10.7 / 11.0 / 11.6, bfloat16 with tally 8.4 / 11.7 / 19.0 against 11.1 / 11.4 / 12.0; 512 tiles, 4 bits 11.7 / 18.0 / 30.0
+    // against 20.7 / 25.7 / 36.9, bfloat16 with tally 15.6 / 26.3 / 54.9 against 20.6 / 32.7 / 58.6.  Longer tiles would gain too where all are alike, and lose much where they are not.
     x.solo = (tile <= 16 || (tile <= 32 && tiles >= 256)) && G <= kQ;  // (of a tile that is all of a KV head, the tally is its own too)
     const size_t records = (size_t)2 * x.groups * kWaves * x.rows;
     x.z_row = tally ? (s->Tcap + kUnit - 1) / kUnit * kUnit : 0;
