@@ -196,14 +196,19 @@ struct StepWhere {
 // The weights of eight tokens as three bfloat16 operands whose sum they are, all 24 bits of them.  A term is what the ones before leave,
 // cut off after 8 bits: a mask, a difference, and a byte permute for two.  (With weights rounded to one bfloat16 term 24 ragged sequences take 38.6 us instead of
 // 39.4 and 256 listed pages a head 24.7 instead of 25.6, 64K tokens 178 instead of 174; but a result then has an error of its own besides its last rounding.)
+// ROWS: the values may be infinite (in 4 bits they are not), and 0 times that is NaN: a term for which nothing is left is 2^-30 of the weight instead, two of them
+// a 32nd of its last bit (of weights below 2^-96 nothing is left of that either).
+template <bool ROWS>
 __device__ __forceinline__ void split3(const f32x4 &p0, const f32x4 &p1, bf16x8 (&out)[3])
 {
     uint32_t w[3][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float a = i < 2 ? p0[2 * i] : p1[2 * i - 4], b = i < 2 ? p0[2 * i + 1] : p1[2 * i - 3];
+        const float least_a = a * 0x1p-30f, least_b = b * 0x1p-30f;
 #pragma unroll
         for (int n = 0; n < 3; ++n) {
+            if (ROWS && n > 0) a = fmaxf(a, least_a), b = fmaxf(b, least_b);
             const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
             w[n][i] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);  // the upper halves, a's below
             if (n < 2) a -= __uint_as_float(ua & 0xffff0000u), b -= __uint_as_float(ub & 0xffff0000u);
@@ -309,15 +314,15 @@ struct StepRows<true, ST, D> {
                     *reinterpret_cast<uint4 *>(tile + row * ROW + (((lane & 3) * NK + c) ^ swizzle(row)) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-            product32<D>(tile, p[2 * half], p[2 * half + 1], o, l16, lg);
+            product32<D, false>(tile, p[2 * half], p[2 * half + 1], o, l16, lg);
         }
     }
     // 32 tokens, whose values are in the tile
-    template <int DD>
+    template <int DD, bool ROWS>
     __device__ __forceinline__ static void product32(const char *tile, const f32x4 &p0, const f32x4 &p1, f32x4 (&o)[DD / 16], int l16, int lg)
     {
         bf16x8 pf[3];
-        split3(p0, p1, pf);
+        split3<ROWS>(p0, p1, pf);
         const int r = 4 * lg + (l16 >> 2);
         const uint32_t at = (uint32_t)(r * 2 * DD + ((((l16 & 3) >> 1) ^ swizzle(r)) * 16) + 8 * (l16 & 1));
 #pragma unroll
@@ -399,7 +404,7 @@ struct StepRows<false, ST, D> {
                 *reinterpret_cast<f32x4 *>(tile + row * ROW + ((lane % CR) ^ swizzle(row)) * 16) = vx[h][i];
             }
         if constexpr (BF) {
-            StepRows<true, ST, D>::template product32<D>(tile, p[0], p[1], o, l16, lg);
+            StepRows<true, ST, D>::template product32<D, true>(tile, p[0], p[1], o, l16, lg);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -242,3 +242,31 @@ def test_tallies_of_two_graphs_that_share_a_workspace(rs, kind, dtype):
             d.check(before, 0)
             if turn == 1:
                 other.run(fresh=0, ws=ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Tcap,L", [(64, 1), (300, 300), (5000, 4999)])
+@pytest.mark.parametrize("big", [0.0, 1.0])
+def test_infinite_values(rs, dtype, Tcap, L, big):
+    """An infinite value with a weight, also one of few bits (rows of equal scores), is an infinite result, as the formula has it; of both signs: NaN."""
+    say("infinite values", dtype, Tcap, L, big)
+    d = Decode(rs, "rows", dtype, 2, 4, 2, 64, Tcap, [L, L], seed=16, big=big)
+    t = L // 2
+    for h in (0, 1):
+        d.cache[1][0, h, t, 3] = float("inf")
+        d.cache[1][0, h, L - 1, 60] = -float("inf")
+        d.v[0, h, t, 3] = d.v[0, h, L - 1, 60] = 0
+    if L > 1:
+        d.cache[1][0, 1, t + 1, 3] = -float("inf")
+        d.v[0, 1, t + 1, 3] = 0
+    before = d.tally.clone()
+    d.run()
+    a, b = d.out[0, :2].clone(), d.out[0, 2:].clone()
+    assert (a[:, 3] == float("inf")).all() and (a[:, 60] == -float("inf")).all() and (b[:, 60] == -float("inf")).all()
+    assert (b[:, 3].isnan() if L > 1 else b[:, 3] == float("inf")).all()
+    # the other channels, and all else, as ever
+    for c in (3, 60):
+        d.out[0, :, c] = 0
+        d.v[0, :, :, c] = 0
+    check(d)
+    assert d.lse.isfinite().all() and not d.tally.isnan().any() and torch.equal(d.tally[:, :, L:], before[:, :, L:])
